@@ -19,6 +19,7 @@
  *      ctc_collapse_tree, ctc_raw_tree
  *      tree_verify_attn, draft_layer_forward
  *      verify_head_argmax
+ *      calls of prefix_verify_attn that share a workspace
  *    Two calls of one of these lines race on it.  Every other call uses none.  (Ordering a call behind those
  *    whose outputs it reads is the caller's part, as everywhere.)
  *  - Row-major, innermost index last, no padding unless stated.  bf16 is the upper half of an IEEE
@@ -446,6 +447,104 @@ size_t ctc_loss_workspace_bytes(int B, int T, int Lmax);
 int ctc_loss(ctcspec_ctx* ctx, const float* logits, const int32_t* labels, const int32_t* label_len,
              const int32_t* frame_len, int B, int T, int Vp1, int Lmax, int32_t blank_id, void* workspace,
              size_t workspace_bytes, float* loss, float* grad);
+
+/*
+ * prefix_verify_attn - one attention layer of the verification pass (as tree_verify_attn) for a batch whose sequences
+ * continue ONE common prefix: a system prompt, a document that all of them ask about.  The prefix's keys and values exist
+ * once, are read once and are multiplied once for the rows of all sequences; behind them each sequence has its own cached
+ * rows and its token tree.  Heads may share keys (grouped heads): head h reads key head h / (H / H_kv).
+ *
+ *   keys(b, i) = the first prefix_len rows of the prefix + the ctx_len[b] cached rows + the tree nodes j < n_nodes[b] with
+ *                bit j of anc_mask row i set
+ *   lse[b,h,i]   = log sum_{j in keys} exp(scale * q[b,h,i,:] . key_j)
+ *   out[b,h,i,:] = sum_{j in keys} exp(scale * q[b,h,i,:] . key_j - lse[b,h,i]) * value_j
+ *
+ * A row that sees no key at all (no prefix, no cached row, an empty mask row) has out = 0 and lse = -inf.  Rows
+ * i >= n_nodes[b] are not written; n_nodes[b] may be 0 (a place of the batch that is not in use).  No positional encoding is
+ * applied.  The lengths are read on the device; those beyond their capacity count as the capacity, negative ones as 0.
+ * A value that is infinite or not a number reaches the rows that see its key and no other row; a score that is, likewise.
+ *
+ * dt            element type of q and of all keys and values
+ * q             [B,H,max_nodes,dh]
+ * k_prefix, v_prefix  [H_kv,prefix_cap,dh]; prefix_len [1] int32 device (0 is allowed; rows beyond are not read)
+ * k_cache, v_cache, kv_off, ctx_len, kv_cap   as for tree_verify_attn, with [H_kv][kv_cap][dh] per sequence
+ * k_tree, v_tree [B,H_kv,max_nodes,dh]
+ * n_nodes, anc_mask   as for tree_verify_attn
+ * scale         positive and finite
+ * workspace     device scratch of at least prefix_verify_attn_workspace_bytes(B, H, H_kv, dh, max_nodes) bytes, owned by the
+ *               caller, contents undefined afterwards; calls that share it must not overlap.  Bytes for some B and max_nodes
+ *               serve every smaller B and max_nodes
+ * out_dt, out   [B,H,max_nodes,dh] out: CTCSPEC_F32 (weights carried with 16 or more bits of mantissa), or CTCSPEC_BF16 with
+ *               bf16 operands (weights rounded to bf16 as well: a third less work)
+ * lse           [B,H,max_nodes] float out or NULL: what kv_weight_update takes
+ * Pointers 16-byte aligned (prefix_len, ctx_len, n_nodes, kv_off, anc_mask and lse as their types are).
+ * Limits: dh % 8 == 0, dh <= CTCSPEC_MAX_HEAD_DIM, max_nodes <= CTCSPEC_MAX_NODES; B, H, dh, max_nodes within the context's
+ * limits; H % H_kv == 0.  The same bits on every run.
+ */
+size_t prefix_verify_attn_workspace_bytes(int B, int H, int H_kv, int dh, int max_nodes);
+
+int prefix_verify_attn(ctcspec_ctx* ctx, ctcspec_dtype dt, const void* q, const void* k_prefix, const void* v_prefix,
+                       const int32_t* prefix_len, int prefix_cap, const void* k_cache, const void* v_cache,
+                       const int64_t* kv_off, const int32_t* ctx_len, int kv_cap, const void* k_tree, const void* v_tree,
+                       const int32_t* n_nodes, const uint64_t* anc_mask, int B, int H, int H_kv, int dh, int max_nodes,
+                       float scale, void* workspace, size_t workspace_bytes, ctcspec_dtype out_dt, void* out, float* lse);
+
+/*
+ * kv_weight_update - the attention weight that every cached key has gathered, brought up to date after a step: what the
+ * accepted rows gave each key is added up, so that kv_evict can tell which rows a sequence still looks at.  Called once per
+ * layer between accept_longest and kv_commit (whose arguments it shares).  With a_0 = root, a_1, .. the accepted path
+ * (accept_nodes[b, 0..accept_len[b]]) and the heads h of key head hk:
+ *
+ *   weight[b,hk,j]               += sum_h sum_r exp(scale * q[b,h,a_r,:] . k_cache_j - lse[b,h,a_r])        j < ctx_len[b]
+ *   weight[b,hk,ctx_len[b] + m]   = sum_h sum_{r >= m} exp(scale * q[b,h,a_r,:] . k_tree[b,hk,a_m,:] - lse[b,h,a_r])
+ *   pos[b,hk,ctx_len[b] + m]      = next_pos[b] + m                                              m = 0..accept_len[b]
+ *
+ * - the second and third line for the rows that kv_commit appends; those beyond kv_cap are dropped as there.  An entry of
+ * accept_nodes that is no node counts for nothing and writes nothing, and so does a row with lse = -inf; every other entry of
+ * weight and pos keeps its value.
+ *
+ * dt            element type of q, k_cache, k_tree (16-byte aligned)
+ * q             [B,H,max_nodes,dh]; lse [B,H,max_nodes] float as written by prefix_verify_attn
+ * k_cache, kv_off, ctx_len, kv_cap   as for prefix_verify_attn (before kv_commit)
+ * k_tree        [B,H_kv,max_nodes,dh]
+ * accept_len, accept_nodes, T   as for kv_commit (accept_len outside 0..T counts as the nearer end)
+ * weight        [B,H_kv,kv_cap] float, in and out
+ * pos           [B,H_kv,kv_cap] int32, in and out, or NULL: the position of every cached row in its sequence
+ * next_pos      [B] int32 in: the position of the root; NULL only without pos
+ * Limits: as for prefix_verify_attn, T <= CTCSPEC_MAX_SLOTS, (T + 1) * H / H_kv <= 2304.  The same bits on every run.
+ */
+int kv_weight_update(ctcspec_ctx* ctx, ctcspec_dtype dt, const void* q, const float* lse, const void* k_cache,
+                     const int64_t* kv_off, const int32_t* ctx_len, int kv_cap, const void* k_tree,
+                     const int32_t* accept_len, const int32_t* accept_nodes, int T, int B, int H, int H_kv, int dh,
+                     int max_nodes, float scale, float* weight, int32_t* pos, const int32_t* next_pos);
+
+/*
+ * kv_evict - a layer's cache brought down to `budget` rows per sequence and key head.  Sequences with ctx_len[b] <= budget keep
+ * everything.  Of the others every key head keeps, with n = budget:
+ *   the rows with pos < sink (the first positions of the sequence) and those with pos >= next_pos[b] - recent (its last ones),
+ *   then those with the largest weight - equal weights: the smaller index; a weight that is not a number: behind all others.
+ * (Should positions occur more than once, so that more than n rows are among the first kind, the n of smallest index stay.)
+ * Kept rows with an index below n stay where they are; those from n on move, in ascending order, into the places that became
+ * free, in ascending order.  Attention does not ask for an order (keys carry their position), and nothing else has to move.
+ *
+ *   kept[b,hk,j]     = the old index of row j of the new cache, j < min(ctx_len[b], budget); -1 for the other j < budget
+ *   weight_out, pos_out [b,hk,j] = weight, pos [b,hk,kept[b,hk,j]]; entries j >= ctx_len_out[b] are not written
+ *   ctx_len_out[b]   = min(ctx_len[b], budget)
+ *
+ * dt            element type of the caches
+ * k_cache, v_cache, kv_off, ctx_len, kv_cap   as for tree_verify_attn with [H_kv][kv_cap][dh] per sequence; rewritten in place
+ *               (only rows below ctx_len_out[b]).  16-byte aligned; sequences must not share rows
+ * weight        [B,H_kv,kv_cap] float; pos [B,H_kv,kv_cap] int32 or NULL; next_pos [B] int32 or NULL: as kv_weight_update
+ *               leaves them (next_pos: the position that the next row will have)
+ * sink, recent  >= 0, together <= budget; either needs pos and pos_out, recent needs next_pos
+ * kept          [B,H_kv,budget] int32 out
+ * weight_out, pos_out, ctx_len_out   out, other buffers than the inputs
+ * Limits: dh % 8 == 0, dh <= CTCSPEC_MAX_HEAD_DIM, B, H_kv, dh within the context's limits.  The same bits on every run.
+ */
+int kv_evict(ctcspec_ctx* ctx, ctcspec_dtype dt, void* k_cache, void* v_cache, const int64_t* kv_off,
+             const int32_t* ctx_len, int kv_cap, const float* weight, const int32_t* pos, const int32_t* next_pos, int B,
+             int H_kv, int dh, int budget, int sink, int recent, int32_t* kept, float* weight_out, int32_t* pos_out,
+             int32_t* ctx_len_out);
 
 #ifdef __cplusplus
 }

@@ -20,9 +20,13 @@ from .binding import (  # noqa: F401
     draft_layer_forward,
     draft_layer_workspace_bytes,
     kv_commit,
+    kv_evict,
+    kv_weight_update,
     layer_weights,
     library_path,
     load_library,
+    prefix_verify_attn,
+    prefix_verify_attn_workspace_bytes,
     prepared,
     tree_verify_attn,
     verify_head_argmax,

@@ -18,6 +18,7 @@ EXPORTS = (
     "accept_longest", "verify_head_argmax", "kv_commit", "draft_layer_workspace_bytes", "draft_layer_forward",
     "ctc_sum_score", "ctc_raw_tree", "ctc_loss_workspace_bytes", "ctc_loss", "verify_sample_tokens",
     "ctc_draft_topk_noalloc", "ctcspec_defer_topk_merge", "ctcspec_flush", "ctcspec_stream_probe",
+    "prefix_verify_attn_workspace_bytes", "prefix_verify_attn", "kv_weight_update", "kv_evict",
 )
 
 CTCSPEC_F32, CTCSPEC_BF16 = 0, 1
@@ -106,6 +107,16 @@ def load_library():
     lib.ctc_raw_tree.argtypes = lib.ctc_collapse_tree.argtypes + [c_void_p]
     lib.ctc_sum_score.restype = c_int
     lib.ctc_sum_score.argtypes = [c_void_p] * 6 + [c_int, c_int, c_int, c_int32, c_int, c_void_p, c_void_p]
+    lib.prefix_verify_attn_workspace_bytes.restype = c_size_t
+    lib.prefix_verify_attn_workspace_bytes.argtypes = [c_int] * 5
+    lib.prefix_verify_attn.restype = c_int
+    lib.prefix_verify_attn.argtypes = ([c_void_p, c_int] + [c_void_p] * 4 + [c_int] + [c_void_p] * 4 + [c_int] +
+                                       [c_void_p] * 4 + [c_int] * 5 + [c_float, c_void_p, c_size_t, c_int] + [c_void_p] * 2)
+    lib.kv_weight_update.restype = c_int
+    lib.kv_weight_update.argtypes = ([c_void_p, c_int] + [c_void_p] * 5 + [c_int] + [c_void_p] * 3 + [c_int] * 6 +
+                                     [c_float] + [c_void_p] * 3)
+    lib.kv_evict.restype = c_int
+    lib.kv_evict.argtypes = [c_void_p, c_int] + [c_void_p] * 4 + [c_int] + [c_void_p] * 3 + [c_int] * 6 + [c_void_p] * 4
     _LIB = lib
     return lib
 
@@ -463,4 +474,86 @@ def verify_sample_tokens(ctx, logits, n_nodes, uniforms, temperature, *, out=Non
     rc = ctx.lib.verify_sample_tokens(ctx.handle, _ptr(logits, torch.float32), _ptr(n_nodes, torch.int32),
                                       _ptr(uniforms, torch.float32), float(temperature), B, N, V, _ptr(res))
     ctx._check(rc, "verify_sample_tokens")
+    return res
+
+
+def prefix_verify_attn_workspace_bytes(B, H, H_kv, dh, max_nodes) -> int:
+    return int(load_library().prefix_verify_attn_workspace_bytes(B, H, H_kv, dh, max_nodes))
+
+
+def _shaped(name, t, shape):
+    if tuple(t.shape) != tuple(shape):
+        raise CtcspecError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    return t
+
+
+def prefix_verify_attn(ctx, q, k_prefix, v_prefix, prefix_len, k_cache, v_cache, kv_off, ctx_len, kv_cap, k_tree, v_tree,
+                       n_nodes, anc_mask, scale, *, out_dtype=torch.float32, want_lse=False, workspace=None, out=None):
+    """q [B,H,max_nodes,dh], k_prefix/v_prefix [H_kv,prefix_cap,dh] shared by the batch, k_tree/v_tree [B,H_kv,max_nodes,dh],
+    caches as for tree_verify_attn -> dict(out [B,H,max_nodes,dh][, lse [B,H,max_nodes]])."""
+    B, H, N, dh = q.shape
+    H_kv, prefix_cap, dev = k_prefix.shape[0], k_prefix.shape[1], q.device
+    _shaped("k_prefix", k_prefix, (H_kv, prefix_cap, dh)), _shaped("v_prefix", v_prefix, (H_kv, prefix_cap, dh))
+    _shaped("k_tree", k_tree, (B, H_kv, N, dh)), _shaped("v_tree", v_tree, (B, H_kv, N, dh))
+    _shaped("anc_mask", anc_mask, (B, N, (N + 63) // 64)), _shaped("prefix_len", prefix_len, (1,))
+    for name, t in (("kv_off", kv_off), ("ctx_len", ctx_len), ("n_nodes", n_nodes)):
+        _shaped(name, t, (B,))
+    if workspace is None:
+        workspace = torch.empty(prefix_verify_attn_workspace_bytes(B, H, H_kv, dh, N), dtype=torch.uint8, device=dev)
+    res = {"out": _out(out, "out", (B, H, N, dh), out_dtype, dev)}
+    if want_lse:
+        res["lse"] = _out(out, "lse", (B, H, N), torch.float32, dev)
+    rc = ctx.lib.prefix_verify_attn(
+        ctx.handle, _dtype_code(q), _ptr(q), _ptr(k_prefix, q.dtype), _ptr(v_prefix, q.dtype), _ptr(prefix_len, torch.int32),
+        prefix_cap, _ptr(k_cache, q.dtype), _ptr(v_cache, q.dtype), _ptr(kv_off, torch.int64), _ptr(ctx_len, torch.int32), kv_cap,
+        _ptr(k_tree, q.dtype), _ptr(v_tree, q.dtype), _ptr(n_nodes, torch.int32), _ptr(anc_mask, torch.int64), B, H, H_kv, dh, N,
+        c_float(scale), _ptr(workspace, torch.uint8), workspace.numel(), _dtype_code(res["out"]), _ptr(res["out"]),
+        _ptr(res.get("lse")))
+    ctx._check(rc, "prefix_verify_attn")
+    return res
+
+
+def kv_weight_update(ctx, q, lse, k_cache, kv_off, ctx_len, kv_cap, k_tree, accept_len, accept_nodes, scale, weight, *,
+                     pos=None, next_pos=None):
+    """Add what the accepted rows (q [B,H,max_nodes,dh], their lse [B,H,max_nodes]) gave every cached key to weight
+    [B,H_kv,kv_cap] in place; pos [B,H_kv,kv_cap] int32 receives the new rows' positions, next_pos [B] on."""
+    B, H, N, dh = q.shape
+    H_kv = k_tree.shape[1]
+    _shaped("k_tree", k_tree, (B, H_kv, N, dh)), _shaped("lse", lse, (B, H, N)), _shaped("weight", weight, (B, H_kv, kv_cap))
+    T = _shaped("accept_nodes", accept_nodes, (B, accept_nodes.shape[-1])).shape[1] - 1
+    for name, t in (("kv_off", kv_off), ("ctx_len", ctx_len), ("accept_len", accept_len)):
+        _shaped(name, t, (B,))
+    if pos is not None:
+        _shaped("pos", pos, (B, H_kv, kv_cap))
+    if next_pos is not None:
+        _shaped("next_pos", next_pos, (B,))
+    rc = ctx.lib.kv_weight_update(
+        ctx.handle, _dtype_code(q), _ptr(q), _ptr(lse, torch.float32), _ptr(k_cache, q.dtype), _ptr(kv_off, torch.int64),
+        _ptr(ctx_len, torch.int32), kv_cap, _ptr(k_tree, q.dtype), _ptr(accept_len, torch.int32), _ptr(accept_nodes, torch.int32),
+        T, B, H, H_kv, dh, N, c_float(scale), _ptr(weight, torch.float32), _ptr(pos, torch.int32), _ptr(next_pos, torch.int32))
+    ctx._check(rc, "kv_weight_update")
+
+
+def kv_evict(ctx, k_cache, v_cache, kv_off, ctx_len, kv_cap, dh, weight, budget, *, pos=None, next_pos=None, sink=0, recent=0,
+             out=None):
+    """Bring the caches down to `budget` rows per sequence and key head, in place; weight, pos [B,H_kv,kv_cap] as
+    kv_weight_update leaves them -> dict(kept [B,H_kv,budget], weight, ctx_len[, pos]) of the new cache."""
+    B, H_kv = weight.shape[:2]
+    dev = weight.device
+    _shaped("weight", weight, (B, H_kv, kv_cap)), _shaped("kv_off", kv_off, (B,)), _shaped("ctx_len", ctx_len, (B,))
+    if v_cache.dtype != k_cache.dtype:
+        raise CtcspecError("k_cache and v_cache must have one dtype")
+    if next_pos is not None:
+        _shaped("next_pos", next_pos, (B,))
+    res = {"kept": _out(out, "kept", (B, H_kv, budget), torch.int32, dev),
+           "weight": _out(out, "weight", (B, H_kv, kv_cap), torch.float32, dev),
+           "ctx_len": _out(out, "ctx_len", (B,), torch.int32, dev)}
+    if pos is not None:
+        _shaped("pos", pos, (B, H_kv, kv_cap))
+        res["pos"] = _out(out, "pos", (B, H_kv, kv_cap), torch.int32, dev)
+    rc = ctx.lib.kv_evict(
+        ctx.handle, _dtype_code(k_cache), _ptr(k_cache), _ptr(v_cache), _ptr(kv_off, torch.int64), _ptr(ctx_len, torch.int32),
+        kv_cap, _ptr(weight, torch.float32), _ptr(pos, torch.int32), _ptr(next_pos, torch.int32), B, H_kv, dh, budget, sink, recent,
+        _ptr(res["kept"]), _ptr(res["weight"]), _ptr(res.get("pos")), _ptr(res["ctx_len"]))
+    ctx._check(rc, "kv_evict")
     return res

@@ -103,6 +103,9 @@ hipError_t prepare_accept();
 hipError_t prepare_sum_score();
 hipError_t prepare_ctc_loss();
 hipError_t prepare_verify_sample();
+hipError_t prepare_prefix_attn();
+hipError_t prepare_kv_weight();
+hipError_t prepare_kv_evict();
 
 #define CTCSPEC_REQUIRE(ctx, cond, code, ...) \
   do {                                        \

@@ -105,6 +105,9 @@ extern "C" int ctcspec_create(ctcspec_ctx** out, void* hip_stream, const ctcspec
   if (e == hipSuccess) e = prepare_sum_score();
   if (e == hipSuccess) e = prepare_ctc_loss();
   if (e == hipSuccess) e = prepare_verify_sample();
+  if (e == hipSuccess) e = prepare_prefix_attn();
+  if (e == hipSuccess) e = prepare_kv_weight();
+  if (e == hipSuccess) e = prepare_kv_evict();
   if (e != hipSuccess) {
     delete ctx;
     return fail(nullptr, CTCSPEC_EHIP, "preparing the kernels failed: %s", hipGetErrorString(e));

@@ -1,0 +1,336 @@
+"""prefix_verify_attn against the float64 oracle: head layouts, types, lengths from nothing to several iterations of every
+kernel shape, empty rows, values that are no numbers in hidden places, and its refusals."""
+import ctypes
+import math
+
+import numpy as np
+import pytest
+
+import oracle
+import paper_2412_00061_amd as pkg
+from workloads.device import dev_i32, dev_i64, to_device
+from workloads.generate import bf16_bits_to_f32, f32_to_bf16_bits, round_to_storage
+
+pytestmark = pytest.mark.gpu
+
+
+def make(seed, B, H, Hkv, N, dh, P, ctx, n_nodes, dtype, *, spread=1.0, spikes=0):
+    """Operands with room behind every length that holds NaN; the sequences' blocks lie in another order than they count."""
+    rng = np.random.default_rng(seed)
+    f = lambda *s: round_to_storage(rng.standard_normal(s, dtype=np.float32), dtype)  # noqa: E731
+    cap, pcap = max(ctx) + int(rng.integers(0, 5)), P + int(rng.integers(0, 4))
+    c = dict(B=B, H=H, Hkv=Hkv, N=N, dh=dh, P=P, cap=cap, pcap=pcap, ctx=list(ctx), n=list(n_nodes), dtype=dtype, scale=dh ** -0.5)
+    c["q"] = round_to_storage(f(B, H, N, dh) * np.float32(spread), dtype)
+    c["kp"], c["vp"] = f(Hkv, pcap, dh), f(Hkv, pcap, dh)
+    c["kt"], c["vt"] = f(B, Hkv, N, dh), f(B, Hkv, N, dh)
+    c["kc"], c["vc"] = f(B, Hkv, cap, dh), f(B, Hkv, cap, dh)
+    for _ in range(spikes):  # keys that rows cannot overlook, anywhere
+        c["kp"][rng.integers(Hkv), rng.integers(max(P, 1)) if P else 0] *= 8 if P else 1
+        b = rng.integers(B)
+        if ctx[b]:
+            c["kc"][b, rng.integers(Hkv), rng.integers(ctx[b])] *= 8
+    c["kp"][:, P:] = c["vp"][:, P:] = np.nan
+    seen = np.zeros((B, N, N), dtype=bool)
+    for b in range(B):
+        c["kc"][b, :, ctx[b]:] = c["vc"][b, :, ctx[b]:] = np.nan
+        c["kt"][b, :, n_nodes[b]:] = c["vt"][b, :, n_nodes[b]:] = np.nan
+        c["q"][b, :, n_nodes[b]:] = np.nan
+        for i in range(n_nodes[b]):
+            if i:
+                seen[b, i] = seen[b, rng.integers(i)]
+            seen[b, i, i] = True
+    c["seen"] = seen
+    c["place"] = rng.permutation(B)
+    return c
+
+
+def mask_words(seen, N):
+    words = (N + 63) // 64
+    m = np.zeros(seen.shape[:2] + (words,), dtype=np.uint64)
+    for j in range(N):
+        m[:, :, j // 64] |= seen[:, :, j].astype(np.uint64) << np.uint64(j % 64)
+    return m
+
+
+def upload(c):
+    B, Hkv, cap, dh = c["B"], c["Hkv"], c["cap"], c["dh"]
+    caches = {}
+    for name in ("kc", "vc"):
+        flat = np.empty((B, Hkv, cap, dh), dtype=np.float32)
+        flat[c["place"]] = c[name]
+        caches[name] = to_device(flat.reshape(-1) if flat.size else np.zeros(8, dtype=np.float32), c["dtype"])
+    d = {n: to_device(c[n] if c[n].size else np.zeros(c[n].shape, dtype=np.float32), c["dtype"]) for n in ("q", "kp", "vp", "kt", "vt")}
+    d.update(caches, off=dev_i64(c["place"].astype(np.int64) * (Hkv * cap * dh)), ctx=dev_i32(c["ctx"]), n=dev_i32(c["n"]),
+             plen=dev_i32([c["P"]]), mask=dev_i64(mask_words(c["seen"], c["N"]).view(np.int64)))
+    return d
+
+
+def context(c, **more):
+    lim = dict(max_batch=c["B"], max_slots=1, max_topk=1, max_vocab_rows=16, max_nodes=c["N"], max_heads=c["H"], max_head_dim=c["dh"])
+    lim.update(more)
+    return pkg.Context(**lim)
+
+
+def call(ctx, c, d, out_dtype, **more):
+    return pkg.prefix_verify_attn(ctx, d["q"], d["kp"], d["vp"], d["plen"], d["kc"], d["vc"], d["off"], d["ctx"], c["cap"], d["kt"],
+                                  d["vt"], d["n"], d["mask"], c["scale"], out_dtype=out_dtype, want_lse=True, **more)
+
+
+def reference(c, b):
+    L, n = c["ctx"][b], c["n"][b]
+    return oracle.prefix_attention(c["q"][b, :, :n], c["kp"][:, :c["P"]], c["vp"][:, :c["P"]], c["kc"][b, :, :L], c["vc"][b, :, :L],
+                                   c["kt"][b], c["vt"][b], n, c["seen"][b, :n, :n], c["scale"])
+
+
+def allowed(c, b, bf16_out):
+    """How far an output may be off: per row the relative error of a weight times the weighted mean of |v|, plus the rounding of the
+    output.  A score is a sum of dh products, each exact (bf16) or rounded once, added in float32: off by at most
+    (dh + 2) 2^-24 sum |q k| scale, and as much again where it is scaled; a weight by twice that (numerator and sum), by 2^-22
+    for the exponential and its argument's rounding, 2^-24 per addition of up to 32 keys' tiles in a lane and of the joins; bf16
+    weights are two numbers whose sum is within 2^-15 of them, or one within 2^-8."""
+    n, L, P = c["n"][b], c["ctx"][b], c["P"]
+    group = c["H"] // c["Hkv"]
+    mean, score = np.zeros((c["H"], n)), np.zeros((c["H"], n))
+    for h in range(c["H"]):
+        g = h // group
+        k = np.concatenate([c["kp"][g, :P], c["kc"][b, g, :L], c["kt"][b, g, :n]]).astype(np.float64)
+        if len(k):
+            score[h] = (np.abs(k) @ np.abs(c["q"][b, h, :n].astype(np.float64)).T).max(0) * c["scale"]
+    keys = P + L + n
+    rel = 4 * (c["dh"] + 2) * 2.0 ** -24 * score + 2.0 ** -21 + (keys / 16 + 64) * 2.0 ** -24
+    if c["dtype"] == "bf16":
+        rel = rel + (2.0 ** -8 if bf16_out else 2.0 ** -15)
+    absolute, _ = oracle.prefix_attention(c["q"][b, :, :n], c["kp"][:, :P], np.abs(c["vp"][:, :P]), c["kc"][b, :, :L],
+                                          np.abs(c["vc"][b, :, :L]), c["kt"][b], np.abs(c["vt"][b]), n, c["seen"][b, :n, :n], c["scale"])
+    return rel, absolute
+
+
+def check(c, res, sentinel=None):
+    import torch
+    out, lse = res["out"].float().cpu().numpy().astype(np.float64), res["lse"].cpu().numpy().astype(np.float64)
+    bf16_out = res["out"].dtype == torch.bfloat16
+    for b in range(c["B"]):
+        n = c["n"][b]
+        if sentinel is not None:
+            assert np.all(out[b, :, n:] == sentinel) and np.all(lse[b, :, n:] == sentinel)
+        if not n:
+            continue
+        want, want_lse = reference(c, b)
+        rel, absolute = allowed(c, b, bf16_out)
+        off = np.abs(out[b, :, :n] - want)
+        limit = rel[..., None] * absolute + (2.0 ** -8 if bf16_out else 2.0 ** -23) * np.abs(want) + 1e-30
+        assert np.all(off <= limit), (b, float((off / limit).max()))
+        got = lse[b, :, :n]
+        none = np.isneginf(want_lse)
+        assert np.array_equal(np.isneginf(got), none) and np.all(out[b, :, :n][none] == 0)
+        # (the weights' rounding to bf16 does not enter the sums)
+        lim = rel - (0 if c["dtype"] != "bf16" else (2.0 ** -8 if bf16_out else 2.0 ** -15)) + 2.0 ** -22 * np.abs(np.where(none, 0, want_lse))
+        assert np.all(np.abs(got[~none] - want_lse[~none]) <= lim[~none])
+
+
+SHAPES = [
+    # B, H, Hkv, N, dh, P, ctx, n_nodes
+    (1, 1, 1, 1, 8, 0, [0], [1]),                                  # one key: the row's own
+    (1, 2, 2, 1, 128, 1, [0], [1]),
+    (2, 4, 4, 1, 128, 257, [33, 0], [1, 1]),                       # single tokens
+    (3, 4, 2, 7, 64, 31, [1, 64, 30], [7, 1, 5]),
+    (2, 2, 2, 33, 128, 129, [31, 200], [33, 20]),                  # 64 rows a sequence, two blocks' worth for the prefix
+    (8, 2, 2, 64, 128, 700, [0, 5, 32, 33, 63, 64, 65, 500], [64, 1, 63, 33, 32, 31, 64, 2]),
+    (5, 6, 1, 25, 96, 95, [100, 1, 0, 7, 300], [25, 0, 13, 25, 1]),  # six heads on one key head, a place not in use
+    (2, 3, 3, 128, 80, 1100, [1500, 3], [128, 97]),
+    (1, 8, 2, 128, 128, 0, [900], [128]),                          # no prefix; 512 rows share the sequence's own keys
+    (4, 5, 5, 40, 16, 2000, [0, 0, 0, 0], [40, 40, 39, 1]),        # nothing but the prefix and the trees
+    (64, 1, 1, 3, 32, 50, list(range(64)), [i % 4 for i in range(64)]),
+]
+
+
+@pytest.mark.parametrize("dtype,out", [("bf16", "f32"), ("bf16", "bf16"), ("f32", "f32")])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "x".join(map(str, s[:6])))
+def test_against_the_oracle(shape, dtype, out):
+    import torch
+    c = make(sum(map(int, shape[:6])), *shape, dtype)
+    d, ctx = upload(c), context(c)
+    od = torch.bfloat16 if out == "bf16" else torch.float32
+    buf = {"out": torch.full((c["B"], c["H"], c["N"], c["dh"]), 7.0, dtype=od, device="cuda"),
+           "lse": torch.full((c["B"], c["H"], c["N"]), 7.0, device="cuda")}
+    check(c, call(ctx, c, d, od, out=buf), sentinel=7.0)
+    first = {n: t.clone() for n, t in buf.items()}
+    again = call(ctx, c, d, od, out=buf)
+    assert all(torch.equal(first[n], again[n]) for n in first)  # the same bits
+    ctx.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("spread", [6.0, 40.0])
+def test_peaked_scores(dtype, spread):
+    import torch
+    c = make(5, 3, 4, 2, 37, 128 if dtype == "bf16" else 64, 640, [0, 333, 65], [37, 36, 2], dtype, spread=spread, spikes=6)
+    d, ctx = upload(c), context(c)
+    check(c, call(ctx, c, d, torch.float32))
+    ctx.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_whose_mask_is_empty(dtype):
+    import torch
+    for P, L in [(0, 0), (0, 40), (40, 0)]:
+        c = make(7, 2, 2, 2, 70, 64, P, [L, L], [70, 5], dtype)
+        c["seen"][:, 1] = False
+        c["seen"][0, 66] = False
+        d, ctx = upload(c), context(c)
+        check(c, call(ctx, c, d, torch.float32))
+        ctx.close()
+
+
+@pytest.mark.parametrize("dtype,out", [("bf16", "f32"), ("bf16", "bf16"), ("f32", "f32")])
+def test_values_that_are_no_numbers_stay_with_those_who_see_them(dtype, out):
+    import torch
+    c = make(9, 2, 4, 2, 50, 128, 64, [40, 3], [50, 50], dtype)
+    c["seen"][:] = np.tril(np.ones((50, 50), dtype=bool))
+    d, ctx = upload(c), context(c)
+    od = torch.bfloat16 if out == "bf16" else torch.float32
+    clean = call(ctx, c, d, od)["out"].clone()
+    vt = d["vt"]
+    vt[0, 1, 40, 5] = math.nan
+    vt[0, 1, 45, 6] = math.inf
+    vt[0, 1, 46, 6] = -math.inf
+    got = call(ctx, c, d, od)["out"]
+    touched = torch.zeros_like(got, dtype=torch.bool)
+    touched[0, 2:, 40:, 5] = True  # heads 2 and 3 read key head 1
+    touched[0, 2:, 45:, 6] = True
+    assert torch.isnan(got[0, 2:, 40:, 5]).all() and torch.isposinf(got[0, 2:, 45, 6]).all() and torch.isnan(got[0, 2:, 46:, 6]).all()
+    assert torch.equal(got[~touched], clean[~touched])
+    # a hidden key that is no number, and a row's own
+    kt = d["kt"]
+    vt.copy_(to_device(c["vt"], dtype))
+    kt[1, 0, 30, 0] = math.nan
+    got = call(ctx, c, d, od)["out"]
+    hit = torch.zeros_like(got, dtype=torch.bool)
+    hit[1, :2, 30:] = True
+    assert torch.isnan(got[hit]).all() and torch.equal(got[~hit], clean[~hit])
+    kt.copy_(to_device(c["kt"], dtype))
+    d["q"][1, 3, 7] = math.inf
+    got = call(ctx, c, d, od)["out"]
+    hit[:] = False
+    hit[1, 3, 7] = True
+    assert torch.equal(got[~hit], clean[~hit]) and not torch.isfinite(got[hit]).any()
+    ctx.close()
+
+
+def test_lengths_beyond_their_capacity_count_as_the_capacity():
+    import torch
+    c = make(11, 2, 2, 2, 9, 64, 20, [30, 30], [9, 9], "bf16")
+    c["pcap"], c["cap"] = 20, 30
+    c["kp"], c["vp"], c["kc"], c["vc"] = c["kp"][:, :20], c["vp"][:, :20], c["kc"][:, :, :30], c["vc"][:, :, :30]
+    d, ctx = upload(c), context(c)
+    want = call(ctx, c, d, torch.float32)
+    d["plen"][0], d["ctx"][1], d["n"][0] = 5000, 1 << 30, 100
+    got = call(ctx, c, d, torch.float32)
+    assert torch.equal(want["out"], got["out"]) and torch.equal(want["lse"], got["lse"])
+    d["plen"][0], d["ctx"][:], d["n"][0] = -3, -1, -1
+    call(ctx, c, d, torch.float32, out=got)
+    c.update(P=0, ctx=[0, 0], n=[0, 9])
+    assert torch.equal(want["out"][0], got["out"][0])  # not written
+    check(c, got)
+    ctx.close()
+
+
+def test_one_workspace_serves_smaller_batches():
+    import torch
+    ws = torch.empty(pkg.prefix_verify_attn_workspace_bytes(8, 4, 2, 64, 64), dtype=torch.uint8, device="cuda")
+    for B, N in [(8, 64), (8, 1), (1, 64), (3, 17), (7, 33)]:
+        c = make(B + N, B, 4, 2, N, 64, 300, [37 * b for b in range(B)], [N] * B, "bf16")
+        d, ctx = upload(c), context(c)
+        ws.fill_(0xff)  # (whatever a call leaves there is no part of the next one's result)
+        check(c, call(ctx, c, d, torch.bfloat16, workspace=ws))
+        ctx.close()
+
+
+def test_captured_and_replayed():
+    """A graph with two calls on one workspace, replayed with new lengths and other work in between."""
+    import torch
+    c = make(21, 4, 4, 2, 30, 128, 333, [10, 100, 0, 250], [30, 12, 1, 30], "bf16")
+    e = make(22, 4, 4, 2, 30, 128, 333, [250, 0, 90, 1], [3, 30, 29, 0], "bf16")
+    c["cap"] = e["cap"] = 250
+    for x in (c, e):
+        for name in ("kc", "vc"):
+            x[name] = x[name][:, :, :250]
+        x["pcap"], x["kp"], x["vp"] = 333, x["kp"][:, :333], x["vp"][:, :333]
+        x["place"] = np.arange(4)
+    d, alt = upload(c), upload(e)
+    stream = torch.cuda.Stream()
+    ctx = context(c, stream=stream)
+    ws = torch.empty(pkg.prefix_verify_attn_workspace_bytes(4, 4, 2, 128, 30), dtype=torch.uint8, device="cuda")
+    o = {n: {"out": torch.zeros((4, 4, 30, 128), device="cuda"), "lse": torch.zeros((4, 4, 30), device="cuda")} for n in "ab"}
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        call(ctx, c, d, torch.float32, workspace=ws, out=o["a"])
+        call(ctx, c, alt, torch.float32, workspace=ws, out=o["b"])
+    torch.cuda.synchronize()
+    mine, other = {n: t.clone() for n, t in d.items()}, alt
+    for rep in range(4):
+        now, what = (mine, c) if rep % 2 == 0 else (other, e)
+        for n in d:
+            d[n].copy_(now[n])
+        for x in o.values():
+            x["out"].zero_(), x["lse"].zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        check(what, o["a"])
+        check(e, o["b"])
+    ctx.close()
+
+
+def test_refusals():
+    import torch
+    c = make(1, 2, 4, 2, 5, 64, 10, [4, 4], [5, 5], "bf16")
+    d, ctx = upload(c), context(c)
+    lib = ctx.lib
+    ws = torch.empty(pkg.prefix_verify_attn_workspace_bytes(2, 4, 2, 64, 5), dtype=torch.uint8, device="cuda")
+    out, lse = torch.zeros((2, 4, 5, 64), device="cuda"), torch.zeros((2, 4, 5), device="cuda")
+    p = lambda t: ctypes.c_void_p(t.data_ptr()) if t is not None else None  # noqa: E731
+
+    def go(want, text, handle=ctx.handle, **k):
+        a = dict(dt=1, q=p(d["q"]), kp=p(d["kp"]), vp=p(d["vp"]), plen=p(d["plen"]), pcap=c["pcap"], kc=p(d["kc"]), vc=p(d["vc"]),
+                 off=p(d["off"]), ctx=p(d["ctx"]), cap=c["cap"], kt=p(d["kt"]), vt=p(d["vt"]), n=p(d["n"]), mask=p(d["mask"]), B=2, H=4,
+                 Hkv=2, dh=64, N=5, scale=0.1, ws=p(ws), wsb=ws.numel(), odt=0, out=p(out), lse=p(lse))
+        a.update(k)
+        assert lib.prefix_verify_attn(handle, *a.values()) == want, k
+        if handle:
+            assert text in ctx.last_error(), (k, ctx.last_error())
+
+    go(-1, "", handle=None)
+    for name in ("q", "kp", "vp", "plen", "kc", "vc", "off", "ctx", "kt", "vt", "n", "mask", "ws", "out"):
+        go(-1, "null", **{name: None})
+    for name in ("B", "H", "Hkv", "dh", "N"):
+        go(-1, "positive", **{name: 0})
+    go(-1, "positive", pcap=-1)
+    go(-1, "positive", cap=-1)
+    go(-1, "multiple of H_kv", Hkv=3)
+    go(-1, "element type", dt=7)
+    go(-1, "output", odt=5)
+    go(-1, "output", dt=0, odt=1)
+    for s in (0.0, -1.0, math.inf, math.nan):
+        go(-1, "scale", scale=s)
+    go(-2, "multiple of 8", dh=60)
+    go(-2, "dh", dh=136)
+    go(-2, "max_nodes", N=129)
+    go(-2, "limits", B=3)
+    go(-2, "limits", H=8)
+    go(-2, "limits", dh=72)
+    go(-2, "limits", N=6)
+    go(-1, "workspace", wsb=ws.numel() // 2)
+    for name in ("q", "kp", "vp", "kc", "vc", "kt", "vt", "ws", "out"):
+        t = {"ws": ws, "out": out}.get(name, d.get(name))
+        go(-1, "aligned", **{name: ctypes.c_void_p(t.data_ptr() + 8)})
+    torch.cuda.synchronize()
+    assert not out.any() and not lse.any()  # nothing was launched
+    bad = dict(d, kt=d["kt"][:, :1].contiguous())
+    with pytest.raises(pkg.CtcspecError, match="k_tree"):
+        call(ctx, c, bad, torch.float32)
+    with pytest.raises(pkg.CtcspecError, match="float32|bfloat16|got"):
+        call(ctx, c, dict(d, vp=d["vp"].float()), torch.float32)
+    go(0, "")
+    ctx.close()
