@@ -42,6 +42,7 @@ struct PrefixAttnParams {
   float sl2;                      // scale * log2(e)
   float* po;                      // partial O of the pass: [slot][R / 32][DHP / 32][4][64 lanes][4]
   float* pml;                     // [slot][2][R]: maximum in the log2 domain, sum
+  int* odd;                       // [slot] of the sequences' own keys: a value of a tree node is infinite or not a number
 };
 
 // a value that is the same in every lane, in scalar registers
@@ -59,11 +60,15 @@ struct Batch {
   int n, first;  // nodes, nodes of the sequences before it
   int ctx;       // cached rows
   int all;       // nodes of all sequences (uniform)
+  long long off; // kv_off
+  int prefix;    // rows of the prefix (uniform)
 };
 __device__ __forceinline__ Batch read_batch(const PrefixAttnParams& p) {
   const int lane = threadIdx.x & 63;
-  Batch t{0, 0, 0, 0};
+  Batch t{0, 0, 0, 0, 0, 0};
+  const int P = *p.prefix_len;
   if (lane < p.B) {
+    t.off = p.kv_off[lane];
     const int n = p.n_nodes[lane], L = p.ctx_len[lane];
     t.n = n < 0 ? 0 : (n > p.max_nodes ? p.max_nodes : n);
     t.ctx = L < 0 ? 0 : (L > p.kv_cap ? p.kv_cap : L);
@@ -76,6 +81,7 @@ __device__ __forceinline__ Batch read_batch(const PrefixAttnParams& p) {
   }
   t.first = sum - t.n;
   t.all = __builtin_amdgcn_readlane(sum, 63);
+  t.prefix = uniform(P < 0 ? 0 : (P > p.prefix_cap ? p.prefix_cap : P));
   return t;
 }
 
@@ -83,54 +89,54 @@ __device__ __forceinline__ Batch read_batch(const PrefixAttnParams& p) {
 template <bool OWN, int R, int TPI>
 struct Blocks {
   // prefix: the same for all; own: lane b's sequence
-  int blocks, iters;   // row blocks of a key head, iterations over the keys
-  long long unit0;     // first unit of the sequence
-  int block0;          // first block of the sequence, over its key heads
-  long long units;     // of the pass (uniform)
+  int blocks, iters;  // row blocks of a key head, iterations over the keys
+  int unit0, block0;  // first unit and first block of the sequence, over its key heads
+  int units;          // of the pass (uniform)
   __device__ __forceinline__ static Blocks make(const PrefixAttnParams& p, const Batch& t) {
     Blocks k;
     if constexpr (!OWN) {
-      int P = uniform(*p.prefix_len);
-      P = P < 0 ? 0 : (P > p.prefix_cap ? p.prefix_cap : P);
-      k.blocks = (t.all * p.group + R - 1) / R;
-      k.iters = ((P + 31) / 32 + TPI - 1) / TPI;
+      k.blocks = uniform((t.all * p.group + R - 1) / R);
+      k.iters = ((t.prefix + 31) / 32 + TPI - 1) / TPI;
       k.unit0 = 0;
       k.block0 = 0;
-      k.units = (long long)p.H_kv * k.blocks * k.iters;
+      k.units = p.H_kv * k.blocks * k.iters;
     } else {
       const int lane = threadIdx.x & 63;
       k.blocks = (t.n * p.group + R - 1) / R;
       k.iters = t.n ? ((t.ctx + 31) / 32 + (t.n + 31) / 32 + TPI - 1) / TPI : 0;
       const int mine = p.H_kv * k.blocks;
-      int b = mine;
-      long long u = (long long)mine * k.iters;
+      int b = mine, u = mine * k.iters;
 #pragma unroll
       for (int d = 1; d < 64; d *= 2) {
-        const int bb = __shfl_up(b, d, 64);
-        const long long ub = __shfl_up(u, d, 64);
+        const int bb = __shfl_up(b, d, 64), ub = __shfl_up(u, d, 64);
         if (lane >= d) { b += bb; u += ub; }
       }
       k.block0 = b - mine;
-      k.unit0 = u - (long long)mine * k.iters;
-      k.units = uniform(__shfl(u, 63, 64));
+      k.unit0 = u - mine * k.iters;
+      k.units = __builtin_amdgcn_readlane(u, 63);
     }
     return k;
   }
 };
 
-// R = 32 CW rows, CW * KP wavefronts: wavefront w has rows [32 rg, 32 rg + 32), rg = w % CW, and of an iteration's KP * KT key
-// tiles the KT from kp * KT on, kp = w / CW; the KP parts are joined through LDS at the end.  Tiles (32 keys, K and V) go
-// through registers into one of two LDS stages.  FINE: P as two bf16 numbers (16 bits of mantissa).
-template <bool F32_, int DHP_, int CW_, int KP_, int KT_, bool FINE_>
+// R = 32 QT CW rows, CW * KP wavefronts: wavefront w has rows [32 QT rg, 32 QT (rg + 1)), rg = w % CW, and of an iteration's
+// KP * KT key tiles the KT from kp * KT on, kp = w / CW; the KP parts are joined through LDS at the end.  Tiles (32 keys, K and
+// V) go straight into a ring of NS LDS stages.  FINE: P as two bf16 numbers.  WPE: wavefronts of a SIMD.
+constexpr int kPrefixTable = 10 * 64 * 4;
+template <bool F32_, int DHP_, int QT_, int CW_, int KP_, int KT_, int NS_, int WPE_, bool FINE_>
 struct PrefixShape {
   static constexpr bool F32 = F32_, FINE = FINE_;
-  static constexpr int DHP = DHP_, CW = CW_, KP = KP_, KT = KT_, NW = CW * KP, R = 32 * CW, TPI = KP * KT;
+  static constexpr int DHP = DHP_, QT = QT_, CW = CW_, KP = KP_, KT = KT_, NS = NS_, WPE = WPE_;
+  static constexpr int NW = CW * KP, R = 32 * QT * CW, TPI = KP * KT;
   static constexpr int ES = F32 ? 4 : 2, ROWB = DHP * ES, TILE = 32 * ROWB, STAGE = TPI * 2 * TILE;
   static constexpr int RQ = TILE / 1024, NREQ = TPI * 2 * RQ / NW;  // requests of 1 KB per tile, per wavefront and stage
+  static constexpr int RPR = 1024 / ROWB;                           // rows of a request
   static constexpr int DT = DHP / 32, QU = ROWB / 32;               // dh tiles of O; 32-byte steps of a row
-  static constexpr int PART = (DT * 16 + 2) * 64 * 4;               // O, m, l of a wavefront
-  static constexpr int JOIN = (KP - 1) * CW * PART;
-  static constexpr int LDS = 2 * STAGE > JOIN ? 2 * STAGE : JOIN;
+  static constexpr int PART = (DT * 16 + 2) * 64 * 4;               // O, m, l of 32 rows
+  static constexpr int JOIN = (KP - 1) * CW * QT * PART;
+  static constexpr int LDS = (NS * STAGE > JOIN ? NS * STAGE : JOIN) + kPrefixTable;
+  // what 256 compute units hold at once
+  static constexpr int GROUPS = WPE * 4 >= 2 * NW && 2 * LDS <= 160 * 1024 ? 512 : 256;
   static_assert(TPI * 2 * RQ % NW == 0 && LDS <= 160 * 1024, "requests in equal shares; fits the LDS");
   // 16-byte chunk c of row r lies at chunk c ^ f(r).  K: the LDS serves lanes l .. l+7 with l+16 .. l+23 together, which read
   // the same chunk of rows r .. r+7 and r+16 .. r+23 - 16 places of 16 bytes.  V, bf16: 32 lanes read 8 bytes each of four
@@ -153,10 +159,14 @@ __device__ __forceinline__ s16x4 lds_read_tr(unsigned int at) {
 #endif
 
 template <typename SH, bool OWN>
-__global__ __launch_bounds__(64 * SH::NW) void prefix_attn_kernel(PrefixAttnParams p) {
+__global__ __launch_bounds__(64 * SH::NW, SH::WPE) void prefix_attn_kernel(PrefixAttnParams p) {
 #if defined(__HIP_DEVICE_COMPILE__)  // (buffer descriptors exist on the device only)
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-  constexpr int R = SH::R, ROWB = SH::ROWB, TILE = SH::TILE, NREQ = SH::NREQ, DT = SH::DT, QU = SH::QU, TPI = SH::TPI;
+  // Behind the stages (whose places are formed by xor: they begin at a multiple of a row's bytes): what the lanes know about the
+  // sequences, out of the registers while the keys go by, and a flag.
+  int(*table)[64] = (int(*)[64])(smem + SH::LDS - kPrefixTable);
+  enum { kNodes, kCtx, kOff, kOffHigh, kFirst, kBlocks, kIters, kUnit0, kBlock0, kOdd };
+  constexpr int R = SH::R, QT = SH::QT, ROWB = SH::ROWB, TILE = SH::TILE, NREQ = SH::NREQ, DT = SH::DT, QU = SH::QU, TPI = SH::TPI, KT = SH::KT;
   constexpr unsigned int kOutside = 0x40000000u;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -166,25 +176,27 @@ __global__ __launch_bounds__(64 * SH::NW) void prefix_attn_kernel(PrefixAttnPara
 
   const Batch t = read_batch(p);
   const Blocks<OWN, R, TPI> blocks = Blocks<OWN, R, TPI>::make(p, t);
-  const Deal d = prefix_deal(blocks.units);
+  const Deal d = prefix_deal(blocks.units, SH::GROUPS);
   // Workgroups go to the 8 XCDs in turn, each with an L2 of its own: consecutive shares - the row blocks of a key head, which
   // read the same keys - go to the same one.
-  static_assert(kPrefixGroups % 8 == 0);
+  static_assert(SH::GROUPS % 8 == 0 && SH::GROUPS <= kPrefixMaxGroups);
   const int per = (d.groups + 7) / 8, w = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
   if ((int)(blockIdx.x >> 3) >= per || w >= d.groups) return;
-  long long u = uniform(d.begin(w));
-  const long long u1 = uniform(d.begin(w + 1));
-
-  // ---- loads: number x of a stage is tile x / (2 RQ), K then V, 1 KB after 1 KB; its place in the tile in memory and in LDS --
-  unsigned int voff[NREQ], wplace[NREQ];
+  int u = uniform(d.begin(w));
+  const int u1 = uniform(d.begin(w + 1));
+  if (wave == 0) {
+    const int own[9] = {t.n, t.ctx, (int)t.off, (int)(t.off >> 32), t.first, blocks.blocks, blocks.iters, blocks.unit0, blocks.block0};
 #pragma unroll
-  for (int j = 0; j < NREQ; ++j) {
-    const int x = wave * NREQ + j, part = x % SH::RQ;
-    const bool is_v = x / SH::RQ & 1;
-    const int row = part * (1024 / ROWB) + lane / (ROWB / 16), chunk = lane % (ROWB / 16);
-    voff[j] = chunk * 16 < rb ? (unsigned)(row * rb + chunk * 16) : kOutside;
-    wplace[j] = x / SH::RQ * TILE + row * ROWB + ((chunk ^ (is_v ? SH::fv(row) : SH::fk(row))) << 4);
+    for (int i = 0; i < 9; ++i) table[i][lane] = own[i];
   }
+  __syncthreads();
+  auto of = [&](int what, int b) __attribute__((always_inline)) { return uniform(table[what][b]); };
+  const int all = t.all, prefix = t.prefix, pblocks = uniform(blocks.blocks), piters = uniform(blocks.iters);
+
+  // ---- requests: number x of a stage is tile x / (2 RQ), K then V, 1 KB (RPR rows) after 1 KB.  Lane l of a request fills the l-th
+  // 16 bytes of its kilobyte: with the chunk that belongs there.  The row's bits above those of lrow turn the chunks further,
+  // request by request (f(a + b) = f(a) ^ f(b)).
+  const int lrow = lane / (ROWB / 16), kchunk = lane % (ROWB / 16) ^ SH::fk(lrow), vchunk = lane % (ROWB / 16) ^ SH::fv(lrow);
   const unsigned int lds0 = (unsigned)(size_t)(lds_byte*)smem;
   // this lane's place in a K tile (row c, first half of a 32-byte step) and in a V tile
   const unsigned int kplace = c * ROWB + ((h2 ^ SH::fk(c)) << 4);
@@ -193,225 +205,288 @@ __global__ __launch_bounds__(64 * SH::NW) void prefix_attn_kernel(PrefixAttnPara
     vplace = 4 * h2 * ROWB + (((c >> 2) ^ (h2 << 3)) << 4) + (c & 3) * 4;  // key 4 h2 (+ 8 (i / 4) + i % 4), dh c (+ 32 t)
   } else {
     // the transposing read: 16 lanes fetch 4 rows x 16 dh, 8 bytes each, and lane s of them receives dh s of the four rows
-    const int s = lane & 15, row = 4 * h2 + (s >> 2), chunk = ((c >> 4) << 1) + ((s & 3) >> 1);
-    vplace = row * ROWB + ((chunk ^ SH::fv(row)) << 4) + (s & 1) * 8;
+    const int s = lane & 15, row = 4 * h2 + (s >> 2), ch = ((c >> 4) << 1) + ((s & 3) >> 1);
+    vplace = row * ROWB + ((ch ^ SH::fv(row)) << 4) + (s & 1) * 8;
   }
 
   while (u < u1) {
+    // (The lane's number, as something new: addresses that only a segment's ends need are then formed there, not kept in registers
+    // all the way - with them the kernels for one sequence's rows did not fit.)
+    int seg_lane = lane;
+    asm volatile("" : "+v"(seg_lane));
+    const int sc = seg_lane & 31, sh = seg_lane >> 5;
     // ---- which block of rows, which keys -------------------------------------------------------------------------------
     int b = 0, kh, blk, it0, iters, slot;
     if constexpr (OWN) {
       // (sequences without nodes have no units: the last sequence that starts at or before u and has some)
-      const unsigned long long some = __builtin_amdgcn_ballot_w64(lane < p.B && blocks.iters > 0 && blocks.blocks > 0 && blocks.unit0 <= u);
-      b = 63 - __builtin_clzll(some);
-      iters = __builtin_amdgcn_readlane(blocks.iters, b);
-      const int nb = __builtin_amdgcn_readlane(blocks.blocks, b);
-      const long long rel = u - uniform(__shfl(blocks.unit0, b, 64));
-      const int item = uniform((int)(rel / iters));
-      it0 = uniform((int)(rel - (long long)item * iters));
+      b = 63 - __builtin_clzll(__builtin_amdgcn_ballot_w64(table[kIters][seg_lane] > 0 && table[kUnit0][seg_lane] <= u));
+      iters = of(kIters, b);
+      const int nb = of(kBlocks, b), rel = u - of(kUnit0, b);
+      const int item = uniform(rel / iters);
+      it0 = rel - item * iters;
       kh = uniform(item / nb);
       blk = item - kh * nb;
-      slot = w + __builtin_amdgcn_readlane(blocks.block0, b) + item;
+      slot = w + of(kBlock0, b) + item;
     } else {
-      iters = blocks.iters;
-      const int item = uniform((int)(u / iters));
-      it0 = uniform((int)(u - (long long)item * iters));
-      kh = uniform(item / blocks.blocks);
-      blk = item - kh * blocks.blocks;
+      iters = piters;
+      const int item = uniform(u / iters);
+      it0 = u - item * iters;
+      kh = uniform(item / pblocks);
+      blk = item - kh * pblocks;
       slot = w + item;
     }
-    const long long room = u1 - u;
-    const int niter = uniform((int)(iters - it0 < room ? iters - it0 : room));
+    const int niter = uniform(iters - it0 < u1 - u ? iters - it0 : u1 - u);
     u += niter;
 
-    const int n = OWN ? __builtin_amdgcn_readlane(t.n, b) : t.all;  // nodes behind the rows
-    int L;
+    const int n = OWN ? of(kNodes, b) : all;  // nodes behind the rows
+    const int L = OWN ? of(kCtx, b) : prefix;
     const unsigned char *kc, *vc, *kt = nullptr, *vt = nullptr;
     if constexpr (OWN) {
-      L = __builtin_amdgcn_readlane(t.ctx, b);
-      const size_t at = ((size_t)uniform((long long)p.kv_off[b]) + (size_t)kh * p.kv_cap * p.dh) * SH::ES;
-      kc = p.k_cache + at;
-      vc = p.v_cache + at;
+      const long long off = (long long)((unsigned long long)(unsigned)of(kOffHigh, b) << 32 | (unsigned)of(kOff, b));
+      const size_t at = ((size_t)off + (size_t)kh * p.kv_cap * p.dh) * SH::ES;
       const size_t ta = ((size_t)b * p.H_kv + kh) * p.max_nodes * rb;
-      kt = p.k_tree + ta;
-      vt = p.v_tree + ta;
+      kc = p.k_cache + at; vc = p.v_cache + at;
+      kt = p.k_tree + ta; vt = p.v_tree + ta;
     } else {
-      L = uniform(*p.prefix_len);
-      L = L > p.prefix_cap ? p.prefix_cap : L;
       kc = p.k_prefix + (size_t)kh * p.prefix_cap * rb;
       vc = p.v_prefix + (size_t)kh * p.prefix_cap * rb;
     }
     kc = uniform(kc); vc = uniform(vc); kt = uniform(kt); vt = uniform(vt);
     const int ctx_tiles = (L + 31) / 32;
 
-    // ---- this lane's query row -------------------------------------------------------------------------------------------
-    const int r = blk * R + rg * 32 + c;
-    const bool live = r < n * p.group;
-    const bool live_wave = blk * R + rg * 32 < n * p.group;
-    u32x4 qf[QU];
-    unsigned long long mw0 = 0, mw1 = 0;
-    {
+    // ---- the tiles of iteration i of this segment into their stage -----------------------------------------------------------
+    // (The bases are parameters: captured, the choice between them becomes one between their addresses, in scratch memory.  The
+    // instruction is written out because the compiler would let every transposing read wait for all requests that it knows of;
+    // it has no register for a result, and the loop below waits for it.)
+    auto request = [&](int i, const unsigned char* kc, const unsigned char* vc, const unsigned char* kt, const unsigned char* vt)
+        __attribute__((always_inline)) {
+      const int first = (it0 + i) * TPI;
+      const unsigned int stage = lds0 + i % SH::NS * SH::STAGE;
+#pragma unroll
+      for (int j = 0; j < NREQ; ++j) {
+        const int x = wave * NREQ + j, k = first + x / (2 * SH::RQ), part0 = x % SH::RQ * SH::RPR;
+        const bool is_v = x / SH::RQ & 1;
+        const bool tree = OWN && k >= ctx_tiles;
+        const int row0 = (tree ? k - ctx_tiles : k) * 32 + part0;
+        int left = (tree ? n : L) - row0;  // rows behind the last key, and all behind the last iteration: zeros, nothing is read
+        left = left < 0 || i >= niter ? 0 : (left > SH::RPR ? SH::RPR : left);
+        const unsigned char* base = is_v ? (tree ? vt : vc) : (tree ? kt : kc);
+        const int from = left > 0 ? row0 : 0;
+        const unsigned long long at = (unsigned long long)base + (size_t)from * rb;
+        const u32x4 rsrc = {(unsigned)uniform((int)at), (unsigned)uniform((int)(at >> 32)) & 0xffffu, (unsigned)uniform(left * rb), 0x00020000u};
+        const int chunk = (is_v ? vchunk ^ SH::fv(part0) : kchunk ^ SH::fk(part0)) * 16;
+        const unsigned int off = chunk < rb ? (unsigned)(lrow * rb + chunk) : kOutside;
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(stage + x * 1024), "v"(off), "s"(rsrc)
+                     : "memory", "m0");
+      }
+    };
+    constexpr int kEarly = SH::NS > 2 ? 2 : 1;  // stages in front of the rows, which everything waits for together
+#pragma unroll
+    for (int i = 0; i < kEarly; ++i) request(i, kc, vc, kt, vt);
+    if (OWN && threadIdx.x == 0) table[kOdd][0] = 0;
+
+    // ---- this lane's query rows ------------------------------------------------------------------------------------------
+    const int row_first = blk * R + rg * 32 * QT;
+    const bool live_wave = row_first < n * p.group;
+    u32x4 qf[QT][QU];
+    unsigned long long mw0[QT], mw1[QT];
+#pragma unroll
+    for (int qt = 0; qt < QT; ++qt) {
+      const int r = row_first + qt * 32 + sc;
+      const bool live = r < n * p.group;
       int node = r / p.group, bq = b;
       const int hg = r - node * p.group;
       if constexpr (!OWN) {
+        // (sequences without nodes begin where the next one does: the last of those that begin here has the node)
         bq = 0;
-        for (int i = 1; i < p.B; ++i) bq += node >= __builtin_amdgcn_readlane(t.first, i) ? 1 : 0;
-        // (sequences without nodes begin where the next one does: the last of them that begins here has the node)
-        node -= __shfl(t.first, bq, 64);
+        for (int i = 1; i < p.B; ++i) bq += node >= table[kFirst][i] ? 1 : 0;
+        node -= table[kFirst][bq];
       }
       const unsigned char* qrow = p.q + (((size_t)bq * p.H + kh * p.group + hg) * p.max_nodes + node) * rb;
 #pragma unroll
       for (int i = 0; i < QU; ++i) {
-        const int at = (2 * i + h2) * 16;
-        qf[i] = u32x4{0u, 0u, 0u, 0u};
-        if (live && at < rb) qf[i] = *(const u32x4*)(qrow + at);
+        const int at = (2 * i + sh) * 16;
+        qf[qt][i] = u32x4{0u, 0u, 0u, 0u};
+        if (live && at < rb) qf[qt][i] = *(const u32x4*)(qrow + at);
       }
+      mw0[qt] = mw1[qt] = 0ull;
       if (OWN && live) {
         const int W = (p.max_nodes + 63) >> 6;
         const unsigned long long* m = p.anc_mask + ((size_t)b * p.max_nodes + node) * W;
-        mw0 = m[0];
-        if (W > 1) mw1 = m[1];
+        mw0[qt] = m[0];
+        if (W > 1) mw1[qt] = m[1];
       }
     }
 
-    // ---- the tiles of iteration i of this segment into registers, and from there into a stage ------------------------------
-    // (The bases are parameters: captured, the choice between them becomes one between their addresses, in scratch memory.
-    // Loads straight into LDS are not an option: the compiler lets every transposing read wait for all of them.)
-    u32x4 ld[NREQ];
-    auto load = [&](int i, const unsigned char* kc, const unsigned char* vc, const unsigned char* kt, const unsigned char* vt)
+    // (Here, for all wavefronts: a load that the compiler knows of and that may be under way in the loop would have it wait there
+    // for everything.)
+#pragma unroll
+    for (int qt = 0; qt < QT; ++qt) {
+#pragma unroll
+      for (int i = 0; i < QU; ++i) asm volatile("" : "+v"(qf[qt][i]));
+      asm volatile("" : "+v"(mw0[qt]), "+v"(mw1[qt]));
+    }
+#pragma unroll
+    for (int i = kEarly; i < SH::NS - 1; ++i) request(i, kc, vc, kt, vt);
+
+    f32x16 o[QT][DT], s[QT], s2[QT];
+    float m_run[QT], l_run[QT];
+    bool odd = false;  // values that are no numbers were met (below)
+#pragma unroll
+    for (int qt = 0; qt < QT; ++qt) {
+      m_run[qt] = -INFINITY;
+      l_run[qt] = 0.f;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[qt][dt][i] = 0.f;
+    }
+
+    // S^T = K Q^T of a tile, the keys as rows: a lane then holds 16 scores of one query row, its neighbour 32 lanes away the other
+    // 16 - register i, half h2: key 8 (i / 4) + 4 h2 + i % 4 -, and P in the same registers is the right operand of O^T += V^T P.
+    // A tile is a step of three parts: the products of the NEXT tile's scores with most of this tile's exponentials, the products of
+    // the first half of its values with the rest of them, those of the second half with the search for the next tile's maximum.
+    // Product by product, some of each: left alone, the scheduler puts all products at one end.
+    constexpr int kAhead = QU < 4 ? QU : 4;  // keys' fragments that are read ahead of their products
+    constexpr int kPairsA = 6;               // of the 8 pairs of exponentials, those of the first part
+    u32x4 a[kAhead];
+    auto read_keys = [&](unsigned int tile) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) a[i] = lds_read<u32x4>((tile + kplace) ^ (i << 5));
+    };
+    auto score = [&](int i, f32x16 (&s)[QT]) __attribute__((always_inline)) {  // product i of a tile's scores
+#pragma unroll
+      for (int qt = 0; qt < QT; ++qt) {
+        if constexpr (SH::F32) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            s[qt] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[i % kAhead][e]), __uint_as_float(qf[qt][i][e]), s[qt], 0, 0, 0);
+        } else {
+          s[qt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a[i % kAhead]), __builtin_bit_cast(bf16x8, qf[qt][i]), s[qt], 0, 0, 0);
+        }
+      }
+    };
+    // scores of keys that are not there or not seen
+    auto hide = [&](int k, bool any, f32x16 (&s)[QT], const unsigned long long (&mw0)[QT], const unsigned long long (&mw1)[QT])
         __attribute__((always_inline)) {
-#pragma unroll
-      for (int j = 0; j < NREQ; ++j) {
-        const int x = wave * NREQ + j, tile = x / (2 * SH::RQ);
-        const bool is_v = x / SH::RQ & 1;
-        const int k = (it0 + (i < niter ? i : niter - 1)) * TPI + tile;  // (behind the last iteration: the last one again)
-        const bool tree = OWN && k >= ctx_tiles;
-        const int row0 = (tree ? k - ctx_tiles : k) * 32;
-        int left = (tree ? n : L) - row0;  // rows behind the last key: zeros, nothing is read
-        left = left < 0 ? 0 : (left > 32 ? 32 : left);  // (a vector instruction: hence uniform() below)
-        const unsigned char* base = is_v ? (tree ? vt : vc) : (tree ? kt : kc);
-        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)(base + (size_t)row0 * rb), 0, (unsigned)uniform(left * rb), 0x00020000);
-        ld[j] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, voff[j], 0, 0));
-      }
-    };
-    auto commit = [&](int stage) __attribute__((always_inline)) {
-#pragma unroll
-      for (int j = 0; j < NREQ; ++j) *(__attribute__((address_space(3))) u32x4*)(lds0 + stage * SH::STAGE + wplace[j]) = ld[j];
-    };
-
-    f32x16 o[DT];
-    float m_run = -INFINITY, l_run = 0.f;
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
-
-    // one tile: S^T = K Q^T with the keys as rows - a lane then holds 16 scores of one query row, its neighbour 32 lanes away
-    // the other 16 -, P in the same registers is the right operand of O^T += V^T P
-    auto compute = [&](int k, unsigned int tile, unsigned long long mw0, unsigned long long mw1) __attribute__((always_inline)) {
       const bool tree = OWN && k >= ctx_tiles;
-      const int left = (tree ? n - (k - ctx_tiles) * 32 : L - k * 32);
-      if (left <= 0) return;
-      f32x16 s;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = 0.f;
-      const unsigned int ka = tile + kplace, va = tile + TILE + vplace;
-      // (the fragments of up to 8 steps are requested together)
-#pragma unroll
-      for (int i0 = 0; i0 < QU; i0 += 8) {
-        u32x4 a[QU < 8 ? QU : 8];
-#pragma unroll
-        for (int i = 0; i < 8 && i < QU; ++i) a[i] = lds_read<u32x4>(ka ^ ((i0 + i) << 5));
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int i = 0; i < 8 && i < QU; ++i) {
-          if constexpr (SH::F32) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[i][e]), __uint_as_float(qf[i0 + i][e]), s, 0, 0, 0);
-          } else {
-            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a[i]), __builtin_bit_cast(bf16x8, qf[i0 + i]), s, 0, 0, 0);
-          }
-        }
-      }
-      // V^T fragments: requested under the softmax
-      s16x8 v[SH::F32 ? 1 : DT][2];
-      if constexpr (!SH::F32) {
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-          for (int dt = 0; dt < DT; ++dt) {
-            const s16x4 v0 = lds_read_tr((va ^ (dt << 6)) + 16 * kb * ROWB), v1 = lds_read_tr((va ^ (dt << 6)) + (16 * kb + 8) * ROWB);
-            v[dt][kb] = s16x8{v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
-          }
-        __builtin_amdgcn_sched_barrier(0);
-      }
-      // register i, half h2: key 8 (i / 4) + 4 h2 + i % 4
-      unsigned int vis = 0xffffffffu;
+      const int row0 = (tree ? k - ctx_tiles : k) * 32;
+      const int left = any ? (tree ? n : L) - row0 : 0;
       if (tree || left < 32) {
-        vis = left >= 32 ? 0xffffffffu : ((1u << left) - 1u);
-        if (tree) {
-          const int row0 = (k - ctx_tiles) * 32;
-          vis &= (unsigned int)((row0 < 64 ? mw0 : mw1) >> (row0 & 63));
-        }
+        const unsigned int there = left >= 32 ? 0xffffffffu : (left > 0 ? (1u << left) - 1u : 0u);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] = (vis >> (8 * (i / 4) + 4 * h2 + i % 4)) & 1u ? s[i] : -INFINITY;
-      }
-      float mx = s[0];
+        for (int qt = 0; qt < QT; ++qt) {
+          const unsigned int vis = there & (tree ? (unsigned int)((row0 < 64 ? mw0[qt] : mw1[qt]) >> (row0 & 63)) : 0xffffffffu);
 #pragma unroll
-      for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
-      // The reference only has to be near the maximum: it is moved when a score exceeds it by more than 2^8, so that P stays
-      // below 256; the two lanes of a row then agree on the larger.
-      if (__builtin_amdgcn_ballot_w64((mx - m_run) * p.sl2 > 8.0f) != 0ull) {
-        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-        if ((mx - m_run) * p.sl2 > 8.0f) {
-          const float alpha = __builtin_amdgcn_exp2f((m_run - mx) * p.sl2);  // 0 on first use
-          l_run *= alpha;
-#pragma unroll
-          for (int dt = 0; dt < DT; ++dt) o[dt] *= alpha;
-          m_run = mx;
+          for (int i = 0; i < 16; ++i) s[qt][i] = (vis >> (8 * (i / 4) + 4 * h2 + i % 4)) & 1u ? s[qt][i] : -INFINITY;
         }
       }
-      const float ms = (m_run > -INFINITY ? m_run : 0.f) * p.sl2;
-      float sum = 0.f;
+    };
+    // The reference only has to be near the maximum: it is moved when a score exceeds it by more than 2^8, so that P stays
+    // below 256; the two lanes of a row then agree on the larger.
+    auto reference = [&](const float (&mx)[QT]) __attribute__((always_inline)) {
+      bool far = false;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], p.sl2, -ms));
-        sum += s[i];
+      for (int qt = 0; qt < QT; ++qt) far |= (mx[qt] - m_run[qt]) * p.sl2 > 8.0f;
+      if (__builtin_amdgcn_ballot_w64(far) != 0ull) {
+#pragma unroll
+        for (int qt = 0; qt < QT; ++qt) {
+          const float m = fmaxf(mx[qt], __shfl_xor(mx[qt], 32, 64));
+          if ((m - m_run[qt]) * p.sl2 > 8.0f) {
+            const float alpha = __builtin_amdgcn_exp2f((m_run[qt] - m) * p.sl2);  // 0 on first use
+            l_run[qt] *= alpha;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) o[qt][dt] *= alpha;
+            m_run[qt] = m;
+          }
+        }
       }
-      l_run += sum;
-      // A value that is no number or infinite must not reach the rows that do not see its key, and 0 times it is no number: in
-      // a tile of tree nodes such values take part as 0 and are added afterwards where they are seen.
-      bool odd = false;
+    };
+
+    // Tile k at `tile`, its scores in s and the reference set for them; the next tile k1 at `next` (any1: it is part of the
+    // segment), whose scores go to sn; read_next() requests the first fragments of the tile behind it.
+    auto step = [&](int k, unsigned int tile, int k1, bool any1, unsigned int next, f32x16 (&s)[QT], f32x16 (&sn)[QT], auto&& read_next,
+                    const unsigned long long (&mw0)[QT], const unsigned long long (&mw1)[QT]) __attribute__((always_inline)) {
+      const bool tree = OWN && k >= ctx_tiles;
+      const unsigned int ka = next + kplace, va = tile + TILE + vplace;
+      float ms[QT], sum[QT], mx[QT];
+#pragma unroll
+      for (int qt = 0; qt < QT; ++qt) {
+        ms[qt] = (m_run[qt] > -INFINITY ? m_run[qt] : 0.f) * p.sl2;
+        sum[qt] = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sn[qt][i] = 0.f;
+      }
+      // A value that is no number or infinite must not reach the rows that do not see its key, and 0 times it is no number: in a
+      // tile of tree nodes such values take part as 0, and the join adds them where they are seen.
       if constexpr (SH::F32) {
+#pragma unroll
+        for (int i = 0; i < QU; ++i) {
+          score(i, sn);
+          if (i + kAhead < QU) a[i % kAhead] = lds_read<u32x4>(ka ^ ((i + kAhead) << 5));
+        }
+#pragma unroll
+        for (int qt = 0; qt < QT; ++qt)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            s[qt][i] = __builtin_amdgcn_exp2f(fmaf(s[qt][i], p.sl2, -ms[qt]));
+            sum[qt] += s[qt][i];
+          }
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
-            float a = lds_read<float>((va ^ (dt << 7)) + (8 * (i / 4) + i % 4) * ROWB);
+            float x = lds_read<float>((va ^ (dt << 7)) + (8 * (i / 4) + i % 4) * ROWB);
             if (tree) {
-              const bool bad = (__float_as_uint(a) & 0x7f800000u) == 0x7f800000u;
+              const bool bad = (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u;
               odd |= bad;
-              a = bad ? 0.f : a;
+              x = bad ? 0.f : x;
             }
-            o[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, s[i], o[dt], 0, 0, 0);
-          }
-      } else {
-        u32x4 hi[2], lo[2];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float p0 = s[2 * i], p1 = s[2 * i + 1];
-          if constexpr (SH::FINE) {
-            // P = hi + lo: hi is P cut to its upper 16 bits, lo the rounded rest
-            const unsigned int u0 = __float_as_uint(p0), u1b = __float_as_uint(p1);
-            hi[i / 4][i % 4] = __builtin_amdgcn_perm(u1b, u0, 0x07060302u);
-            lo[i / 4][i % 4] = __builtin_bit_cast(
-                unsigned int, bf16x2{(__bf16)(p0 - __uint_as_float(u0 & 0xffff0000u)), (__bf16)(p1 - __uint_as_float(u1b & 0xffff0000u))});
-          } else {
-            // rounded to bf16, as the values are and as the result will be
-            hi[i / 4][i % 4] = __builtin_bit_cast(unsigned int, bf16x2{(__bf16)p0, (__bf16)p1});
+            for (int qt = 0; qt < QT; ++qt) o[qt][dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, s[qt][i], o[qt][dt], 0, 0, 0);
           }
+        read_next();
+        hide(k1, any1, sn, mw0, mw1);
+#pragma unroll
+        for (int qt = 0; qt < QT; ++qt) {
+          mx[qt] = sn[qt][0];
+#pragma unroll
+          for (int i = 1; i < 16; ++i) mx[qt] = fmaxf(mx[qt], sn[qt][i]);
         }
+      } else {
+        u32x4 hi[QT][2], lo[QT][2];
+        s16x4 vr[DT][2][2];
+        auto exponentials = [&](int from, int to) __attribute__((always_inline)) {  // pairs of registers
+#pragma unroll
+          for (int j = from; j < to; ++j)
+#pragma unroll
+            for (int qt = 0; qt < QT; ++qt) {
+              // P is rounded to bf16, as the values are and as the result will be; FINE: P = hi + lo, within 2^-17 of it
+              const float p0 = __builtin_amdgcn_exp2f(fmaf(s[qt][2 * j], p.sl2, -ms[qt]));
+              const float p1 = __builtin_amdgcn_exp2f(fmaf(s[qt][2 * j + 1], p.sl2, -ms[qt]));
+              sum[qt] += p0 + p1;
+              asm volatile("" : "+v"(sum[qt]));  // (here, not at the end of the tile)
+              const unsigned int h = __builtin_bit_cast(unsigned int, bf16x2{(__bf16)p0, (__bf16)p1});
+              hi[qt][j / 4][j % 4] = h;
+              if constexpr (SH::FINE)
+                lo[qt][j / 4][j % 4] = __builtin_bit_cast(
+                    unsigned int, bf16x2{(__bf16)(p0 - __uint_as_float(h << 16)), (__bf16)(p1 - __uint_as_float(h & 0xffff0000u))});
+            }
+        };
+        constexpr int kReads = 4 * DT / QU;
+#pragma unroll
+        for (int i = 0; i < QU; ++i) {
+          __builtin_amdgcn_sched_barrier(0);
+          score(i, sn);
+          if (i + kAhead < QU) a[i % kAhead] = lds_read<u32x4>(ka ^ ((i + kAhead) << 5));
+#pragma unroll
+          for (int j = i * kReads; j < (i + 1) * kReads; ++j) {
+            const int dt = j / 2 % DT, half = j % 2, kb = j / (2 * DT);
+            vr[dt][kb][half] = lds_read_tr((va ^ (dt << 6)) + (16 * kb + 8 * half) * ROWB);
+          }
+          exponentials(i * kPairsA / QU, (i + 1) * kPairsA / QU);
+        }
+        __builtin_amdgcn_sched_barrier(0);
         if (tree) {
 #pragma unroll
           for (int dt = 0; dt < DT; ++dt)
@@ -419,107 +494,169 @@ __global__ __launch_bounds__(64 * SH::NW) void prefix_attn_kernel(PrefixAttnPara
             for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
               for (int e = 0; e < 8; ++e) {
-                const bool bad = (v[dt][kb][e] & 0x7f80) == 0x7f80;
+                const short x = vr[dt][kb][e / 4][e % 4];
+                const bool bad = (x & 0x7f80) == 0x7f80;
                 odd |= bad;
-                v[dt][kb][e] = bad ? (short)0 : v[dt][kb][e];
+                vr[dt][kb][e / 4][e % 4] = bad ? (short)0 : x;
               }
         }
+        auto value = [&](int dt, int kb, const u32x4 (&w)[QT][2]) __attribute__((always_inline)) {
+          const s16x4 v0 = vr[dt][kb][0], v1 = vr[dt][kb][1];
+          const bf16x8 v = __builtin_bit_cast(bf16x8, s16x8{v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]});
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
+          for (int qt = 0; qt < QT; ++qt) o[qt][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(bf16x8, w[qt][kb]), o[qt][dt], 0, 0, 0);
+        };
 #pragma unroll
-          for (int dt = 0; dt < DT; ++dt)
-            o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v[dt][kb]), __builtin_bit_cast(bf16x8, hi[kb]), o[dt], 0, 0, 0);
+        for (int dt = 0; dt < DT; ++dt) {
+          __builtin_amdgcn_sched_barrier(0);
+          value(dt, 0, hi);
+          exponentials(kPairsA + dt * (8 - kPairsA) / DT, kPairsA + (dt + 1) * (8 - kPairsA) / DT);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        read_next();
+        hide(k1, any1, sn, mw0, mw1);
         if constexpr (SH::FINE) {
 #pragma unroll
-          for (int kb = 0; kb < 2; ++kb)
+          for (int dt = 0; dt < DT; ++dt) value(dt, 0, lo);
+        }
 #pragma unroll
-            for (int dt = 0; dt < DT; ++dt)
-              o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v[dt][kb]), __builtin_bit_cast(bf16x8, lo[kb]), o[dt], 0, 0, 0);
+        for (int dt = 0; dt < DT; ++dt) {
+          __builtin_amdgcn_sched_barrier(0);
+          value(dt, 1, hi);
+#pragma unroll
+          for (int qt = 0; qt < QT; ++qt)
+#pragma unroll
+            for (int i = dt * 16 / DT; i < (dt + 1) * 16 / DT; ++i) mx[qt] = i == 0 ? sn[qt][0] : fmaxf(mx[qt], sn[qt][i]);
+#pragma unroll
+          for (int qt = 0; qt < QT; ++qt) asm volatile("" : "+v"(mx[qt]));
+        }
+        if constexpr (SH::FINE) {
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt) value(dt, 1, lo);
         }
       }
-      if (tree && __builtin_amdgcn_ballot_w64(odd) != 0ull) {
-        for (int key = 0; key < (left < 32 ? left : 32); ++key) {
-          const bool seen = (vis >> key) & 1u;
 #pragma unroll
-          for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const int at = (32 * dt + 8 * (i / 4) + 4 * h2 + i % 4) * SH::ES;
-              const unsigned int place = tile + TILE + key * ROWB + (((at >> 4) ^ SH::fv(key)) << 4) + (at & 15);
-              float v;
-              if constexpr (SH::F32) v = lds_read<float>(place);
-              else v = bf16_bits_to_float(lds_read<unsigned short>(place));
-              if (seen && (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u) o[dt][i] += v;
-            }
-        }
-      }
+      for (int qt = 0; qt < QT; ++qt) l_run[qt] += sum[qt];
+      reference(mx);
     };
 
-    // ---- the loop: two stages; the next iteration's tiles are in registers, and in LDS behind the first of this one's ------
-    load(0, kc, vc, kt, vt);
-    commit(0);
-    load(1, kc, vc, kt, vt);
+    // ---- the loop ---------------------------------------------------------------------------------------------------------
+    // arrive(i): stage i + 1 is there - this wavefront's requests are counted, those of the others stand behind the barrier -, and
+    // all reads of stage i - 1 lie behind it: its place takes stage i - 1 + NS.  (Behind the last stage requests read nothing, but
+    // are made, so that the wait can count.)
+    const unsigned int mine = kp * KT * 2 * TILE;  // this wavefront's tiles of a stage
+    auto place = [&](int i) __attribute__((always_inline)) { return lds0 + i % SH::NS * SH::STAGE + mine; };
+    auto arrive = [&](int i) __attribute__((always_inline)) {
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"((SH::NS - 3) * NREQ) : "memory");
+      lds_barrier();
+      request(i - 1 + SH::NS, kc, vc, kt, vt);
+    };
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((SH::NS - 1 - kEarly) * NREQ) : "memory");
     lds_barrier();
-    for (int i = 0; i < niter; ++i) {
-      const int stage = i & 1;
+    if (live_wave) {
+      read_keys(place(0));
 #pragma unroll
-      for (int q = 0; q < SH::KT; ++q) {
-        if (live_wave)
-          compute((it0 + i) * TPI + kp * SH::KT + q, lds0 + stage * SH::STAGE + (kp * SH::KT + q) * 2 * TILE, mw0, mw1);
-        if (q == 0) {
-          commit(stage ^ 1);
-          load(i + 2, kc, vc, kt, vt);
-        }
+      for (int qt = 0; qt < QT; ++qt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[qt][i] = 0.f;
+#pragma unroll
+      for (int i = 0; i < QU; ++i) {
+        score(i, s);
+        if (i + kAhead < QU) a[i % kAhead] = lds_read<u32x4>((place(0) + kplace) ^ ((i + kAhead) << 5));
       }
-      lds_barrier();  // (not __syncthreads(): the loads stay in flight)
+      hide(it0 * TPI + kp * KT, true, s, mw0, mw1);
+      float mx[QT];
+#pragma unroll
+      for (int qt = 0; qt < QT; ++qt) {
+        mx[qt] = s[qt][0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) mx[qt] = fmaxf(mx[qt], s[qt][i]);
+      }
+      reference(mx);
+      if constexpr (KT > 1) read_keys(place(0) + 2 * TILE);
     }
+    for (int i = 0; i < niter; ++i) {
+      if constexpr (KT == 1) {
+        arrive(i);
+        const int k = (it0 + i) * TPI + kp;
+        if (live_wave) {
+          read_keys(place(i + 1));
+          step(k, place(i), k + TPI, i + 1 < niter, place(i + 1), s, s2, []() {}, mw0, mw1);
+#pragma unroll
+          for (int qt = 0; qt < QT; ++qt) s[qt] = s2[qt];
+        }
+      } else {
+        static_assert(KT == 2);
+        const int k = (it0 + i) * TPI + kp * 2;
+        const unsigned int at = place(i), then = place(i + 1);
+        if (live_wave)
+          step(k, at, k + 1, true, at + 2 * TILE, s, s2, [&]() __attribute__((always_inline)) { arrive(i); read_keys(then); }, mw0, mw1);
+        else
+          arrive(i);
+        if (live_wave)
+          step(k + 1, at + 2 * TILE, k + TPI, i + 1 < niter, then, s2, s, [&]() __attribute__((always_inline)) { read_keys(then + 2 * TILE); }, mw0, mw1);
+      }
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    if (OWN && __builtin_amdgcn_ballot_w64(odd) != 0ull) table[kOdd][0] = 1;
+    __syncthreads();  // every request has landed, every tile is consumed: the LDS is free
+    if (OWN && threadIdx.x == 0) p.odd[slot] = table[kOdd][0];
 
     // ---- the key parts of a row group joined ------------------------------------------------------------------------------
     if constexpr (SH::KP > 1) {
       float* part = (float*)smem;
       if (kp > 0) {
-        float* mine = part + ((kp - 1) * SH::CW + rg) * (SH::PART / 4) + lane * 4;
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) *(f32x4*)(mine + (dt * 4 + i) * 256) = f32x4{o[dt][4 * i], o[dt][4 * i + 1], o[dt][4 * i + 2], o[dt][4 * i + 3]};
-        float* ml = part + ((kp - 1) * SH::CW + rg) * (SH::PART / 4) + DT * 16 * 64;
-        ml[lane] = m_run;
-        ml[64 + lane] = l_run;
-      }
-      __syncthreads();
-      if (kp == 0) {
-        for (int q = 0; q < SH::KP - 1; ++q) {
-          const float* its = part + (q * SH::CW + rg) * (SH::PART / 4);
-          const float mo = its[DT * 16 * 64 + lane], lo = its[DT * 16 * 64 + 64 + lane];
-          const float m = fmaxf(m_run, mo), base = m > -INFINITY ? m : 0.f;
-          const float a0 = __builtin_amdgcn_exp2f((m_run - base) * p.sl2), a1 = __builtin_amdgcn_exp2f((mo - base) * p.sl2);
-          l_run = l_run * a0 + lo * a1;
+        for (int qt = 0; qt < QT; ++qt) {
+          float* its = part + (((kp - 1) * SH::CW + rg) * QT + qt) * (SH::PART / 4);
 #pragma unroll
           for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const f32x4 v = *(const f32x4*)(its + lane * 4 + (dt * 4 + i) * 256);
-#pragma unroll
-              for (int e = 0; e < 4; ++e) o[dt][4 * i + e] = o[dt][4 * i + e] * a0 + v[e] * a1;
-            }
-          m_run = m;
+            for (int i = 0; i < 4; ++i)
+              *(f32x4*)(its + seg_lane * 4 + (dt * 4 + i) * 256) = f32x4{o[qt][dt][4 * i], o[qt][dt][4 * i + 1], o[qt][dt][4 * i + 2], o[qt][dt][4 * i + 3]};
+          its[DT * 1024 + seg_lane] = m_run[qt];
+          its[DT * 1024 + 64 + seg_lane] = l_run[qt];
         }
       }
-      __syncthreads();  // (the next segment's requests write there)
+      __syncthreads();
+      if (kp == 0) {
+#pragma unroll
+        for (int qt = 0; qt < QT; ++qt)
+          for (int q = 0; q < SH::KP - 1; ++q) {
+            const float* its = part + ((q * SH::CW + rg) * QT + qt) * (SH::PART / 4);
+            const float mo = its[DT * 1024 + seg_lane], lother = its[DT * 1024 + 64 + seg_lane];
+            const float m = fmaxf(m_run[qt], mo), base = m > -INFINITY ? m : 0.f;
+            const float a0 = __builtin_amdgcn_exp2f((m_run[qt] - base) * p.sl2), a1 = __builtin_amdgcn_exp2f((mo - base) * p.sl2);
+            l_run[qt] = l_run[qt] * a0 + lother * a1;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const f32x4 x = *(const f32x4*)(its + seg_lane * 4 + (dt * 4 + i) * 256);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[qt][dt][4 * i + e] = o[qt][dt][4 * i + e] * a0 + x[e] * a1;
+              }
+            m_run[qt] = m;
+          }
+      }
+      __syncthreads();  // (the next segment's tiles go there)
     }
     // ---- what the segment leaves, in the order of the registers -------------------------------------------------------------
     if (kp == 0 && live_wave) {
-      l_run += __shfl_xor(l_run, 32, 64);
-      float* po = p.po + ((size_t)slot * SH::CW + rg) * (DT * 1024) + lane * 4;
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt)
+      for (int qt = 0; qt < QT; ++qt) {
+        l_run[qt] += __shfl_xor(l_run[qt], 32, 64);
+        float* po = p.po + ((size_t)slot * (R / 32) + rg * QT + qt) * (DT * 1024) + seg_lane * 4;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) *(f32x4*)(po + (dt * 4 + i) * 256) = f32x4{o[dt][4 * i], o[dt][4 * i + 1], o[dt][4 * i + 2], o[dt][4 * i + 3]};
-      if (h2 == 0) {
-        float* ml = p.pml + (size_t)slot * 2 * R + rg * 32 + c;
-        ml[0] = m_run * p.sl2;
-        ml[R] = l_run;
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            *(f32x4*)(po + (dt * 4 + i) * 256) = f32x4{o[qt][dt][4 * i], o[qt][dt][4 * i + 1], o[qt][dt][4 * i + 2], o[qt][dt][4 * i + 3]};
+        if (sh == 0) {
+          float* ml = p.pml + (size_t)slot * 2 * R + (rg * QT + qt) * 32 + sc;
+          ml[0] = m_run[qt] * p.sl2;
+          ml[R] = l_run[qt];
+        }
       }
     }
   }
@@ -530,6 +667,7 @@ __global__ __launch_bounds__(64 * SH::NW) void prefix_attn_kernel(PrefixAttnPara
 struct PrefixJoinParams {
   PrefixAttnParams a;
   const float *prefix_o, *prefix_ml, *own_o, *own_ml;
+  const int* own_odd;
   int out_bf16;
   void* out;   // [B][H][max_nodes][dh]
   float* lse;  // [B][H][max_nodes] or null
@@ -537,30 +675,30 @@ struct PrefixJoinParams {
 
 // One workgroup of DHP / 32 wavefronts per (32 rows of a sequence, key head): every wavefront weighs the rows' partial results
 // and adds up 32 components of them, in ascending order of the slots.
-template <int DHP, int RP, int RO, int TPIP, int TPIO>
-__global__ __launch_bounds__(2 * DHP) void prefix_join_kernel(PrefixJoinParams p) {
-  constexpr int DT = DHP / 32;
+template <typename SP, typename SO>
+__global__ __launch_bounds__(2 * SP::DHP) void prefix_join_kernel(PrefixJoinParams p) {
+  constexpr int DT = SP::DT, RP = SP::R, RO = SO::R;
   const int lane = threadIdx.x & 63, dt = threadIdx.x >> 6, c = lane & 31, h2 = lane >> 5;
   const int kh = blockIdx.y, b = blockIdx.z, r = blockIdx.x * 32 + c;
   const Batch t = read_batch(p.a);
-  const auto pb = Blocks<false, RP, TPIP>::make(p.a, t);
-  const auto ob = Blocks<true, RO, TPIO>::make(p.a, t);
+  const auto pb = Blocks<false, RP, SP::TPI>::make(p.a, t);
+  const auto ob = Blocks<true, RO, SO::TPI>::make(p.a, t);
   const int n = __builtin_amdgcn_readlane(t.n, b);
   if ((int)blockIdx.x * 32 >= n * p.a.group) return;
   const bool live = r < n * p.a.group;
-  const Deal pd = prefix_deal(pb.units), od = prefix_deal(ob.units);
+  const Deal pd = prefix_deal(pb.units, SP::GROUPS), od = prefix_deal(ob.units, SO::GROUPS);
   // this row's place among all rows of the key head and in its sequence; the slots of its blocks
   const int rr = live ? r : 0;
   const int rp = __builtin_amdgcn_readlane(t.first, b) * p.a.group + rr;
   int w0 = 0, w1 = -1, item = 0;
   if (pb.iters > 0) {
     item = kh * pb.blocks + rp / RP;
-    w0 = pd.owner((long long)item * pb.iters);
-    w1 = pd.owner((long long)item * pb.iters + pb.iters - 1);
+    w0 = pd.owner(item * pb.iters);
+    w1 = pd.owner(item * pb.iters + pb.iters - 1);
   }
   const int oi = __builtin_amdgcn_readlane(ob.iters, b), onb = __builtin_amdgcn_readlane(ob.blocks, b);
   const int oitem = kh * onb + rr / RO;
-  const long long ou = __shfl(ob.unit0, b, 64) + (long long)oitem * oi;
+  const int ou = __builtin_amdgcn_readlane(ob.unit0, b) + oitem * oi;
   const int x0 = od.owner(ou), x1 = od.owner(ou + oi - 1), oslot = __builtin_amdgcn_readlane(ob.block0, b) + oitem;
   const float* pml = p.prefix_ml + (size_t)item * 2 * RP + rp % RP;
   const float* oml = p.own_ml + (size_t)oslot * 2 * RO + rr % RO;
@@ -588,6 +726,27 @@ __global__ __launch_bounds__(2 * DHP) void prefix_join_kernel(PrefixJoinParams p
   }
   if (!live) return;
   const int node = r / p.a.group, hg = r - node * p.a.group;
+  int odd = 0;
+  for (int w = x0; w <= x1; ++w) odd |= p.own_odd[w + oslot];
+  if (odd) {  // values of tree nodes that are infinite or not a number, left out so far: into the rows that see them
+    const int W = (p.a.max_nodes + 63) >> 6;
+    const unsigned long long* mask = p.a.anc_mask + ((size_t)b * p.a.max_nodes + node) * W;
+    const unsigned char* vt = p.a.v_tree + ((size_t)b * p.a.H_kv + kh) * p.a.max_nodes * p.a.dh * SP::ES;
+    for (int j = 0; j < n; ++j) {
+      if (!((mask[j >> 6] >> (j & 63)) & 1ull)) continue;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int at = 32 * dt + 8 * i + 4 * h2 + e;
+          if (at >= p.a.dh) continue;
+          float v;
+          if constexpr (SP::F32) v = ((const float*)vt)[(size_t)j * p.a.dh + at];
+          else v = bf16_bits_to_float(((const unsigned short*)vt)[(size_t)j * p.a.dh + at]);
+          if ((__float_as_uint(v) & 0x7f800000u) == 0x7f800000u) o[i][e] += v;
+        }
+    }
+  }
   const size_t row = ((size_t)b * p.a.H + kh * p.a.group + hg) * p.a.max_nodes + node;
   const bool none = m == -INFINITY && l == 0.f;  // no key at all
   const float inv = none ? 0.f : 1.0f / l;
@@ -609,12 +768,13 @@ __global__ __launch_bounds__(2 * DHP) void prefix_join_kernel(PrefixJoinParams p
 // ---- host side -----------------------------------------------------------------------------------------------------------
 template <bool F32, int DHP, int R, bool FINE>
 struct ShapeFor;
-template <int DHP, bool FINE> struct ShapeFor<false, DHP, 256, FINE> { using type = PrefixShape<false, DHP, 8, 1, 2, FINE>; };
-template <int DHP, bool FINE> struct ShapeFor<false, DHP, 128, FINE> { using type = PrefixShape<false, DHP, 4, 2, 1, FINE>; };
-template <int DHP, bool FINE> struct ShapeFor<false, DHP, 64, FINE> { using type = PrefixShape<false, DHP, 2, 4, 1, FINE>; };
-template <int DHP, bool FINE> struct ShapeFor<false, DHP, 32, FINE> { using type = PrefixShape<false, DHP, 1, 4, 1, FINE>; };
-template <int DHP> struct ShapeFor<true, DHP, 128, true> { using type = PrefixShape<true, DHP, 4, 1, 1, true>; };
-template <int DHP> struct ShapeFor<true, DHP, 32, true> { using type = PrefixShape<true, DHP, 1, 2, 1, true>; };
+//                                                                                        F32   DHP  QT CW KP KT NS WPE
+template <int DHP, bool FINE> struct ShapeFor<false, DHP, 256, FINE> { using type = PrefixShape<false, DHP, 1, 8, 1, 2, 4, 2, FINE>; };
+template <int DHP, bool FINE> struct ShapeFor<false, DHP, 128, FINE> { using type = PrefixShape<false, DHP, 1, 4, 2, 1, 4, 2, FINE>; };
+template <int DHP, bool FINE> struct ShapeFor<false, DHP, 64, FINE> { using type = PrefixShape<false, DHP, 1, 2, 2, 1, 4, 1, FINE>; };
+template <int DHP, bool FINE> struct ShapeFor<false, DHP, 32, FINE> { using type = PrefixShape<false, DHP, 1, 1, 2, 1, 4, 1, FINE>; };
+template <int DHP> struct ShapeFor<true, DHP, 128, true> { using type = PrefixShape<true, DHP, 1, 4, 1, 1, 4, 1, true>; };
+template <int DHP> struct ShapeFor<true, DHP, 32, true> { using type = PrefixShape<true, DHP, 1, 1, DHP == 64 ? 2 : 1, 1, 3, 1, true>; };
 
 // f(shape tag) for the shape that R, dh, the type and the precision of P ask for
 template <bool F32, int DHP, bool FINE, typename F>
@@ -647,7 +807,8 @@ hipError_t prepare_prefix_attn() {
           e = with_shape(f32, dhp, fine, rows, [](auto shape) {
             using SH = decltype(shape);
             const hipError_t e1 = hipFuncSetAttribute((const void*)prefix_attn_kernel<SH, false>, hipFuncAttributeMaxDynamicSharedMemorySize, SH::LDS);
-            return e1 != hipSuccess ? e1 : hipFuncSetAttribute((const void*)prefix_attn_kernel<SH, true>, hipFuncAttributeMaxDynamicSharedMemorySize, SH::LDS);
+            if constexpr (SH::R > kPrefixOwnRows) return e1;
+            else return e1 != hipSuccess ? e1 : hipFuncSetAttribute((const void*)prefix_attn_kernel<SH, true>, hipFuncAttributeMaxDynamicSharedMemorySize, SH::LDS);
           });
         }
   return e;
@@ -685,6 +846,9 @@ extern "C" int prefix_verify_attn(ctcspec_ctx* ctx, ctcspec_dtype dt, const void
   CTCSPEC_REQUIRE(ctx, B <= ctx->lim.max_batch && B <= 64 && max_nodes <= ctx->lim.max_nodes && H <= ctx->lim.max_heads &&
                            dh <= ctx->lim.max_head_dim && H_kv <= 65535,
                   CTCSPEC_EUNSUPPORTED, "prefix_verify_attn: shape exceeds the context's limits");
+  CTCSPEC_REQUIRE(ctx, prefix_units_fit(1, H_kv, (long long)B * max_nodes * (H / H_kv), prefix_cap, 0) &&
+                           prefix_units_fit(B, H_kv, (long long)max_nodes * (H / H_kv), kv_cap, max_nodes),
+                  CTCSPEC_EUNSUPPORTED, "prefix_verify_attn: capacities of this size need more than 32 bits for the work's units");
   for (const void* a : {q, k_prefix, v_prefix, k_cache, v_cache, k_tree, v_tree, (const void*)workspace, (const void*)out})
     CTCSPEC_REQUIRE(ctx, aligned16(a), CTCSPEC_EINVAL, "prefix_verify_attn: pointers must be 16-byte aligned");
   const bool f32 = dt == CTCSPEC_F32, fine = out_dt == CTCSPEC_F32;
@@ -703,7 +867,7 @@ extern "C" int prefix_verify_attn(ctcspec_ctx* ctx, ctcspec_dtype dt, const void
   p.prefix_cap = prefix_cap; p.kv_cap = kv_cap; p.B = B; p.H = H; p.H_kv = H_kv; p.group = H / H_kv; p.dh = dh; p.max_nodes = max_nodes;
   p.sl2 = scale * 1.4426950408889634f;
   j.prefix_o = (float*)(base + ws.prefix_o); j.prefix_ml = (float*)(base + ws.prefix_ml);
-  j.own_o = (float*)(base + ws.own_o); j.own_ml = (float*)(base + ws.own_ml);
+  j.own_odd = p.odd = (int*)(base + ws.own_odd); j.own_o = (float*)(base + ws.own_o); j.own_ml = (float*)(base + ws.own_ml);
   j.out_bf16 = out_dt == CTCSPEC_BF16; j.out = out; j.lse = lse;
   const int dhp = prefix_padded_dim(dh);
   hipStream_t st = ctx->stream;
@@ -711,18 +875,18 @@ extern "C" int prefix_verify_attn(ctcspec_ctx* ctx, ctcspec_dtype dt, const void
     using SP = decltype(prefix_shape);
     p.po = (float*)(base + ws.prefix_o);
     p.pml = (float*)(base + ws.prefix_ml);
-    hipLaunchKernelGGL((prefix_attn_kernel<SP, false>), dim3(kPrefixGroups), dim3(64 * SP::NW), SP::LDS, st, p);
+    hipLaunchKernelGGL((prefix_attn_kernel<SP, false>), dim3(SP::GROUPS), dim3(64 * SP::NW), SP::LDS, st, p);
     if (const hipError_t e1 = hipGetLastError(); e1 != hipSuccess) return e1;
     return with_rows<SP::F32, SP::DHP, SP::FINE>(ws.own_rows, [&](auto own_shape) {
       using SO = decltype(own_shape);
-      if constexpr (SO::R > SP::R) {
+      if constexpr (SO::R > SP::R || SO::R > kPrefixOwnRows) {
         return hipErrorInvalidValue;  // (one sequence's rows are among all rows)
       } else {
         p.po = (float*)(base + ws.own_o);
         p.pml = (float*)(base + ws.own_ml);
-        hipLaunchKernelGGL((prefix_attn_kernel<SO, true>), dim3(kPrefixGroups), dim3(64 * SO::NW), SO::LDS, st, p);
+        hipLaunchKernelGGL((prefix_attn_kernel<SO, true>), dim3(SO::GROUPS), dim3(64 * SO::NW), SO::LDS, st, p);
         if (const hipError_t e1 = hipGetLastError(); e1 != hipSuccess) return e1;
-        hipLaunchKernelGGL((prefix_join_kernel<SP::DHP, SP::R, SO::R, SP::TPI, SO::TPI>),
+        hipLaunchKernelGGL((prefix_join_kernel<SP, SO>),
                            dim3((unsigned)((max_nodes * p.group + 31) / 32), (unsigned)H_kv, (unsigned)B), dim3(2 * SP::DHP), 0, st, j);
         return hipGetLastError();
       }

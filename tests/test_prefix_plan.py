@@ -14,15 +14,15 @@ PROGRAM = r"""
 #include "prefix_plan.h"
 using namespace ctcspec;
 // blocks of rows with so many units each -> 0 or what is wrong
-static int check(const long long* units, int blocks) {
+static int check(const long long* units, int blocks, int groups) {
   static bool taken[1 << 20];
   static long long covered[1 << 16];
   long long total = 0;
   for (int i = 0; i < blocks; ++i) { total += units[i]; covered[i] = 0; }
-  const Deal d = prefix_deal(total);
-  if (d.groups > kPrefixGroups || (total > 0) != (d.groups > 0)) return 1;
+  const Deal d = prefix_deal((int)total, groups);
+  if (d.groups > groups || (total > 0) != (d.groups > 0)) return 1;
   if (d.begin(d.groups) != total) return 2;
-  for (int s = 0; s < kPrefixGroups + blocks; ++s) taken[s] = false;
+  for (int s = 0; s < groups + blocks; ++s) taken[s] = false;
   long long start = 0;
   int block = 0;
   for (int w = 0; w < d.groups; ++w) {
@@ -34,7 +34,7 @@ static int check(const long long* units, int blocks) {
       while (u >= start + units[block]) start += units[block++];
       const long long room = start + units[block] - u, n = room < u1 - u ? room : u1 - u;
       const int slot = w + block;
-      if (slot >= kPrefixGroups + blocks || taken[slot]) return 5;
+      if (slot >= groups + blocks || taken[slot]) return 5;
       taken[slot] = true;
       covered[block] += n;
       u += n;
@@ -48,7 +48,7 @@ int main() {
   static long long units[1 << 16];
   while (scanf("%d", &blocks) == 1) {
     for (int i = 0; i < blocks; ++i) if (scanf("%lld", units + i) != 1) return 1;
-    printf("%d\n", check(units, blocks));
+    printf("%d\n", check(units, blocks, kPrefixMaxGroups) + 10 * check(units, blocks, 256));
   }
 }
 """
@@ -64,7 +64,7 @@ def program(tmp_path_factory):
 
 def test_every_unit_once_and_every_partial_result_in_its_own_place(program):
     rng = random.Random(1)
-    cases = [[1], [0, 0, 1, 0], [2], [255], [256], [257], [511], [513], [1] * 300, [0] * 5, [1 << 33, 3], [7] * 5000]
+    cases = [[1], [0, 0, 1, 0], [2], [255], [256], [257], [511], [513], [1] * 300, [0] * 5, [1 << 30, 3], [7] * 5000]
     for _ in range(400):
         n = rng.choice([1, 2, 8, 32, 65, 700])
         most = rng.choice([1, 3, 40, 5000])
