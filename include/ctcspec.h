@@ -466,7 +466,8 @@ int ctc_loss(ctcspec_ctx* ctx, const float* logits, const int32_t* labels, const
  *
  * dt            element type of q and of all keys and values
  * q             [B,H,max_nodes,dh]
- * k_prefix, v_prefix  [H_kv,prefix_cap,dh]; prefix_len [1] int32 device (0 is allowed; rows beyond are not read)
+ * k_prefix, v_prefix  [H_kv,prefix_cap,dh], NULL only with prefix_cap 0; prefix_len [1] int32 device (0 is allowed; rows
+ *               beyond are not read)
  * k_cache, v_cache, kv_off, ctx_len, kv_cap   as for tree_verify_attn, with [H_kv][kv_cap][dh] per sequence
  * k_tree, v_tree [B,H_kv,max_nodes,dh]
  * n_nodes, anc_mask   as for tree_verify_attn

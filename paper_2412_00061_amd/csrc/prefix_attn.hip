@@ -2,16 +2,15 @@
 //
 //   out[b,h,i] = sum_j p_j v_j,  p = softmax over the prefix's keys, the sequence's cached keys and the tree nodes it sees
 //
-// Softmax parts over disjoint keys join exactly: (O, m, l) with O = sum exp2(s - m) v, l = sum exp2(s - m).  So the prefix is a
-// pass of its own in which the rows of ALL sequences (and of the heads that share a key head) stand side by side against
-// each key tile - read and multiplied once for the batch -, the sequences' own keys are a second pass, and a third kernel joins
-// what the two left.
+// Softmax parts over disjoint keys join exactly: (O, m, l) with O = sum exp2(s - m) v, l = sum exp2(s - m).  So the rows of ALL
+// sequences (and of the heads that share a key head) stand side by side against each tile of the prefix's keys - read and
+// multiplied once for the batch -, every sequence's rows against its own keys, and a second kernel joins what they left.
 //
-// Both passes run prefix_attn_kernel.  The work is cut into units - one iteration over the keys (KP * KT tiles of 32) for one
-// block of R rows - and the units of a pass, in the order (key head, row block, keys), are dealt to the workgroups in equal
-// consecutive shares: lengths, node counts and prefix length are read on the device, and no workgroup waits for a longer one.  A
-// workgroup whose share crosses from one block of rows into the next leaves a partial result for each.  Partial results are
-// numbered workgroup + block: consecutive ones differ in either, so no two share a number (prefix_plan.h).
+// prefix_attn_kernel: the work is cut into units - one iteration over the keys (KP * KT tiles of 32) for one block of R rows -
+// and the units, in the order (prefix: key head, row block, keys), (own: key head, sequence, row block, keys), are dealt to the
+// workgroups in equal consecutive shares: lengths, node counts and prefix length are read on the device, and no workgroup waits
+// for a longer one.  A workgroup whose share crosses from one block of rows into the next leaves a partial result for each, in a
+// place of its own (prefix_plan.h).
 #include <type_traits>
 #include <utility>
 
@@ -40,9 +39,9 @@ struct PrefixAttnParams {
   const unsigned long long* anc_mask;
   int prefix_cap, kv_cap, B, H, H_kv, group, dh, max_nodes;  // group: heads that share a key head
   float sl2;                      // scale * log2(e)
-  float* po;                      // partial O of the pass: [slot][R / 32][DHP / 32][4][64 lanes][4]
+  float* po;                      // partial O: [slot][R / 32][DHP / 32][4][64 lanes][4]
   float* pml;                     // [slot][2][R]: maximum in the log2 domain, sum
-  int* odd;                       // [slot] of the sequences' own keys: a value of a tree node is infinite or not a number
+  int* odd;                       // [slot]: a value of a tree node is infinite or not a number
 };
 
 // a value that is the same in every lane, in scalar registers
@@ -55,17 +54,21 @@ __device__ __forceinline__ const unsigned char* uniform(const unsigned char* p) 
   return (const unsigned char*)uniform((long long)p);
 }
 
-// what a pass or the join knows about the batch: lane b holds sequence b's (the limits allow 64 sequences)
-struct Batch {
-  int n, first;  // nodes, nodes of the sequences before it
-  int ctx;       // cached rows
-  int all;       // nodes of all sequences (uniform)
-  long long off; // kv_off
-  int prefix;    // rows of the prefix (uniform)
+// What both kernels know about the work: lane b holds sequence b's part (the limits allow 64 sequences), the rest is uniform.
+struct Work {
+  int n, first, ctx;          // lane: nodes, nodes of the sequences before it, cached rows
+  int blocks, iters;          // lane: blocks of the sequence's rows, iterations over its own keys
+  int unit0, block0;          // lane: units and blocks of the sequences before it, for one key head
+  long long off;              // lane: kv_off
+  int all, prefix;            // nodes of all sequences, rows of the prefix
+  int pblocks, piters;        // blocks of all rows, iterations over the prefix
+  int head_units, head_blocks;  // own units and blocks of a key head
+  int punits, pitems, units;  // units and blocks of the prefix over all key heads; all units
 };
-__device__ __forceinline__ Batch read_batch(const PrefixAttnParams& p) {
+template <int R, int TPI>
+__device__ __forceinline__ Work read_work(const PrefixAttnParams& p) {
   const int lane = threadIdx.x & 63;
-  Batch t{0, 0, 0, 0, 0, 0};
+  Work t{};
   const int P = *p.prefix_len;
   if (lane < p.B) {
     t.off = p.kv_off[lane];
@@ -73,55 +76,28 @@ __device__ __forceinline__ Batch read_batch(const PrefixAttnParams& p) {
     t.n = n < 0 ? 0 : (n > p.max_nodes ? p.max_nodes : n);
     t.ctx = L < 0 ? 0 : (L > p.kv_cap ? p.kv_cap : L);
   }
-  int sum = t.n;
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const int below = __shfl_up(sum, d, 64);
-    if (lane >= d) sum += below;
+  t.blocks = (t.n * p.group + R - 1) / R;
+  t.iters = t.n ? ((t.ctx + 31) / 32 + (t.n + 31) / 32 + TPI - 1) / TPI : 0;
+  int n = t.n, b = t.blocks, u = t.blocks * t.iters;
+  for (int d = 1; d < p.B; d *= 2) {
+    const int nb = __shfl_up(n, d, 64), bb = __shfl_up(b, d, 64), ub = __shfl_up(u, d, 64);
+    if (lane >= d) { n += nb; b += bb; u += ub; }
   }
-  t.first = sum - t.n;
-  t.all = __builtin_amdgcn_readlane(sum, 63);
+  t.first = n - t.n;
+  t.block0 = b - t.blocks;
+  t.unit0 = u - t.blocks * t.iters;
+  t.all = __builtin_amdgcn_readlane(n, p.B - 1);
+  t.head_blocks = __builtin_amdgcn_readlane(b, p.B - 1);
+  t.head_units = __builtin_amdgcn_readlane(u, p.B - 1);
   t.prefix = uniform(P < 0 ? 0 : (P > p.prefix_cap ? p.prefix_cap : P));
+  t.piters = ((t.prefix + 31) / 32 + TPI - 1) / TPI;
+  t.pblocks = uniform((t.all * p.group + R - 1) / R);
+  t.pitems = t.piters ? p.H_kv * t.pblocks : 0;
+  t.punits = t.pitems * t.piters;
+  t.units = t.punits + p.H_kv * t.head_units;
   return t;
 }
 
-// the blocks of rows of a pass
-template <bool OWN, int R, int TPI>
-struct Blocks {
-  // prefix: the same for all; own: lane b's sequence
-  int blocks, iters;  // row blocks of a key head, iterations over the keys
-  int unit0, block0;  // first unit and first block of the sequence, over its key heads
-  int units;          // of the pass (uniform)
-  __device__ __forceinline__ static Blocks make(const PrefixAttnParams& p, const Batch& t) {
-    Blocks k;
-    if constexpr (!OWN) {
-      k.blocks = uniform((t.all * p.group + R - 1) / R);
-      k.iters = ((t.prefix + 31) / 32 + TPI - 1) / TPI;
-      k.unit0 = 0;
-      k.block0 = 0;
-      k.units = p.H_kv * k.blocks * k.iters;
-    } else {
-      const int lane = threadIdx.x & 63;
-      k.blocks = (t.n * p.group + R - 1) / R;
-      k.iters = t.n ? ((t.ctx + 31) / 32 + (t.n + 31) / 32 + TPI - 1) / TPI : 0;
-      const int mine = p.H_kv * k.blocks;
-      int b = mine, u = mine * k.iters;
-#pragma unroll
-      for (int d = 1; d < 64; d *= 2) {
-        const int bb = __shfl_up(b, d, 64), ub = __shfl_up(u, d, 64);
-        if (lane >= d) { b += bb; u += ub; }
-      }
-      k.block0 = b - mine;
-      k.unit0 = u - mine * k.iters;
-      k.units = __builtin_amdgcn_readlane(u, 63);
-    }
-    return k;
-  }
-};
-
-// R = 32 QT CW rows, CW * KP wavefronts: wavefront w has rows [32 QT rg, 32 QT (rg + 1)), rg = w % CW, and of an iteration's
-// KP * KT key tiles the KT from kp * KT on, kp = w / CW; the KP parts are joined through LDS at the end.  Tiles (32 keys, K and
-// V) go straight into a ring of NS LDS stages.  FINE: P as two bf16 numbers.  WPE: wavefronts of a SIMD.
 constexpr int kPrefixTable = 10 * 64 * 4;
 template <bool F32_, int DHP_, int QT_, int CW_, int KP_, int KT_, int NS_, int WPE_, bool FINE_>
 struct PrefixShape {
@@ -158,7 +134,7 @@ __device__ __forceinline__ s16x4 lds_read_tr(unsigned int at) {
 }
 #endif
 
-template <typename SH, bool OWN>
+template <typename SH>
 __global__ __launch_bounds__(64 * SH::NW, SH::WPE) void prefix_attn_kernel(PrefixAttnParams p) {
 #if defined(__HIP_DEVICE_COMPILE__)  // (buffer descriptors exist on the device only)
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
@@ -174,9 +150,8 @@ __global__ __launch_bounds__(64 * SH::NW, SH::WPE) void prefix_attn_kernel(Prefi
   const int c = lane & 31, h2 = lane >> 5;
   const int rb = p.dh * SH::ES;  // bytes of a row
 
-  const Batch t = read_batch(p);
-  const Blocks<OWN, R, TPI> blocks = Blocks<OWN, R, TPI>::make(p, t);
-  const Deal d = prefix_deal(blocks.units, SH::GROUPS);
+  const Work t = read_work<R, TPI>(p);
+  const Deal d = prefix_deal(t.units, SH::GROUPS);
   // Workgroups go to the 8 XCDs in turn, each with an L2 of its own: consecutive shares - the row blocks of a key head, which
   // read the same keys - go to the same one.
   static_assert(SH::GROUPS % 8 == 0 && SH::GROUPS <= kPrefixMaxGroups);
@@ -185,18 +160,27 @@ __global__ __launch_bounds__(64 * SH::NW, SH::WPE) void prefix_attn_kernel(Prefi
   int u = uniform(d.begin(w));
   const int u1 = uniform(d.begin(w + 1));
   if (wave == 0) {
-    const int own[9] = {t.n, t.ctx, (int)t.off, (int)(t.off >> 32), t.first, blocks.blocks, blocks.iters, blocks.unit0, blocks.block0};
+    const int own[9] = {t.n, t.ctx, (int)t.off, (int)(t.off >> 32), t.first, t.blocks, t.iters, t.unit0, t.block0};
 #pragma unroll
     for (int i = 0; i < 9; ++i) table[i][lane] = own[i];
   }
   __syncthreads();
   auto of = [&](int what, int b) __attribute__((always_inline)) { return uniform(table[what][b]); };
-  const int all = t.all, prefix = t.prefix, pblocks = uniform(blocks.blocks), piters = uniform(blocks.iters);
+  const int all = t.all, prefix = t.prefix, pblocks = t.pblocks, piters = t.piters, punits = t.punits, pitems = t.pitems;
+  const int head_units = t.head_units, head_blocks = t.head_blocks;
 
-  // ---- requests: number x of a stage is tile x / (2 RQ), K then V, 1 KB (RPR rows) after 1 KB.  Lane l of a request fills the l-th
-  // 16 bytes of its kilobyte: with the chunk that belongs there.  The row's bits above those of lrow turn the chunks further,
-  // request by request (f(a + b) = f(a) ^ f(b)).
-  const int lrow = lane / (ROWB / 16), kchunk = lane % (ROWB / 16) ^ SH::fk(lrow), vchunk = lane % (ROWB / 16) ^ SH::fv(lrow);
+  // ---- requests: number x of a stage is tile x / (2 RQ), K then V, 1 KB (RPR rows) after 1 KB; this wavefront has NREQ in a
+  // row, of one operand tile or of several whole ones.  Lane l of a request fills the l-th 16 bytes of its kilobyte: with the
+  // chunk of the row that belongs there.
+  constexpr int kRun = NREQ < SH::RQ ? NREQ : SH::RQ, kOperands = NREQ / kRun;  // requests of an operand tile, operand tiles
+  static_assert(SH::RQ % kRun == 0 && NREQ % kRun == 0 && kOperands <= 2 && (kOperands == 1 || kRun == SH::RQ), "requests of a wavefront");
+  unsigned int voff[NREQ];
+#pragma unroll
+  for (int j = 0; j < NREQ; ++j) {
+    const int x = wave * NREQ + j, row = x % SH::RQ * SH::RPR + lane / (ROWB / 16);
+    const int chunk = lane % (ROWB / 16) ^ (x / SH::RQ & 1 ? SH::fv(row) : SH::fk(row));
+    voff[j] = chunk * 16 < rb ? (unsigned)(row * rb + chunk * 16) : kOutside;
+  }
   const unsigned int lds0 = (unsigned)(size_t)(lds_byte*)smem;
   // this lane's place in a K tile (row c, first half of a 32-byte step) and in a V tile
   const unsigned int kplace = c * ROWB + ((h2 ^ SH::fk(c)) << 4);
@@ -216,17 +200,27 @@ __global__ __launch_bounds__(64 * SH::NW, SH::WPE) void prefix_attn_kernel(Prefi
     asm volatile("" : "+v"(seg_lane));
     const int sc = seg_lane & 31, sh = seg_lane >> 5;
     // ---- which block of rows, which keys -------------------------------------------------------------------------------
-    int b = 0, kh, blk, it0, iters, slot;
-    if constexpr (OWN) {
-      // (sequences without nodes have no units: the last sequence that starts at or before u and has some)
-      b = 63 - __builtin_clzll(__builtin_amdgcn_ballot_w64(table[kIters][seg_lane] > 0 && table[kUnit0][seg_lane] <= u));
+    const bool own = u >= punits;
+    int b = 0, kh, blk, it0, iters, slot, n, L;
+    const unsigned char *kc, *vc, *kt, *vt;
+    if (own) {
+      const int rel = u - punits;
+      kh = uniform(rel / head_units);
+      const int in_head = rel - kh * head_units;
+      // (sequences without nodes have no units: the last sequence that starts at or before the unit and has some)
+      b = 63 - __builtin_clzll(__builtin_amdgcn_ballot_w64(table[kIters][seg_lane] > 0 && table[kUnit0][seg_lane] <= in_head));
       iters = of(kIters, b);
-      const int nb = of(kBlocks, b), rel = u - of(kUnit0, b);
-      const int item = uniform(rel / iters);
-      it0 = rel - item * iters;
-      kh = uniform(item / nb);
-      blk = item - kh * nb;
-      slot = w + of(kBlock0, b) + item;
+      const int in_seq = in_head - of(kUnit0, b);
+      blk = uniform(in_seq / iters);
+      it0 = in_seq - blk * iters;
+      slot = w + pitems + kh * head_blocks + of(kBlock0, b) + blk;
+      n = of(kNodes, b);
+      L = of(kCtx, b);
+      const long long off = (long long)((unsigned long long)(unsigned)of(kOffHigh, b) << 32 | (unsigned)of(kOff, b));
+      const size_t at = ((size_t)off + (size_t)kh * p.kv_cap * p.dh) * SH::ES;
+      const size_t ta = ((size_t)b * p.H_kv + kh) * p.max_nodes * rb;
+      kc = p.k_cache + at; vc = p.v_cache + at;
+      kt = p.k_tree + ta; vt = p.v_tree + ta;
     } else {
       iters = piters;
       const int item = uniform(u / iters);
@@ -234,25 +228,16 @@ __global__ __launch_bounds__(64 * SH::NW, SH::WPE) void prefix_attn_kernel(Prefi
       kh = uniform(item / pblocks);
       blk = item - kh * pblocks;
       slot = w + item;
+      n = all;
+      L = prefix;
+      kc = p.k_prefix + (size_t)kh * p.prefix_cap * rb;
+      vc = p.v_prefix + (size_t)kh * p.prefix_cap * rb;
+      kt = kc; vt = vc;
     }
     const int niter = uniform(iters - it0 < u1 - u ? iters - it0 : u1 - u);
     u += niter;
-
-    const int n = OWN ? of(kNodes, b) : all;  // nodes behind the rows
-    const int L = OWN ? of(kCtx, b) : prefix;
-    const unsigned char *kc, *vc, *kt = nullptr, *vt = nullptr;
-    if constexpr (OWN) {
-      const long long off = (long long)((unsigned long long)(unsigned)of(kOffHigh, b) << 32 | (unsigned)of(kOff, b));
-      const size_t at = ((size_t)off + (size_t)kh * p.kv_cap * p.dh) * SH::ES;
-      const size_t ta = ((size_t)b * p.H_kv + kh) * p.max_nodes * rb;
-      kc = p.k_cache + at; vc = p.v_cache + at;
-      kt = p.k_tree + ta; vt = p.v_tree + ta;
-    } else {
-      kc = p.k_prefix + (size_t)kh * p.prefix_cap * rb;
-      vc = p.v_prefix + (size_t)kh * p.prefix_cap * rb;
-    }
     kc = uniform(kc); vc = uniform(vc); kt = uniform(kt); vt = uniform(vt);
-    const int ctx_tiles = (L + 31) / 32;
+    const int ctx_tiles = own ? (L + 31) / 32 : 0x7fffffff;  // the tiles from here on are tree nodes
 
     // ---- the tiles of iteration i of this segment into their stage -----------------------------------------------------------
     // (The bases are parameters: captured, the choice between them becomes one between their addresses, in scratch memory.  The
@@ -260,30 +245,28 @@ __global__ __launch_bounds__(64 * SH::NW, SH::WPE) void prefix_attn_kernel(Prefi
     // it has no register for a result, and the loop below waits for it.)
     auto request = [&](int i, const unsigned char* kc, const unsigned char* vc, const unsigned char* kt, const unsigned char* vt)
         __attribute__((always_inline)) {
-      const int first = (it0 + i) * TPI;
-      const unsigned int stage = lds0 + i % SH::NS * SH::STAGE;
+      const unsigned int stage = lds0 + i % SH::NS * SH::STAGE + wave * NREQ * 1024;
 #pragma unroll
-      for (int j = 0; j < NREQ; ++j) {
-        const int x = wave * NREQ + j, k = first + x / (2 * SH::RQ), part0 = x % SH::RQ * SH::RPR;
-        const bool is_v = x / SH::RQ & 1;
-        const bool tree = OWN && k >= ctx_tiles;
-        const int row0 = (tree ? k - ctx_tiles : k) * 32 + part0;
+      for (int q = 0; q < kOperands; ++q) {
+        const int operand = wave * NREQ / SH::RQ + q, k = (it0 + i) * TPI + operand / 2;
+        const bool tree = k >= ctx_tiles;
+        const int row0 = (tree ? k - ctx_tiles : k) * 32;
         int left = (tree ? n : L) - row0;  // rows behind the last key, and all behind the last iteration: zeros, nothing is read
-        left = left < 0 || i >= niter ? 0 : (left > SH::RPR ? SH::RPR : left);
-        const unsigned char* base = is_v ? (tree ? vt : vc) : (tree ? kt : kc);
+        left = left < 0 || i >= niter ? 0 : (left > 32 ? 32 : left);
+        const unsigned char* base = operand & 1 ? (tree ? vt : vc) : (tree ? kt : kc);
         const int from = left > 0 ? row0 : 0;
         const unsigned long long at = (unsigned long long)base + (size_t)from * rb;
         const u32x4 rsrc = {(unsigned)uniform((int)at), (unsigned)uniform((int)(at >> 32)) & 0xffffu, (unsigned)uniform(left * rb), 0x00020000u};
-        const int chunk = (is_v ? vchunk ^ SH::fv(part0) : kchunk ^ SH::fk(part0)) * 16;
-        const unsigned int off = chunk < rb ? (unsigned)(lrow * rb + chunk) : kOutside;
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(stage + x * 1024), "v"(off), "s"(rsrc)
-                     : "memory", "m0");
+#pragma unroll
+        for (int j = q * kRun; j < (q + 1) * kRun; ++j)
+          asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(stage + j * 1024), "v"(voff[j]), "s"(rsrc)
+                       : "memory", "m0");
       }
     };
     constexpr int kEarly = SH::NS > 2 ? 2 : 1;  // stages in front of the rows, which everything waits for together
 #pragma unroll
     for (int i = 0; i < kEarly; ++i) request(i, kc, vc, kt, vt);
-    if (OWN && threadIdx.x == 0) table[kOdd][0] = 0;
+    if (threadIdx.x == 0) table[kOdd][0] = 0;
 
     // ---- this lane's query rows ------------------------------------------------------------------------------------------
     const int row_first = blk * R + rg * 32 * QT;
@@ -296,21 +279,23 @@ __global__ __launch_bounds__(64 * SH::NW, SH::WPE) void prefix_attn_kernel(Prefi
       const bool live = r < n * p.group;
       int node = r / p.group, bq = b;
       const int hg = r - node * p.group;
-      if constexpr (!OWN) {
+      if (!own) {
         // (sequences without nodes begin where the next one does: the last of those that begin here has the node)
         bq = 0;
         for (int i = 1; i < p.B; ++i) bq += node >= table[kFirst][i] ? 1 : 0;
         node -= table[kFirst][bq];
       }
+      // (rows that are none read some row's query: nobody reads what comes of it)
+      if (!live) { node = 0; bq = 0; }
       const unsigned char* qrow = p.q + (((size_t)bq * p.H + kh * p.group + hg) * p.max_nodes + node) * rb;
 #pragma unroll
       for (int i = 0; i < QU; ++i) {
         const int at = (2 * i + sh) * 16;
-        qf[qt][i] = u32x4{0u, 0u, 0u, 0u};
-        if (live && at < rb) qf[qt][i] = *(const u32x4*)(qrow + at);
+        qf[qt][i] = *(const u32x4*)(qrow + (at < rb ? at : 0));
+        if (rb < ROWB) qf[qt][i] = at < rb ? qf[qt][i] : u32x4{0u, 0u, 0u, 0u};
       }
       mw0[qt] = mw1[qt] = 0ull;
-      if (OWN && live) {
+      if (own && live) {
         const int W = (p.max_nodes + 63) >> 6;
         const unsigned long long* m = p.anc_mask + ((size_t)b * p.max_nodes + node) * W;
         mw0[qt] = m[0];
@@ -369,7 +354,7 @@ __global__ __launch_bounds__(64 * SH::NW, SH::WPE) void prefix_attn_kernel(Prefi
     // scores of keys that are not there or not seen
     auto hide = [&](int k, bool any, f32x16 (&s)[QT], const unsigned long long (&mw0)[QT], const unsigned long long (&mw1)[QT])
         __attribute__((always_inline)) {
-      const bool tree = OWN && k >= ctx_tiles;
+      const bool tree = k >= ctx_tiles;
       const int row0 = (tree ? k - ctx_tiles : k) * 32;
       const int left = any ? (tree ? n : L) - row0 : 0;
       if (tree || left < 32) {
@@ -407,7 +392,7 @@ __global__ __launch_bounds__(64 * SH::NW, SH::WPE) void prefix_attn_kernel(Prefi
     // segment), whose scores go to sn; read_next() requests the first fragments of the tile behind it.
     auto step = [&](int k, unsigned int tile, int k1, bool any1, unsigned int next, f32x16 (&s)[QT], f32x16 (&sn)[QT], auto&& read_next,
                     const unsigned long long (&mw0)[QT], const unsigned long long (&mw1)[QT]) __attribute__((always_inline)) {
-      const bool tree = OWN && k >= ctx_tiles;
+      const bool tree = k >= ctx_tiles;
       const unsigned int ka = next + kplace, va = tile + TILE + vplace;
       float ms[QT], sum[QT], mx[QT];
 #pragma unroll
@@ -598,9 +583,9 @@ __global__ __launch_bounds__(64 * SH::NW, SH::WPE) void prefix_attn_kernel(Prefi
       }
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    if (OWN && __builtin_amdgcn_ballot_w64(odd) != 0ull) table[kOdd][0] = 1;
+    if (__builtin_amdgcn_ballot_w64(odd) != 0ull) table[kOdd][0] = 1;
     __syncthreads();  // every request has landed, every tile is consumed: the LDS is free
-    if (OWN && threadIdx.x == 0) p.odd[slot] = table[kOdd][0];
+    if (threadIdx.x == 0) p.odd[slot] = table[kOdd][0];
 
     // ---- the key parts of a row group joined ------------------------------------------------------------------------------
     if constexpr (SH::KP > 1) {
@@ -666,72 +651,81 @@ __global__ __launch_bounds__(64 * SH::NW, SH::WPE) void prefix_attn_kernel(Prefi
 // ---- the join ------------------------------------------------------------------------------------------------------------
 struct PrefixJoinParams {
   PrefixAttnParams a;
-  const float *prefix_o, *prefix_ml, *own_o, *own_ml;
-  const int* own_odd;
   int out_bf16;
   void* out;   // [B][H][max_nodes][dh]
   float* lse;  // [B][H][max_nodes] or null
 };
 
 // One workgroup of DHP / 32 wavefronts per (32 rows of a sequence, key head): every wavefront weighs the rows' partial results
-// and adds up 32 components of them, in ascending order of the slots.
-template <typename SP, typename SO>
-__global__ __launch_bounds__(2 * SP::DHP) void prefix_join_kernel(PrefixJoinParams p) {
-  constexpr int DT = SP::DT, RP = SP::R, RO = SO::R;
+// and adds up 32 components of them - the prefix's, then the sequence's own, each in the order of its keys, four at a time
+// under way.
+template <typename SH>
+__global__ __launch_bounds__(2 * SH::DHP) void prefix_join_kernel(PrefixJoinParams p) {
+  constexpr int DT = SH::DT, R = SH::R;
   const int lane = threadIdx.x & 63, dt = threadIdx.x >> 6, c = lane & 31, h2 = lane >> 5;
   const int kh = blockIdx.y, b = blockIdx.z, r = blockIdx.x * 32 + c;
-  const Batch t = read_batch(p.a);
-  const auto pb = Blocks<false, RP, SP::TPI>::make(p.a, t);
-  const auto ob = Blocks<true, RO, SO::TPI>::make(p.a, t);
+  const Work t = read_work<R, SH::TPI>(p.a);
   const int n = __builtin_amdgcn_readlane(t.n, b);
   if ((int)blockIdx.x * 32 >= n * p.a.group) return;
   const bool live = r < n * p.a.group;
-  const Deal pd = prefix_deal(pb.units, SP::GROUPS), od = prefix_deal(ob.units, SO::GROUPS);
-  // this row's place among all rows of the key head and in its sequence; the slots of its blocks
-  const int rr = live ? r : 0;
+  const Deal d = prefix_deal(t.units, SH::GROUPS);
+  const int rr = live ? r : 0;  // this row's place in its sequence, and among all rows
   const int rp = __builtin_amdgcn_readlane(t.first, b) * p.a.group + rr;
-  int w0 = 0, w1 = -1, item = 0;
-  if (pb.iters > 0) {
-    item = kh * pb.blocks + rp / RP;
-    w0 = pd.owner(item * pb.iters);
-    w1 = pd.owner(item * pb.iters + pb.iters - 1);
-  }
-  const int oi = __builtin_amdgcn_readlane(ob.iters, b), onb = __builtin_amdgcn_readlane(ob.blocks, b);
-  const int oitem = kh * onb + rr / RO;
-  const int ou = __builtin_amdgcn_readlane(ob.unit0, b) + oitem * oi;
-  const int x0 = od.owner(ou), x1 = od.owner(ou + oi - 1), oslot = __builtin_amdgcn_readlane(ob.block0, b) + oitem;
-  const float* pml = p.prefix_ml + (size_t)item * 2 * RP + rp % RP;
-  const float* oml = p.own_ml + (size_t)oslot * 2 * RO + rr % RO;
-  float m = -INFINITY;
-  for (int w = w0; w <= w1; ++w) m = fmaxf(m, pml[(size_t)w * 2 * RP]);
-  for (int w = x0; w <= x1; ++w) m = fmaxf(m, oml[(size_t)w * 2 * RO]);
-  const float base = m > -INFINITY ? m : 0.f;
-  const float* po = p.prefix_o + ((size_t)item * (RP / 32) + rp % RP / 32) * (DT * 1024) + dt * 1024 + (h2 * 32 + rp % 32) * 4;
-  const float* oo = p.own_o + ((size_t)oslot * (RO / 32) + rr % RO / 32) * (DT * 1024) + dt * 1024 + (h2 * 32 + rr % 32) * 4;
-  float l = 0.f;
+  float m = -INFINITY, l = 0.f;
   f32x4 o[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (int w = w0; w <= w1; ++w) {
-    const float a = __builtin_amdgcn_exp2f(pml[(size_t)w * 2 * RP] - base);
-    l += a * pml[(size_t)w * 2 * RP + RP];
+  // partial results w0 + item .. w1 + item of the block of rows that holds `row`
+  auto gather = [&](int item, int w0, int w1, int row) __attribute__((always_inline)) {
+    const float* ml = p.a.pml + (size_t)item * 2 * R + row % R;
+    const float* po = p.a.po + ((size_t)item * (R / 32) + row % R / 32) * (DT * 1024) + dt * 1024 + (h2 * 32 + row % 32) * 4;
+    constexpr int kBatch = 4;
+    for (int w = w0; w <= w1; w += kBatch) {
+      float pm[kBatch], pl[kBatch];
+      f32x4 x[kBatch][4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) o[i] += a * *(const f32x4*)(po + (size_t)w * (RP / 32) * (DT * 1024) + i * 256);
-  }
-  for (int w = x0; w <= x1; ++w) {
-    const float a = __builtin_amdgcn_exp2f(oml[(size_t)w * 2 * RO] - base);
-    l += a * oml[(size_t)w * 2 * RO + RO];
+      for (int q = 0; q < kBatch; ++q) {  // (behind the last one: the last one again, with no weight)
+        const size_t s = w + q < w1 ? w + q : w1;
+        pm[q] = ml[s * 2 * R];
+        pl[q] = ml[s * 2 * R + R];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) o[i] += a * *(const f32x4*)(oo + (size_t)w * (RO / 32) * (DT * 1024) + i * 256);
+        for (int i = 0; i < 4; ++i) x[q][i] = *(const f32x4*)(po + s * (R / 32) * (DT * 1024) + i * 256);
+      }
+      float top = m;
+#pragma unroll
+      for (int q = 0; q < kBatch; ++q) top = fmaxf(top, pm[q]);
+      const float base = top > -INFINITY ? top : 0.f, old = __builtin_amdgcn_exp2f(m - base);
+      l *= old;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[i] *= old;
+#pragma unroll
+      for (int q = 0; q < kBatch; ++q) {
+        if (w + q > w1) continue;
+        const float a = __builtin_amdgcn_exp2f(pm[q] - base);
+        l += a * pl[q];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] += a * x[q][i];
+      }
+      m = top;
+    }
+  };
+  if (t.piters > 0) {
+    const int item = kh * t.pblocks + rp / R;
+    gather(item, d.owner(item * t.piters), d.owner(item * t.piters + t.piters - 1), rp);
   }
+  const int oi = __builtin_amdgcn_readlane(t.iters, b), blk = rr / R;
+  const int ou = t.punits + kh * t.head_units + __builtin_amdgcn_readlane(t.unit0, b) + blk * oi;
+  const int oitem = t.pitems + kh * t.head_blocks + __builtin_amdgcn_readlane(t.block0, b) + blk;
+  const int x0 = d.owner(ou), x1 = d.owner(ou + oi - 1);
+  gather(oitem, x0, x1, rr);
   if (!live) return;
   const int node = r / p.a.group, hg = r - node * p.a.group;
   int odd = 0;
-  for (int w = x0; w <= x1; ++w) odd |= p.own_odd[w + oslot];
+  for (int w = x0; w <= x1; ++w) odd |= p.a.odd[w + oitem];
   if (odd) {  // values of tree nodes that are infinite or not a number, left out so far: into the rows that see them
     const int W = (p.a.max_nodes + 63) >> 6;
     const unsigned long long* mask = p.a.anc_mask + ((size_t)b * p.a.max_nodes + node) * W;
-    const unsigned char* vt = p.a.v_tree + ((size_t)b * p.a.H_kv + kh) * p.a.max_nodes * p.a.dh * SP::ES;
+    const unsigned char* vt = p.a.v_tree + ((size_t)b * p.a.H_kv + kh) * p.a.max_nodes * p.a.dh * SH::ES;
     for (int j = 0; j < n; ++j) {
       if (!((mask[j >> 6] >> (j & 63)) & 1ull)) continue;
 #pragma unroll
@@ -741,7 +735,7 @@ __global__ __launch_bounds__(2 * SP::DHP) void prefix_join_kernel(PrefixJoinPara
           const int at = 32 * dt + 8 * i + 4 * h2 + e;
           if (at >= p.a.dh) continue;
           float v;
-          if constexpr (SP::F32) v = ((const float*)vt)[(size_t)j * p.a.dh + at];
+          if constexpr (SH::F32) v = ((const float*)vt)[(size_t)j * p.a.dh + at];
           else v = bf16_bits_to_float(((const unsigned short*)vt)[(size_t)j * p.a.dh + at]);
           if ((__float_as_uint(v) & 0x7f800000u) == 0x7f800000u) o[i][e] += v;
         }
@@ -806,9 +800,7 @@ hipError_t prepare_prefix_attn() {
           if (e != hipSuccess || (f32 && rows != 32 && rows != 128)) continue;
           e = with_shape(f32, dhp, fine, rows, [](auto shape) {
             using SH = decltype(shape);
-            const hipError_t e1 = hipFuncSetAttribute((const void*)prefix_attn_kernel<SH, false>, hipFuncAttributeMaxDynamicSharedMemorySize, SH::LDS);
-            if constexpr (SH::R > kPrefixOwnRows) return e1;
-            else return e1 != hipSuccess ? e1 : hipFuncSetAttribute((const void*)prefix_attn_kernel<SH, true>, hipFuncAttributeMaxDynamicSharedMemorySize, SH::LDS);
+            return hipFuncSetAttribute((const void*)prefix_attn_kernel<SH>, hipFuncAttributeMaxDynamicSharedMemorySize, SH::LDS);
           });
         }
   return e;
@@ -820,8 +812,13 @@ using namespace ctcspec;
 
 extern "C" size_t prefix_verify_attn_workspace_bytes(int B, int H, int H_kv, int dh, int max_nodes) {
   if (B < 1 || H < 1 || H_kv < 1 || H % H_kv || dh < 1 || max_nodes < 1) return 0;
-  const size_t a = prefix_workspace(B, H, H_kv, dh, max_nodes, false).total, f = prefix_workspace(B, H, H_kv, dh, max_nodes, true).total;
-  return a > f ? a : f;
+  size_t most = 0;  // (the rows of a workgroup may depend on the prefix's length: the largest of the choices)
+  for (int cap : {0, kPrefixLong})
+    for (bool f32 : {false, true}) {
+      const size_t bytes = prefix_workspace(B, H, H_kv, dh, max_nodes, cap, f32).total;
+      most = bytes > most ? bytes : most;
+    }
+  return most;
 }
 
 extern "C" int prefix_verify_attn(ctcspec_ctx* ctx, ctcspec_dtype dt, const void* q, const void* k_prefix, const void* v_prefix,
@@ -831,8 +828,8 @@ extern "C" int prefix_verify_attn(ctcspec_ctx* ctx, ctcspec_dtype dt, const void
                                   float scale, void* workspace, size_t workspace_bytes, ctcspec_dtype out_dt, void* out, float* lse) {
   if (!ctx) return CTCSPEC_EINVAL;
   if (const int owed = flush_deferred(ctx)) return owed;
-  CTCSPEC_REQUIRE(ctx, q && k_prefix && v_prefix && prefix_len && k_cache && v_cache && kv_off && ctx_len && k_tree && v_tree &&
-                           n_nodes && anc_mask && workspace && out,
+  CTCSPEC_REQUIRE(ctx, q && prefix_len && kv_off && ctx_len && k_tree && v_tree && n_nodes && anc_mask && workspace && out &&
+                           ((k_prefix && v_prefix) || prefix_cap == 0) && ((k_cache && v_cache) || kv_cap == 0),
                   CTCSPEC_EINVAL, "prefix_verify_attn: null pointer");
   CTCSPEC_REQUIRE(ctx, B > 0 && H > 0 && H_kv > 0 && dh > 0 && max_nodes > 0 && prefix_cap >= 0 && kv_cap >= 0, CTCSPEC_EINVAL,
                   "prefix_verify_attn: sizes must be positive");
@@ -846,13 +843,12 @@ extern "C" int prefix_verify_attn(ctcspec_ctx* ctx, ctcspec_dtype dt, const void
   CTCSPEC_REQUIRE(ctx, B <= ctx->lim.max_batch && B <= 64 && max_nodes <= ctx->lim.max_nodes && H <= ctx->lim.max_heads &&
                            dh <= ctx->lim.max_head_dim && H_kv <= 65535,
                   CTCSPEC_EUNSUPPORTED, "prefix_verify_attn: shape exceeds the context's limits");
-  CTCSPEC_REQUIRE(ctx, prefix_units_fit(1, H_kv, (long long)B * max_nodes * (H / H_kv), prefix_cap, 0) &&
-                           prefix_units_fit(B, H_kv, (long long)max_nodes * (H / H_kv), kv_cap, max_nodes),
+  CTCSPEC_REQUIRE(ctx, prefix_units_fit(B, H_kv, (long long)max_nodes * (H / H_kv), prefix_cap, kv_cap, max_nodes),
                   CTCSPEC_EUNSUPPORTED, "prefix_verify_attn: capacities of this size need more than 32 bits for the work's units");
   for (const void* a : {q, k_prefix, v_prefix, k_cache, v_cache, k_tree, v_tree, (const void*)workspace, (const void*)out})
     CTCSPEC_REQUIRE(ctx, aligned16(a), CTCSPEC_EINVAL, "prefix_verify_attn: pointers must be 16-byte aligned");
   const bool f32 = dt == CTCSPEC_F32, fine = out_dt == CTCSPEC_F32;
-  const PrefixWorkspace ws = prefix_workspace(B, H, H_kv, dh, max_nodes, f32);
+  const PrefixWorkspace ws = prefix_workspace(B, H, H_kv, dh, max_nodes, prefix_cap, f32);
   CTCSPEC_REQUIRE(ctx, workspace_bytes >= ws.total, CTCSPEC_EINVAL, "prefix_verify_attn: workspace of %zu bytes needed, %zu given",
                   ws.total, workspace_bytes);
 
@@ -866,31 +862,16 @@ extern "C" int prefix_verify_attn(ctcspec_ctx* ctx, ctcspec_dtype dt, const void
   p.anc_mask = (const unsigned long long*)anc_mask;
   p.prefix_cap = prefix_cap; p.kv_cap = kv_cap; p.B = B; p.H = H; p.H_kv = H_kv; p.group = H / H_kv; p.dh = dh; p.max_nodes = max_nodes;
   p.sl2 = scale * 1.4426950408889634f;
-  j.prefix_o = (float*)(base + ws.prefix_o); j.prefix_ml = (float*)(base + ws.prefix_ml);
-  j.own_odd = p.odd = (int*)(base + ws.own_odd); j.own_o = (float*)(base + ws.own_o); j.own_ml = (float*)(base + ws.own_ml);
+  p.po = (float*)(base + ws.o); p.pml = (float*)(base + ws.ml); p.odd = (int*)(base + ws.odd);
   j.out_bf16 = out_dt == CTCSPEC_BF16; j.out = out; j.lse = lse;
-  const int dhp = prefix_padded_dim(dh);
   hipStream_t st = ctx->stream;
-  const hipError_t e = with_shape(f32, dhp, fine, ws.prefix_rows, [&](auto prefix_shape) {
-    using SP = decltype(prefix_shape);
-    p.po = (float*)(base + ws.prefix_o);
-    p.pml = (float*)(base + ws.prefix_ml);
-    hipLaunchKernelGGL((prefix_attn_kernel<SP, false>), dim3(SP::GROUPS), dim3(64 * SP::NW), SP::LDS, st, p);
+  const hipError_t e = with_shape(f32, prefix_padded_dim(dh), fine, ws.rows, [&](auto shape) {
+    using SH = decltype(shape);
+    hipLaunchKernelGGL(prefix_attn_kernel<SH>, dim3(SH::GROUPS), dim3(64 * SH::NW), SH::LDS, st, p);
     if (const hipError_t e1 = hipGetLastError(); e1 != hipSuccess) return e1;
-    return with_rows<SP::F32, SP::DHP, SP::FINE>(ws.own_rows, [&](auto own_shape) {
-      using SO = decltype(own_shape);
-      if constexpr (SO::R > SP::R || SO::R > kPrefixOwnRows) {
-        return hipErrorInvalidValue;  // (one sequence's rows are among all rows)
-      } else {
-        p.po = (float*)(base + ws.own_o);
-        p.pml = (float*)(base + ws.own_ml);
-        hipLaunchKernelGGL((prefix_attn_kernel<SO, true>), dim3(SO::GROUPS), dim3(64 * SO::NW), SO::LDS, st, p);
-        if (const hipError_t e1 = hipGetLastError(); e1 != hipSuccess) return e1;
-        hipLaunchKernelGGL((prefix_join_kernel<SP, SO>),
-                           dim3((unsigned)((max_nodes * p.group + 31) / 32), (unsigned)H_kv, (unsigned)B), dim3(2 * SP::DHP), 0, st, j);
-        return hipGetLastError();
-      }
-    });
+    hipLaunchKernelGGL(prefix_join_kernel<SH>, dim3((unsigned)((max_nodes * p.group + 31) / 32), (unsigned)H_kv, (unsigned)B),
+                       dim3(2 * SH::DHP), 0, st, j);
+    return hipGetLastError();
   });
   CTCSPEC_HIP(ctx, e);
   return CTCSPEC_OK;

@@ -1,4 +1,4 @@
-// prefix_verify_attn: rows of a workgroup in its two passes, how the work is dealt to the workgroups, and the workspace that
+// prefix_verify_attn: rows of a workgroup, how the work is dealt to the workgroups, and the workspace that
 // takes.  Code without HIP, so that a test can ask it which shapes a call takes and where its partial results go.
 #pragma once
 
@@ -12,17 +12,19 @@
 
 namespace ctcspec {
 
-constexpr int kPrefixMaxGroups = 512;  // workgroups of a pass: one or two for each compute unit, each with an equal share of the work
+constexpr int kPrefixMaxGroups = 512;  // workgroups: one or two for each compute unit, each with an equal share of the work
 
-// Query rows of a workgroup, by the rows that may share keys (of all sequences for the prefix, of one for its own keys): as many
-// as there are, up to what the registers hold - every key is then fetched once for all of them.
-inline int prefix_block_rows(long long rows, bool f32) {
+// Query rows of a workgroup, by the rows that share the prefix's keys (without one: the rows of a sequence): as many as there
+// are, up to what the registers hold, so that every key is fetched once for all of them.  256 rows halve what is fetched
+// against 128, and double the partial results (a block's keys are split among the workgroups): they are for long prefixes.
+constexpr int kPrefixLong = 8192;
+inline int prefix_block_rows(long long rows, int prefix_cap, bool f32) {
   if (rows <= 32) return 32;
   if (f32) return 128;
-  return rows <= 64 ? 64 : (rows <= 128 ? 128 : 256);
+  return rows <= 64 ? 64 : (rows <= 128 || prefix_cap < kPrefixLong ? 128 : 256);
 }
 
-// A pass has units of work in a row - iterations over the keys, for block of rows after block of rows -, and workgroup w has
+// The work is units in a row - iterations over the keys, for block of rows after block of rows -, and workgroup w has
 // those from begin(w) to begin(w + 1).  Where its share crosses into another block, it leaves a partial result for each; that
 // of block i is number w + i.  From one partial result to the next in order w or i grows, or both: no two share a number.
 struct Deal {
@@ -45,36 +47,31 @@ CTCSPEC_BOTH Deal prefix_deal(int units, int groups) {
   d.more = units - d.each * d.groups;
   return d;
 }
-// units of a pass are counted in 32 bits: whether that is enough for the largest lengths
-inline bool prefix_units_fit(long long sequences, int H_kv, long long rows, int cap, int max_nodes) {
-  return sequences * H_kv * ((rows + 31) / 32) * ((cap + 31LL) / 32 + max_nodes / 32 + 1) < (1LL << 31);
+// units are counted in 32 bits: whether that is enough for the largest lengths
+inline bool prefix_units_fit(long long B, int H_kv, long long seq_rows, int prefix_cap, int kv_cap, int max_nodes) {
+  const double own = (double)B * ((seq_rows + 31) / 32) * ((kv_cap + 31LL) / 32 + max_nodes / 32 + 1);
+  const double prefix = (double)((B * seq_rows + 31) / 32) * ((prefix_cap + 31LL) / 32);
+  return (own + prefix) * H_kv < 2147483647.0;
 }
-
-// (256 rows of a sequence's own do not fit the registers with their masks)
-constexpr int kPrefixOwnRows = 128;
 
 inline int prefix_padded_dim(int dh) { return dh <= 64 ? 64 : 128; }
 
 struct PrefixWorkspace {
-  int prefix_rows, own_rows;       // rows of a workgroup
-  size_t prefix_o, prefix_ml, own_o, own_ml, own_odd, total;
+  int rows;  // of a workgroup
+  size_t o, ml, odd, total;
 };
 // Numbers of partial results: below workgroups + blocks.
-inline PrefixWorkspace prefix_workspace(int B, int H, int H_kv, int dh, int max_nodes, bool f32) {
+inline PrefixWorkspace prefix_workspace(int B, int H, int H_kv, int dh, int max_nodes, int prefix_cap, bool f32) {
   PrefixWorkspace w;
   size_t off = 0;
   auto carve = [&](size_t bytes) { size_t at = off; off = (off + bytes + 255) / 256 * 256; return at; };
   const long long seq_rows = (long long)max_nodes * (H / H_kv), all_rows = seq_rows * B;
-  w.prefix_rows = prefix_block_rows(all_rows, f32);
-  w.own_rows = prefix_block_rows(seq_rows < kPrefixOwnRows ? seq_rows : kPrefixOwnRows, f32);
-  const size_t prefix_slots = kPrefixMaxGroups + (size_t)H_kv * ((all_rows + w.prefix_rows - 1) / w.prefix_rows);
-  const size_t own_slots = kPrefixMaxGroups + (size_t)B * H_kv * ((seq_rows + w.own_rows - 1) / w.own_rows);
-  const size_t row = (size_t)prefix_padded_dim(dh) * sizeof(float);
-  w.prefix_o = carve(prefix_slots * w.prefix_rows * row);
-  w.prefix_ml = carve(prefix_slots * w.prefix_rows * 2 * sizeof(float));
-  w.own_o = carve(own_slots * w.own_rows * row);
-  w.own_ml = carve(own_slots * w.own_rows * 2 * sizeof(float));
-  w.own_odd = carve(own_slots * sizeof(int));
+  w.rows = prefix_block_rows(prefix_cap > 0 ? all_rows : seq_rows, prefix_cap, f32);
+  const size_t blocks = (size_t)H_kv * ((all_rows + w.rows - 1) / w.rows + B * ((seq_rows + w.rows - 1) / w.rows));
+  const size_t slots = kPrefixMaxGroups + blocks;
+  w.o = carve(slots * w.rows * prefix_padded_dim(dh) * sizeof(float));
+  w.ml = carve(slots * w.rows * 2 * sizeof(float));
+  w.odd = carve(slots * sizeof(int));
   w.total = off;
   return w;
 }
