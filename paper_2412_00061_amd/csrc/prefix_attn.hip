@@ -6,8 +6,8 @@
 // sequences (and of the heads that share a key head) stand side by side against each tile of the prefix's keys - read and
 // multiplied once for the batch -, every sequence's rows against its own keys, and a second kernel joins what they left.
 //
-// prefix_attn_kernel: the work is cut into units - one iteration over the keys (KP * KT tiles of 32) for one block of R rows -
-// and the units, in the order (prefix: key head, row block, keys), (own: key head, sequence, row block, keys), are dealt to the
+// prefix_attn_kernel: the work is cut into units - one iteration over the keys (KP * KT tiles of 32) for one block of R rows, and
+// some for the block itself - and the units, in the order (prefix: key head, row block, keys), (own: key head, sequence, row block, keys), are dealt to the
 // workgroups in equal consecutive shares: lengths, node counts and prefix length are read on the device, and no workgroup waits
 // for a longer one.  A workgroup whose share crosses from one block of rows into the next leaves a partial result for each, in a
 // place of its own (prefix_plan.h).
@@ -65,6 +65,10 @@ struct Work {
   int head_units, head_blocks;  // own units and blocks of a key head
   int punits, pitems, units;  // units and blocks of the prefix over all key heads; all units
 };
+// units of a block of rows
+__device__ __forceinline__ int own_units(int iters) { return kPrefixBlockUnits + iters * kPrefixOwnWeight; }
+template <int R>
+__device__ __forceinline__ int prefix_units(int iters) { return kPrefixBlockUnits + iters * prefix_shared_weight(R); }
 template <int R, int TPI>
 __device__ __forceinline__ Work read_work(const PrefixAttnParams& p) {
   const int lane = threadIdx.x & 63;
@@ -78,14 +82,15 @@ __device__ __forceinline__ Work read_work(const PrefixAttnParams& p) {
   }
   t.blocks = (t.n * p.group + R - 1) / R;
   t.iters = t.n ? ((t.ctx + 31) / 32 + (t.n + 31) / 32 + TPI - 1) / TPI : 0;
-  int n = t.n, b = t.blocks, u = t.blocks * t.iters;
+  const int mine = t.blocks * own_units(t.iters);
+  int n = t.n, b = t.blocks, u = mine;
   for (int d = 1; d < p.B; d *= 2) {
     const int nb = __shfl_up(n, d, 64), bb = __shfl_up(b, d, 64), ub = __shfl_up(u, d, 64);
     if (lane >= d) { n += nb; b += bb; u += ub; }
   }
   t.first = n - t.n;
   t.block0 = b - t.blocks;
-  t.unit0 = u - t.blocks * t.iters;
+  t.unit0 = u - mine;
   t.all = __builtin_amdgcn_readlane(n, p.B - 1);
   t.head_blocks = __builtin_amdgcn_readlane(b, p.B - 1);
   t.head_units = __builtin_amdgcn_readlane(u, p.B - 1);
@@ -93,7 +98,7 @@ __device__ __forceinline__ Work read_work(const PrefixAttnParams& p) {
   t.piters = ((t.prefix + 31) / 32 + TPI - 1) / TPI;
   t.pblocks = uniform((t.all * p.group + R - 1) / R);
   t.pitems = t.piters ? p.H_kv * t.pblocks : 0;
-  t.punits = t.pitems * t.piters;
+  t.punits = t.pitems * prefix_units<R>(t.piters);
   t.units = t.punits + p.H_kv * t.head_units;
   return t;
 }
@@ -201,7 +206,7 @@ __global__ __launch_bounds__(64 * SH::NW, SH::WPE) void prefix_attn_kernel(Prefi
     const int sc = seg_lane & 31, sh = seg_lane >> 5;
     // ---- which block of rows, which keys -------------------------------------------------------------------------------
     const bool own = u >= punits;
-    int b = 0, kh, blk, it0, iters, slot, n, L;
+    int b = 0, kh, blk, at_unit, units, weight, slot, n, L;  // at_unit: in the block's units, the first of which are no iterations
     const unsigned char *kc, *vc, *kt, *vt;
     if (own) {
       const int rel = u - punits;
@@ -209,10 +214,11 @@ __global__ __launch_bounds__(64 * SH::NW, SH::WPE) void prefix_attn_kernel(Prefi
       const int in_head = rel - kh * head_units;
       // (sequences without nodes have no units: the last sequence that starts at or before the unit and has some)
       b = 63 - __builtin_clzll(__builtin_amdgcn_ballot_w64(table[kIters][seg_lane] > 0 && table[kUnit0][seg_lane] <= in_head));
-      iters = of(kIters, b);
+      units = own_units(of(kIters, b));
+      weight = kPrefixOwnWeight;
       const int in_seq = in_head - of(kUnit0, b);
-      blk = uniform(in_seq / iters);
-      it0 = in_seq - blk * iters;
+      blk = uniform(in_seq / units);
+      at_unit = in_seq - blk * units;
       slot = w + pitems + kh * head_blocks + of(kBlock0, b) + blk;
       n = of(kNodes, b);
       L = of(kCtx, b);
@@ -222,9 +228,10 @@ __global__ __launch_bounds__(64 * SH::NW, SH::WPE) void prefix_attn_kernel(Prefi
       kc = p.k_cache + at; vc = p.v_cache + at;
       kt = p.k_tree + ta; vt = p.v_tree + ta;
     } else {
-      iters = piters;
-      const int item = uniform(u / iters);
-      it0 = u - item * iters;
+      units = prefix_units<R>(piters);
+      weight = prefix_shared_weight(R);
+      const int item = uniform(u / units);
+      at_unit = u - item * units;
       kh = uniform(item / pblocks);
       blk = item - kh * pblocks;
       slot = w + item;
@@ -234,8 +241,15 @@ __global__ __launch_bounds__(64 * SH::NW, SH::WPE) void prefix_attn_kernel(Prefi
       vc = p.v_prefix + (size_t)kh * p.prefix_cap * rb;
       kt = kc; vt = vc;
     }
-    const int niter = uniform(iters - it0 < u1 - u ? iters - it0 : u1 - u);
-    u += niter;
+    const int share = uniform(units - at_unit < u1 - u ? units - at_unit : u1 - u);
+    u += share;
+    // the iterations that begin in the share
+    auto iterations = [&](int units) __attribute__((always_inline)) {
+      const int x = units - kPrefixBlockUnits;
+      return uniform(x > 0 ? (x + weight - 1) / weight : 0);
+    };
+    const int it0 = iterations(at_unit), niter = iterations(at_unit + share) - it0;
+    if (niter <= 0) continue;
     kc = uniform(kc); vc = uniform(vc); kt = uniform(kt); vt = uniform(vt);
     const int ctx_tiles = own ? (L + 31) / 32 : 0x7fffffff;  // the tiles from here on are tree nodes
 
@@ -711,12 +725,14 @@ __global__ __launch_bounds__(2 * SH::DHP) void prefix_join_kernel(PrefixJoinPara
   };
   if (t.piters > 0) {
     const int item = kh * t.pblocks + rp / R;
-    gather(item, d.owner(item * t.piters), d.owner(item * t.piters + t.piters - 1), rp);
+    const int first = item * prefix_units<R>(t.piters) + kPrefixBlockUnits;
+    gather(item, d.owner(first), d.owner(first + (t.piters - 1) * prefix_shared_weight(R)), rp);
   }
   const int oi = __builtin_amdgcn_readlane(t.iters, b), blk = rr / R;
-  const int ou = t.punits + kh * t.head_units + __builtin_amdgcn_readlane(t.unit0, b) + blk * oi;
+  const int ou = t.punits + kh * t.head_units + __builtin_amdgcn_readlane(t.unit0, b) +
+                 blk * own_units(oi) + kPrefixBlockUnits;
   const int oitem = t.pitems + kh * t.head_blocks + __builtin_amdgcn_readlane(t.block0, b) + blk;
-  const int x0 = d.owner(ou), x1 = d.owner(ou + oi - 1);
+  const int x0 = d.owner(ou), x1 = d.owner(ou + (oi - 1) * kPrefixOwnWeight);
   gather(oitem, x0, x1, rr);
   if (!live) return;
   const int node = r / p.a.group, hg = r - node * p.a.group;
@@ -812,10 +828,10 @@ using namespace ctcspec;
 
 extern "C" size_t prefix_verify_attn_workspace_bytes(int B, int H, int H_kv, int dh, int max_nodes) {
   if (B < 1 || H < 1 || H_kv < 1 || H % H_kv || dh < 1 || max_nodes < 1) return 0;
-  size_t most = 0;  // (the rows of a workgroup may depend on the prefix's length: the largest of the choices)
-  for (int cap : {0, kPrefixLong})
+  size_t most = 0;
+  for (bool any_prefix : {false, true})
     for (bool f32 : {false, true}) {
-      const size_t bytes = prefix_workspace(B, H, H_kv, dh, max_nodes, cap, f32).total;
+      const size_t bytes = prefix_workspace(B, H, H_kv, dh, max_nodes, any_prefix, f32).total;
       most = bytes > most ? bytes : most;
     }
   return most;
@@ -848,7 +864,7 @@ extern "C" int prefix_verify_attn(ctcspec_ctx* ctx, ctcspec_dtype dt, const void
   for (const void* a : {q, k_prefix, v_prefix, k_cache, v_cache, k_tree, v_tree, (const void*)workspace, (const void*)out})
     CTCSPEC_REQUIRE(ctx, aligned16(a), CTCSPEC_EINVAL, "prefix_verify_attn: pointers must be 16-byte aligned");
   const bool f32 = dt == CTCSPEC_F32, fine = out_dt == CTCSPEC_F32;
-  const PrefixWorkspace ws = prefix_workspace(B, H, H_kv, dh, max_nodes, prefix_cap, f32);
+  const PrefixWorkspace ws = prefix_workspace(B, H, H_kv, dh, max_nodes, prefix_cap > 0, f32);
   CTCSPEC_REQUIRE(ctx, workspace_bytes >= ws.total, CTCSPEC_EINVAL, "prefix_verify_attn: workspace of %zu bytes needed, %zu given",
                   ws.total, workspace_bytes);
 

@@ -15,14 +15,20 @@ namespace ctcspec {
 constexpr int kPrefixMaxGroups = 512;  // workgroups: one or two for each compute unit, each with an equal share of the work
 
 // Query rows of a workgroup, by the rows that share the prefix's keys (without one: the rows of a sequence): as many as there
-// are, up to what the registers hold, so that every key is fetched once for all of them.  256 rows halve what is fetched
-// against 128, and double the partial results (a block's keys are split among the workgroups): they are for long prefixes.
-constexpr int kPrefixLong = 8192;
-inline int prefix_block_rows(long long rows, int prefix_cap, bool f32) {
+// are, up to what the registers hold, so that every key is fetched once for all of them.  (8 sequences x 64 nodes, 32 heads, us
+// with 128 / 256: behind 2048 keys 81 / 82, 8192 without history 135 / 98, 32768 445 / 352.)
+inline int prefix_block_rows(long long rows, bool f32) {
   if (rows <= 32) return 32;
   if (f32) return 128;
-  return rows <= 64 ? 64 : (rows <= 128 || prefix_cap < kPrefixLong ? 128 : 256);
+  return rows <= 64 ? 64 : (rows <= 128 ? 128 : 256);
 }
+
+// Units of work: what an iteration over the prefix and one over a sequence's own keys cost (64 keys against all R rows: products;
+// 64 keys against the sequence's rows: the keys' way in), and a block of rows besides its iterations (the rows' way in, the
+// first keys' way, what it leaves).  8 sequences x 64 nodes behind 2048 keys with 256 to 2048 of their own, us for 2 : 2 / 3 : 2 /
+// 4 : 2 with 256 rows 98 / 82 / 84; 256 short blocks of their own behind 32768 keys take 855 us if a block costs nothing, 312 with 8.
+CTCSPEC_BOTH constexpr int prefix_shared_weight(int rows) { return rows == 256 ? 3 : 2; }
+constexpr int kPrefixOwnWeight = 2, kPrefixBlockUnits = 8;
 
 // The work is units in a row - iterations over the keys, for block of rows after block of rows -, and workgroup w has
 // those from begin(w) to begin(w + 1).  Where its share crosses into another block, it leaves a partial result for each; that
@@ -36,8 +42,8 @@ struct Deal {
     return u < big ? u / (each + 1) : more + (u - big) / each;
   }
 };
-// A share is at least kPrefixMinUnits: what it leaves costs about as much as so many iterations.
-constexpr int kPrefixMinUnits = 2;
+// A share is at least kPrefixMinUnits.
+constexpr int kPrefixMinUnits = 6;
 CTCSPEC_BOTH Deal prefix_deal(int units, int groups) {
   Deal d;
   const int most = (int)(((unsigned)units + kPrefixMinUnits - 1) / kPrefixMinUnits);
@@ -49,8 +55,8 @@ CTCSPEC_BOTH Deal prefix_deal(int units, int groups) {
 }
 // units are counted in 32 bits: whether that is enough for the largest lengths
 inline bool prefix_units_fit(long long B, int H_kv, long long seq_rows, int prefix_cap, int kv_cap, int max_nodes) {
-  const double own = (double)B * ((seq_rows + 31) / 32) * ((kv_cap + 31LL) / 32 + max_nodes / 32 + 1);
-  const double prefix = (double)((B * seq_rows + 31) / 32) * ((prefix_cap + 31LL) / 32);
+  const double own = (double)B * ((seq_rows + 31) / 32) * (kPrefixOwnWeight * ((kv_cap + 31LL) / 32 + max_nodes / 32 + 1) + kPrefixBlockUnits);
+  const double prefix = (double)((B * seq_rows + 31) / 32) * (3 * ((prefix_cap + 31LL) / 32) + kPrefixBlockUnits);
   return (own + prefix) * H_kv < 2147483647.0;
 }
 
@@ -61,12 +67,12 @@ struct PrefixWorkspace {
   size_t o, ml, odd, total;
 };
 // Numbers of partial results: below workgroups + blocks.
-inline PrefixWorkspace prefix_workspace(int B, int H, int H_kv, int dh, int max_nodes, int prefix_cap, bool f32) {
+inline PrefixWorkspace prefix_workspace(int B, int H, int H_kv, int dh, int max_nodes, bool any_prefix, bool f32) {
   PrefixWorkspace w;
   size_t off = 0;
   auto carve = [&](size_t bytes) { size_t at = off; off = (off + bytes + 255) / 256 * 256; return at; };
   const long long seq_rows = (long long)max_nodes * (H / H_kv), all_rows = seq_rows * B;
-  w.rows = prefix_block_rows(prefix_cap > 0 ? all_rows : seq_rows, prefix_cap, f32);
+  w.rows = prefix_block_rows(any_prefix ? all_rows : seq_rows, f32);
   const size_t blocks = (size_t)H_kv * ((all_rows + w.rows - 1) / w.rows + B * ((seq_rows + w.rows - 1) / w.rows));
   const size_t slots = kPrefixMaxGroups + blocks;
   w.o = carve(slots * w.rows * prefix_padded_dim(dh) * sizeof(float));
