@@ -540,7 +540,8 @@ int kv_weight_update(ctcspec_ctx* ctx, ctcspec_dtype dt, const void* q, const fl
  * sink, recent  >= 0, together <= budget; either needs pos and pos_out, recent needs next_pos
  * kept          [B,H_kv,budget] int32 out
  * weight_out, pos_out, ctx_len_out   out, other buffers than the inputs
- * Limits: dh % 8 == 0, dh <= CTCSPEC_MAX_HEAD_DIM, B, H_kv, dh within the context's limits.  The same bits on every run.
+ * Limits: kv_cap <= 524288, dh % 8 == 0, dh <= CTCSPEC_MAX_HEAD_DIM, B, H_kv, dh within the context's limits.  The same bits
+ * on every run.
  */
 int kv_evict(ctcspec_ctx* ctx, ctcspec_dtype dt, void* k_cache, void* v_cache, const int64_t* kv_off,
              const int32_t* ctx_len, int kv_cap, const float* weight, const int32_t* pos, const int32_t* next_pos, int B,

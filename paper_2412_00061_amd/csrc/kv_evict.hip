@@ -28,26 +28,34 @@ struct KvEvictParams {
 };
 
 constexpr int kEvWaves = 16, kEvThreads = 64 * kEvWaves;
-constexpr int kEvBits = 11, kEvBins = 1 << kEvBits;  // three digits: the upper 11 bits, the next 11, the last 10
-constexpr int kEvList = 8192;                        // moved rows per round
+constexpr int kEvBins = 2048;      // of a digit of up to 11 bits
+constexpr int kEvIndexBits = 20;   // of a row
+constexpr int kEvMaxRows = 1 << 19;
+constexpr int kEvTies = 256;       // rows that are compared with each other
+constexpr int kEvList = 8192;      // moved rows per round
+// LDS: the bins, and from then on the list of the moved rows in their place; then for every 64 rows their bits and how many of
+// the kind that counts there lie before them
+constexpr int kEvListBytes = kEvList * 4;
+static_assert(kEvListBytes >= kEvBins * 4 + kEvTies * 8);
+constexpr size_t evict_lds_bytes(int kv_cap) { return kEvListBytes + (size_t)((kv_cap + 63) / 64) * 12; }
 
 // Order of the rows: larger weight first, then smaller index; rows that stay in any case before all others; a weight that is not
-// a number behind all others.
-__device__ __forceinline__ unsigned int evict_key(const KvEvictParams& p, const float* w, const int32_t* pos, int j, int fresh) {
-  const float v = w[j];
-  unsigned int key = v != v ? 0u : float_to_ordered(v);
-  if (pos) {
-    const int at = pos[j];
-    key = at < p.sink || at >= fresh ? 0xffffffffu : key;
-  }
-  return key;
+// a number behind all others.  (fresh: positions from there on stay.)
+__device__ __forceinline__ unsigned int evict_key(float weight, int pos, int sink, int fresh) {
+  const unsigned int key = weight != weight ? 0u : float_to_ordered(weight);
+  return pos < sink || pos >= fresh ? 0xffffffffu : key;
 }
 
+// The order as one number: the key, then the index from the top - no two rows have the same -, searched digit by digit for
+// the n-th largest until the rows that share the digits so far all stay or are few enough to be compared with each other.  Then a
+// bit for every row that stays, and everything else follows from counts of bits.
+// K: a lane holds up to K keys in registers (rows 64 k + lane of its wavefront's range): the passes read memory once.  0: for
+// capacities beyond that; every pass reads the weights again, eight rows of a lane at a time.
+template <int K>
 __global__ __launch_bounds__(kEvThreads) void kv_evict_select_kernel(KvEvictParams p) {
-  __shared__ unsigned int hist[kEvBins];
-  __shared__ int list[kEvList];
-  __shared__ int wsum[2][kEvWaves];
-  __shared__ int found[2];
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  __shared__ int wsum[kEvWaves];
+  __shared__ int found[3];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int kh = blockIdx.x, b = blockIdx.y;
   int L = __builtin_amdgcn_readfirstlane(p.ctx_len[b]);
@@ -61,28 +69,93 @@ __global__ __launch_bounds__(kEvThreads) void kv_evict_select_kernel(KvEvictPara
     for (int j = tid; j < n; j += kEvThreads) kept[j] = j;
     return;
   }
+  unsigned int* hist = (unsigned int*)smem;
+  unsigned long long* ties = (unsigned long long*)(smem + kEvBins * 4);
+  int* list = (int*)smem;
+  const int words = (L + 63) / 64;
+  unsigned long long* bits = (unsigned long long*)(smem + kEvListBytes);
+  int* count = (int*)(bits + words);
+
   const float* w = p.weight + head * p.kv_cap;
   const int32_t* pos = p.pos ? p.pos + head * p.kv_cap : nullptr;
-  const int fresh = p.recent > 0 ? p.next_pos[b] - p.recent : 0x7fffffff;
-  // every wavefront has a range of rows of its own, so that ranks follow from counts
-  const int range = (L + kEvThreads - 1) / kEvThreads * 64, j0 = wave * range, j1 = j0 + range < L ? j0 + range : L;
-
-  // ---- the n-th largest key, digit by digit: `above` keys are larger than all that begin with `prefix`, `want` of those stay --------
-  unsigned int prefix = 0u;
-  int want = n;
-  for (int d = 0; d < 3; ++d) {
-    const int shift = d == 0 ? 21 : (d == 1 ? 10 : 0), bits = d == 2 ? 10 : 11;
-    for (int i = tid; i < kEvBins; i += kEvThreads) hist[i] = 0u;
-    __syncthreads();
-    for (int j = j0 + lane; j < j1; j += 64) {
-      const unsigned int key = evict_key(p, w, pos, j, fresh);
-      if (d == 0 || (key >> (shift + bits)) == prefix) {
-        const unsigned int bin = (key >> shift) & ((1u << bits) - 1u);
-        atomicAdd(&hist[bin], 1u);
+  const int sink = pos ? p.sink : -0x7fffffff - 1, fresh = p.recent > 0 ? p.next_pos[b] - p.recent : 0x7fffffff;
+  const int range = (words + kEvWaves - 1) / kEvWaves * 64, j0 = wave * range;  // this wavefront's rows
+  const int rows = j0 < L ? (L - j0 < range ? L - j0 : range) : 0;
+  // keys of rows j0 + 64 (k0 + i) + lane, i < N; rows that are none get the smallest
+  auto load = [&]<int N>(int k0, unsigned int (&key)[N]) __attribute__((always_inline)) {
+    float v[N];
+    int at[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int j = j0 + 64 * (k0 + i) + lane;
+      v[i] = w[j < L ? j : L - 1];
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) at[i] = 0;
+    if (pos) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int j = j0 + 64 * (k0 + i) + lane;
+        at[i] = pos[j < L ? j : L - 1];
       }
     }
+#pragma unroll
+    for (int i = 0; i < N; ++i) key[i] = evict_key(v[i], at[i], sink, fresh);
+  };
+  unsigned int mine[K ? K : 1];
+  if constexpr (K > 0) {
+    constexpr int N = K < 16 ? K : 16;
+#pragma unroll
+    for (int k = 0; k < K; k += N) {
+      unsigned int some[N];
+      load(k, some);
+#pragma unroll
+      for (int i = 0; i < N; ++i) mine[k + i] = some[i];
+    }
+  }
+  // f(k, whether the row exists, its place in the order)
+  auto each = [&](auto&& f) __attribute__((always_inline)) {
+    auto order = [&](unsigned int key, int k) __attribute__((always_inline)) {
+      return (unsigned long long)key << kEvIndexBits | (unsigned)((1 << kEvIndexBits) - 1 - (j0 + 64 * k + lane));
+    };
+    if constexpr (K > 0) {
+#pragma unroll
+      for (int k = 0; k < K; ++k)
+        if (64 * k < rows) f(k, 64 * k + lane < rows, order(mine[k], k));
+    } else {
+      for (int k0 = 0; 64 * k0 < rows; k0 += 8) {
+        unsigned int some[8];
+        load(k0, some);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (64 * (k0 + i) < rows) f(k0 + i, 64 * (k0 + i) + lane < rows, order(some[i], k0 + i));
+      }
+    }
+  };
+
+  // ---- the search: `want` of the `same` rows whose place begins with `prefix` (the bits from `shift` on) stay, and all before them ----
+  unsigned long long prefix = 0ull;
+  int want = n, same = L, shift = 32 + kEvIndexBits;
+  while (same > want && same > kEvTies) {
+    const int bits_left = shift, digit = bits_left > 30 ? 11 : 10;
+    shift -= digit;
+    hist[tid] = hist[tid + kEvThreads] = 0u;
     __syncthreads();
-    // thread t: bins 2 t' and 2 t' + 1 from the top; how many keys lie in the bins above
+    each([&](int, bool there, unsigned long long at) __attribute__((always_inline)) {
+      const bool counts = there && (at >> (shift + digit)) == prefix;
+      const unsigned int bin = (unsigned)(at >> shift) & ((1u << digit) - 1u);
+      // (equal weights are common - rows that nobody looked at -, and 64 additions to one place follow one another)
+      const unsigned long long m = __builtin_amdgcn_ballot_w64(counts);
+      if (m == 0ull) return;
+      const unsigned int one = (unsigned)__builtin_amdgcn_readlane((int)bin, __builtin_ctzll(m));
+      if (__builtin_amdgcn_ballot_w64(counts && bin != one) == 0ull) {
+        if (lane == 0) atomicAdd(&hist[one], (unsigned)__builtin_popcountll(m));
+      } else if (counts) {
+        atomicAdd(&hist[bin], 1u);
+      }
+    });
+    __syncthreads();
+    // thread t: bins 2 t and 2 t + 1 from the top; how many rows lie in the bins above
     const int hi = kEvBins - 1 - 2 * tid;
     const int c1 = (int)hist[hi], c0 = (int)hist[hi - 1];
     int sum = c0 + c1;
@@ -91,76 +164,102 @@ __global__ __launch_bounds__(kEvThreads) void kv_evict_select_kernel(KvEvictPara
       const int other = __shfl_up(sum, o, 64);
       if (lane >= o) sum += other;
     }
-    if (lane == 63) wsum[0][wave] = sum;
+    if (lane == 63) wsum[wave] = sum;
     __syncthreads();
     int above = sum - c0 - c1;
-    for (int v = 0; v < wave; ++v) above += wsum[0][v];
-    if (above < want && want <= above + c1) { found[0] = hi; found[1] = above; }
-    else if (above + c1 < want && want <= above + c1 + c0) { found[0] = hi - 1; found[1] = above + c1; }
+    for (int v = 0; v < wave; ++v) above += wsum[v];
+    if (above < want && want <= above + c1) { found[0] = hi; found[1] = above; found[2] = c1; }
+    else if (above + c1 < want && want <= above + c1 + c0) { found[0] = hi - 1; found[1] = above + c1; found[2] = c0; }
     __syncthreads();
-    prefix = (prefix << bits) | (unsigned)found[0];
+    prefix = prefix << digit | (unsigned)found[0];
     want -= found[1];
+    same = found[2];
+  }
+  // ---- a bit for every row that stays -----------------------------------------------------------------------------------------------
+  const bool compare = same > want;
+  if (compare) {
+    __syncthreads();
+    if (tid == 0) found[0] = 0;
     __syncthreads();
   }
-  // keys > prefix stay, and the first `want` that equal it
-  auto count = [&](int x, int slot) __attribute__((always_inline)) {  // of the wavefronts before this one; x: this wavefront's
-    if (lane == 0) wsum[slot][wave] = x;
-    __syncthreads();
-    int before = 0;
-    for (int v = 0; v < wave; ++v) before += wsum[slot][v];
-    return before;
-  };
-  int equal = 0;
-  for (int j = j0; j < j1; j += 64) {
-    const bool eq = j + lane < j1 && evict_key(p, w, pos, j + lane, fresh) == prefix;
-    equal += __builtin_popcountll(__builtin_amdgcn_ballot_w64(eq));
-  }
-  const int equal0 = count(equal, 0);
-  const unsigned long long below = (1ull << lane) - 1ull;
-  // f(j, which of rows j .. j + 63 exist, which stay)
-  auto rows = [&](auto&& f) __attribute__((always_inline)) {
-    int eqs = equal0;
-    for (int j = j0; j < j1; j += 64) {
-      const bool there = j + lane < j1;
-      const unsigned int key = there ? evict_key(p, w, pos, j + lane, fresh) : 0u;
-      const bool eq = there && key == prefix;
-      const unsigned long long em = __builtin_amdgcn_ballot_w64(eq);
-      const bool stays = there && (key > prefix || (eq && eqs + __builtin_popcountll(em & below) < want));
-      eqs += __builtin_popcountll(em);
-      f(j, there, stays);
-    }
-  };
-  int holes = 0, moving = 0;
-  rows([&](int j, bool there, bool stays) __attribute__((always_inline)) {
-    holes += __builtin_popcountll(__builtin_amdgcn_ballot_w64(there && !stays && j + lane < n));
-    moving += __builtin_popcountll(__builtin_amdgcn_ballot_w64(stays && j + lane >= n));
+  each([&](int k, bool there, unsigned long long at) __attribute__((always_inline)) {
+    const unsigned long long top = at >> shift;
+    const unsigned long long m = __builtin_amdgcn_ballot_w64(there && (top > prefix || (top == prefix && !compare)));
+    if (lane == 0) bits[j0 / 64 + k] = m;
+    if (compare && there && top == prefix) ties[atomicAdd(&found[0], 1)] = at;
   });
-  const int hole0 = count(holes, 1);
   __syncthreads();
-  const int move0 = count(moving, 0);
+  if (compare) {
+    if (tid < same) {
+      const unsigned long long at = ties[tid];
+      int rank = 0;
+      for (int i = 0; i < same; ++i) rank += ties[i] > at ? 1 : 0;
+      if (rank < want) {
+        const int j = (1 << kEvIndexBits) - 1 - (int)(at & ((1u << kEvIndexBits) - 1u));
+        atomicOr((unsigned int*)bits + j / 32, 1u << (j & 31));
+      }
+    }
+    __syncthreads();
+  }
+  // ---- for every 64 rows: free places (below n) and moving rows (from n on) before them ------------------------------------------------
+  // (n is in the middle of one word, whose rows are of both kinds: its count of moving rows begins at 0, as that of all words behind)
+  auto free_of = [&](int x) __attribute__((always_inline)) {
+    const int left = n - 64 * x;
+    return left <= 0 ? 0ull : ~bits[x] & (left >= 64 ? ~0ull : (1ull << left) - 1ull);
+  };
+  auto moving_of = [&](int x) __attribute__((always_inline)) {
+    const int left = n - 64 * x;
+    return left >= 64 ? 0ull : bits[x] & (left <= 0 ? ~0ull : ~((1ull << left) - 1ull));
+  };
   int total = 0;
-  for (int v = 0; v < kEvWaves; ++v) total += wsum[0][v];
+  {
+    int carry = 0;
+    for (int x0 = 0; x0 < words; x0 += kEvThreads) {
+      const int x = x0 + tid;
+      // one sum over both kinds: free places of the words up to n's, then moving rows on top of all of them
+      const int f = x < words ? __builtin_popcountll(free_of(x)) : 0, m = x < words ? __builtin_popcountll(moving_of(x)) : 0;
+      int sum = f + m;
+#pragma unroll
+      for (int o = 1; o < 64; o *= 2) {
+        const int other = __shfl_up(sum, o, 64);
+        if (lane >= o) sum += other;
+      }
+      __syncthreads();
+      if (lane == 63) wsum[wave] = sum;
+      __syncthreads();
+      int before = carry + sum - f - m, all = 0;
+      for (int v = 0; v < kEvWaves; ++v) {
+        before += v < wave ? wsum[v] : 0;
+        all += wsum[v];
+      }
+      if (x < words) count[x] = before;
+      carry += all;
+    }
+    total = carry / 2;  // as many free places as moving rows
+  }
+  __syncthreads();
   // ---- the j-th moving row into the j-th free place, kEvList of them at a time ---------------------------------------------------------
+  const int nword = n / 64;  // words from here on may have moving rows; their counts begin behind `total` free places
   for (int from = 0; from == 0 || from < total; from += kEvList) {
+    if (from) __syncthreads();
+    for (int x = nword + wave; x < words; x += kEvWaves) {
+      const unsigned long long m = moving_of(x);
+      if ((m >> lane) & 1ull) {
+        const int rank = count[x] + (x == nword ? __builtin_popcountll(free_of(x)) : 0) - total + __builtin_popcountll(m & ((1ull << lane) - 1ull)) - from;
+        if (rank >= 0 && rank < kEvList) list[rank] = 64 * x + lane;
+      }
+    }
     __syncthreads();
-    int at = move0;
-    rows([&](int j, bool, bool stays) __attribute__((always_inline)) {
-      const bool moves = stays && j + lane >= n;
-      const unsigned long long mm = __builtin_amdgcn_ballot_w64(moves);
-      const int rank = at + __builtin_popcountll(mm & below) - from;
-      if (moves && rank >= 0 && rank < kEvList) list[rank] = j + lane;
-      at += __builtin_popcountll(mm);
-    });
-    __syncthreads();
-    at = hole0;
-    rows([&](int j, bool there, bool stays) __attribute__((always_inline)) {
-      const bool hole = there && !stays && j + lane < n;
-      const unsigned long long hm = __builtin_amdgcn_ballot_w64(hole);
-      const int rank = at + __builtin_popcountll(hm & below) - from;
-      if (hole && rank >= 0 && rank < kEvList) kept[j + lane] = list[rank];
-      if (from == 0 && stays && j + lane < n) kept[j + lane] = j + lane;
-      at += __builtin_popcountll(hm);
-    });
+    for (int j = tid; j < n; j += kEvThreads) {
+      const int x = j / 64;  // (the same for a wavefront)
+      const unsigned long long f = free_of(x);
+      if ((f >> lane) & 1ull) {
+        const int rank = count[x] + __builtin_popcountll(f & ((1ull << lane) - 1ull)) - from;
+        if (rank >= 0 && rank < kEvList) kept[j] = list[rank];
+      } else if (from == 0) {
+        kept[j] = j;
+      }
+    }
   }
 }
 
@@ -201,9 +300,16 @@ __global__ __launch_bounds__(256) void kv_evict_move_kernel(KvEvictParams p) {
   }
 }
 
+// f(kernel) for the one that a capacity takes (the lengths are known on the device)
+template <typename F>
+static hipError_t with_select(int kv_cap, F&& f) {
+  if (kv_cap <= 4 * kEvThreads) return f(kv_evict_select_kernel<4>);
+  if (kv_cap <= 16 * kEvThreads) return f(kv_evict_select_kernel<16>);
+  return f(kv_evict_select_kernel<0>);
+}
+
 hipError_t prepare_kv_evict() {
-  hipFuncAttributes attr;
-  return hipFuncGetAttributes(&attr, (const void*)kv_evict_select_kernel);
+  return hipFuncSetAttribute((const void*)kv_evict_select_kernel<0>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)evict_lds_bytes(kEvMaxRows));
 }
 
 }  // namespace ctcspec
@@ -227,9 +333,9 @@ extern "C" int kv_evict(ctcspec_ctx* ctx, ctcspec_dtype dt, void* k_cache, void*
   CTCSPEC_REQUIRE(ctx, weight_out != weight && (!pos || pos_out != pos) && ctx_len_out != ctx_len, CTCSPEC_EINVAL,
                   "kv_evict: weight_out, pos_out and ctx_len_out must not be the inputs");
   CTCSPEC_REQUIRE(ctx, dh % 8 == 0 && dh <= CTCSPEC_MAX_HEAD_DIM && B <= ctx->lim.max_batch && H_kv <= ctx->lim.max_heads &&
-                           dh <= ctx->lim.max_head_dim && B <= 65535 && H_kv <= 65535,
-                  CTCSPEC_EUNSUPPORTED, "kv_evict: dh must be a multiple of 8 and <= %d, the shape within the context's limits",
-                  CTCSPEC_MAX_HEAD_DIM);
+                           dh <= ctx->lim.max_head_dim && B <= 65535 && H_kv <= 65535 && kv_cap <= kEvMaxRows,
+                  CTCSPEC_EUNSUPPORTED, "kv_evict: dh must be a multiple of 8 and <= %d, kv_cap <= %d, the shape within the context's limits",
+                  CTCSPEC_MAX_HEAD_DIM, kEvMaxRows);
   CTCSPEC_REQUIRE(ctx, aligned16(k_cache) && aligned16(v_cache), CTCSPEC_EINVAL, "kv_evict: the caches must be 16-byte aligned");
   KvEvictParams p;
   p.k_cache = (unsigned char*)k_cache; p.v_cache = (unsigned char*)v_cache; p.kv_off = kv_off; p.ctx_len = ctx_len;
@@ -237,8 +343,10 @@ extern "C" int kv_evict(ctcspec_ctx* ctx, ctcspec_dtype dt, void* k_cache, void*
   p.ctx_len_out = ctx_len_out; p.kv_cap = kv_cap; p.H_kv = H_kv; p.budget = budget; p.sink = sink; p.recent = recent;
   p.elem_bytes = dt == CTCSPEC_F32 ? 4 : 2;
   p.row_bytes = dh * p.elem_bytes;
-  hipLaunchKernelGGL(kv_evict_select_kernel, dim3((unsigned)H_kv, (unsigned)B), dim3(kEvThreads), 0, ctx->stream, p);
-  CTCSPEC_HIP(ctx, hipGetLastError());
+  CTCSPEC_HIP(ctx, with_select(kv_cap, [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)H_kv, (unsigned)B), dim3(kEvThreads), evict_lds_bytes(kv_cap), ctx->stream, p);
+    return hipGetLastError();
+  }));
   const int rows = budget < kv_cap ? budget : kv_cap;
   hipLaunchKernelGGL(kv_evict_move_kernel, dim3((unsigned)((rows + 255) / 256), (unsigned)H_kv, (unsigned)B), dim3(256), 0, ctx->stream, p);
   CTCSPEC_HIP(ctx, hipGetLastError());

@@ -3,15 +3,14 @@
 //   weight[b,hk,j] += sum over the heads of hk's group and the accepted rows of exp(scale q . k_j - lse)
 //
 // With the rows' lse at hand (prefix_verify_attn) one read of K is all it takes: at most nine rows per head, so the call is bound by
-// that read.  S = Q K^T goes through matrix instructions with the rows of the group (up to 32 at a time) on one side and 32 keys on
-// the other; a lane then holds 16 rows of ONE key, and their sum is 16 additions and one exchange.
+// that read.  S = Q K^T goes through matrix instructions with 16 rows of the group on one side and 16 keys on the other; a
+// lane then holds four rows of ONE key, and a key's sum is three additions and two exchanges.  (32 x 32 tiles: twice the
+// exponentials for nine rows, and loads of 32 bytes of a key instead of 64.)
 #include <type_traits>
 
 #include "common.h"
 
 namespace ctcspec {
-
-typedef __attribute__((ext_vector_type(16))) float f32x16;
 
 struct KvWeightParams {
   const unsigned char* q;        // [B][H][max_nodes][dh]
@@ -25,46 +24,72 @@ struct KvWeightParams {
   float* weight;                 // [B][H_kv][kv_cap]
   int32_t* pos;                  // [B][H_kv][kv_cap] or null
   const int32_t* next_pos;       // [B] or null
-  int T, kv_cap, H, H_kv, group, dh, max_nodes;
+  int T, kv_cap, H, H_kv, group, dh, max_nodes, tiles;
   float sl2;                     // scale * log2(e)
 };
 
-constexpr int kKwTiles = 4;                       // key tiles of a wavefront
-constexpr int kKwKeys = 4 * 32 * kKwTiles;        // keys of a workgroup
-constexpr int kKwMaxRows = 9 * 256;               // rows of a group: (T + 1) heads
+constexpr int kKwMaxRows = 9 * 256;  // rows of a group: (T + 1) heads
 
-// DHP: dh padded.  ONE: the rows fit one block of 32 and stay in registers.
-template <bool F32, int DHP, bool ONE>
-__global__ __launch_bounds__(256) void kv_weight_kernel(KvWeightParams p) {
+// Tiles of 32 keys that a wavefront takes one after the other, each requested under the products of the one before: enough
+// wavefronts to fill the chip come first.
+inline int weight_tiles(long long tiles) {
+  const long long most = tiles / 4096;
+  return most < 1 ? 1 : (most > 8 ? 8 : (int)most);
+}
+
+// DHP: dh padded.  NB: blocks of 16 rows that stay in registers; 0: as many as there are, read again for every tile.
+template <bool F32, int DHP, int NB>
+__global__ __launch_bounds__(256, 2) void kv_weight_kernel(KvWeightParams p) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  constexpr int ES = F32 ? 4 : 2, QU = DHP * ES / 32;
+  constexpr int ES = F32 ? 4 : 2, QS = DHP * ES / 64;  // steps of 64 bytes of a row
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-  const int tid = threadIdx.x, lane = tid & 63, c = lane & 31, h2 = lane >> 5;
+  const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int kh = blockIdx.y, b = blockIdx.z, rb = p.dh * ES;
+  const bool fresh = blockIdx.x == gridDim.x - 1;  // the last workgroup: the rows that kv_commit appends
   int L = __builtin_amdgcn_readfirstlane(p.ctx_len[b]);
   L = L < 0 ? 0 : (L > p.kv_cap ? p.kv_cap : L);
-  const int key0 = blockIdx.x * kKwKeys;
-  if (key0 >= L && blockIdx.x != 0) return;  // (the first workgroup also has the new rows)
-  int len = __builtin_amdgcn_readfirstlane(p.accept_len[b]);
-  len = len < 0 ? 0 : (len > p.T ? p.T : len);
-  const int32_t* path = p.accept_nodes + (size_t)b * (p.T + 1);
-  const int rows = (len + 1) * p.group, blocks = (rows + 31) / 32;
+  const int key0 = blockIdx.x * p.tiles * 128 + wave * 32, step = 128;
+  if (!fresh && (int)(blockIdx.x * p.tiles * 128) >= L) return;
+  if (fresh && L >= p.kv_cap) return;  // no room for any
+
+  // ---- keys: lane (c, g) has 16 bytes of key c of a half tile, chunk 4 u + g -------------------------------------------------------
+  const unsigned char* kc = p.k_cache + ((size_t)p.kv_off[b] + (size_t)kh * p.kv_cap * p.dh) * ES;
+  auto load_keys = [&](int k0, u32x4 (&kf)[2][QS]) __attribute__((always_inline)) {
+    int left = L - k0;  // rows behind the last key: zeros, nothing is read
+    left = left < 0 ? 0 : (left > 32 ? 32 : left);
+    const unsigned long long at = (unsigned long long)(kc + (size_t)(left ? k0 : 0) * rb);
+    const unsigned long long base = (unsigned long long)(unsigned)__builtin_amdgcn_readfirstlane((int)(at >> 32)) << 32 |
+                                    (unsigned)__builtin_amdgcn_readfirstlane((int)at);
+    const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, (unsigned)__builtin_amdgcn_readfirstlane(left * rb), 0x00020000);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int u = 0; u < QS; ++u) {
+        const int o = u * 64 + g * 16;
+        kf[h][u] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, o < rb ? (16 * h + c) * rb + o : 0x40000000, 0, 0));
+      }
+  };
+  u32x4 kf[2][QS];
+  if (!fresh) load_keys(key0, kf);  // (first of all: nothing else is as far away)
 
   // ---- the rows: row r is head r % group of path entry r / group; its lse in the log2 domain (infinite: counts for nothing) and
   // where its query begins -------------------------------------------------------------------------------------------------------
+  int len = __builtin_amdgcn_readfirstlane(p.accept_len[b]);
+  len = len < 0 ? 0 : (len > p.T ? p.T : len);
+  const int32_t* path = p.accept_nodes + (size_t)b * (p.T + 1);
+  const int rows = (len + 1) * p.group, blocks = (rows + 15) / 16;
   float* row_lse = (float*)smem;
-  int* row_at = (int*)smem + blocks * 32;
+  int* row_at = (int*)smem + blocks * 16;
   const size_t head0 = (size_t)b * p.H + (size_t)kh * p.group;
-  for (int r = tid; r < blocks * 32; r += 256) {
+  for (int r = tid; r < blocks * 16; r += 256) {
     float v = INFINITY;
     int at = -1;
     if (r < rows) {
       const int i = r / p.group, node = path[i];
       if (node >= 0 && node < p.max_nodes) {
-        const int row = (r - i * p.group) * p.max_nodes + node;
-        const float s = p.lse[head0 * p.max_nodes + row];
-        at = row;
+        at = (r - i * p.group) * p.max_nodes + node;
+        const float s = p.lse[head0 * p.max_nodes + at];
         v = s == -INFINITY ? INFINITY : s * 1.4426950408889634f;
       }
     }
@@ -74,93 +99,91 @@ __global__ __launch_bounds__(256) void kv_weight_kernel(KvWeightParams p) {
   __syncthreads();
 
   const unsigned char* q = p.q + head0 * p.max_nodes * rb;
-  u32x4 qf[QU];
-  f32x4 lse[4];
-  auto load_rows = [&](int blk) __attribute__((always_inline)) {
-    const int at = row_at[blk * 32 + c];
+  auto load_rows = [&](int blk, u32x4 (&qf)[QS], f32x4& lse) __attribute__((always_inline)) {
+    const int at = row_at[blk * 16 + c];
 #pragma unroll
-    for (int i = 0; i < QU; ++i) {
-      const int o = (2 * i + h2) * 16;
-      qf[i] = u32x4{0u, 0u, 0u, 0u};
-      if (at >= 0 && o < rb) qf[i] = *(const u32x4*)(q + (size_t)at * rb + o);
+    for (int u = 0; u < QS; ++u) {
+      const int o = u * 64 + g * 16;
+      const u32x4 x = *(const u32x4*)(q + (size_t)(at < 0 ? 0 : at) * rb + (o < rb ? o : 0));
+      qf[u] = at >= 0 && o < rb ? x : u32x4{0u, 0u, 0u, 0u};
     }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) lse[j] = *(const f32x4*)(row_lse + blk * 32 + 8 * j + 4 * h2);  // registers 4 j .. 4 j + 3
+    lse = *(const f32x4*)(row_lse + blk * 16 + 4 * g);  // registers 0 .. 3 of the products
   };
-  // the rows' weights of this lane's key, added up; rows below `from` do not see it
-  auto gathered = [&](const u32x4 (&kf)[QU], int from) __attribute__((always_inline)) {
-    float sum = 0.f;
-    for (int blk = 0; blk < (ONE ? 1 : blocks); ++blk) {
-      if constexpr (!ONE) load_rows(blk);
-      f32x16 s;
+  // a block's weights of this lane's key; rows below `from` do not see it
+  auto weigh = [&](const u32x4 (&qf)[QS], f32x4 lse, const u32x4 (&kf)[QS], int row0, int from) __attribute__((always_inline)) {
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = 0.f;
+    for (int u = 0; u < QS; ++u) {
+      if constexpr (F32) {
 #pragma unroll
-      for (int i = 0; i < QU; ++i) {
-        if constexpr (F32) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            s = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(qf[i][e]), __uint_as_float(kf[i][e]), s, 0, 0, 0);
-        } else {
-          s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, qf[i]), __builtin_bit_cast(bf16x8, kf[i]), s, 0, 0, 0);
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float w = __builtin_amdgcn_exp2f(fmaf(s[i], p.sl2, -lse[i / 4][i % 4]));
-        const int r = blk * 32 + 8 * (i / 4) + 4 * h2 + i % 4;
-        // (a row that counts for nothing: its score may be anything, the query of a row that is none is zero)
-        sum += lse[i / 4][i % 4] < INFINITY || lse[i / 4][i % 4] != lse[i / 4][i % 4] ? (r >= from ? w : 0.f) : 0.f;
+        for (int e = 0; e < 4; ++e)
+          s = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(qf[u][e]), __uint_as_float(kf[u][e]), s, 0, 0, 0);
+      } else {
+        s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, qf[u]), __builtin_bit_cast(bf16x8, kf[u]), s, 0, 0, 0);
       }
     }
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float w = __builtin_amdgcn_exp2f(fmaf(s[i], p.sl2, -lse[i]));
+      // (a row that counts for nothing: its score may be anything)
+      sum += lse[i] == INFINITY || row0 + 4 * g + i < from ? 0.f : w;
+    }
+    return sum;
+  };
+  auto over_lanes = [&](float sum) __attribute__((always_inline)) {
+    sum += __shfl_xor(sum, 16, 64);
     return sum + __shfl_xor(sum, 32, 64);
   };
-  if constexpr (ONE) load_rows(0);
+  u32x4 qf[NB ? NB : 1][QS];
+  f32x4 lse[NB ? NB : 1];
+#pragma unroll
+  for (int i = 0; i < NB; ++i)
+    if (i < blocks) load_rows(i, qf[i], lse[i]);
+  // what the rows give the 16 keys of a half tile
+  auto gathered = [&](const u32x4 (&kf)[QS], int from) __attribute__((always_inline)) {
+    float sum = 0.f;
+    if constexpr (NB > 0) {
+#pragma unroll
+      for (int i = 0; i < NB; ++i)
+        if (i < blocks) sum += weigh(qf[i], lse[i], kf, 16 * i, from);
+    } else {
+      for (int i = 0; i < blocks; ++i) {
+        load_rows(i, qf[0], lse[0]);
+        sum += weigh(qf[0], lse[0], kf, 16 * i, from);
+      }
+    }
+    return over_lanes(sum);
+  };
 
   float* weight = p.weight + ((size_t)b * p.H_kv + kh) * p.kv_cap;
-  const unsigned char* kc = p.k_cache + ((size_t)p.kv_off[b] + (size_t)kh * p.kv_cap * p.dh) * ES;
-  auto load_keys = [&](int k0, u32x4 (&kf)[QU]) __attribute__((always_inline)) {
-    int left = L - k0;  // rows behind the last key: zeros, nothing is read
-    left = left < 0 ? 0 : (left > 32 ? 32 : left);
-    const long long at = (long long)(uintptr_t)(kc + (size_t)(left ? k0 : 0) * rb);
-    const long long base = (long long)((unsigned long long)(unsigned)__builtin_amdgcn_readfirstlane((int)(at >> 32)) << 32 |
-                                       (unsigned)__builtin_amdgcn_readfirstlane((int)at));
-    const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, (unsigned)__builtin_amdgcn_readfirstlane(left * rb), 0x00020000);
-#pragma unroll
-    for (int i = 0; i < QU; ++i) {
-      const int o = (2 * i + h2) * 16;
-      kf[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, o < rb ? c * rb + o : 0x40000000, 0, 0));
-    }
-  };
-  if (key0 < L) {
-    u32x4 kf[2][QU];
-    int k = key0 + wave * 32;
-    load_keys(k, kf[0]);
-#pragma unroll
-    for (int t = 0; t < kKwTiles; ++t, k += 128) {
-      if (k >= L) break;
-      const int j = k + c;
+  if (!fresh) {
+    for (int t = 0, k = key0; t < p.tiles && k < L; ++t, k += step) {
+      u32x4 next[2][QS];
+      const int j = k + (lane & 31);
       float old = 0.f;
-      if (h2 == 0 && j < L) old = weight[j];
-      if (t + 1 < kKwTiles) load_keys(k + 128, kf[(t + 1) & 1]);
-      const float sum = gathered(kf[t & 1], 0);
-      if (h2 == 0 && j < L) weight[j] = old + sum;
+      if (lane < 32 && j < L) old = weight[j];
+      if (t + 1 < p.tiles) load_keys(k + step, next);
+      const float first = gathered(kf[0], 0), second = gathered(kf[1], 0);
+      if (lane < 32 && j < L) weight[j] = old + (lane < 16 ? first : second);
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int u = 0; u < QS; ++u) kf[h][u] = next[h][u];
     }
-  }
-  // ---- the rows that kv_commit appends: path entry m becomes row L + m, seen by entries m and later --------------------------------
-  if (blockIdx.x == 0 && wave == 0) {
+  } else if (wave == 0) {
+    // path entry m becomes row L + m, seen by entries m and later
     const int node = c <= len ? path[c] : -1, j = L + c;
     const bool there = node >= 0 && node < p.max_nodes && j < p.kv_cap;
     const unsigned char* kt = p.k_tree + (((size_t)b * p.H_kv + kh) * p.max_nodes + (there ? node : 0)) * rb;
-    u32x4 kf[QU];
 #pragma unroll
-    for (int i = 0; i < QU; ++i) {
-      const int o = (2 * i + h2) * 16;
-      kf[i] = u32x4{0u, 0u, 0u, 0u};
-      if (there && o < rb) kf[i] = *(const u32x4*)(kt + o);
+    for (int u = 0; u < QS; ++u) {
+      const int o = u * 64 + g * 16;
+      const u32x4 x = *(const u32x4*)(kt + (o < rb ? o : 0));
+      kf[0][u] = o < rb ? x : u32x4{0u, 0u, 0u, 0u};
     }
-    const float sum = gathered(kf, c * p.group);
-    if (there && h2 == 0) {
+    const float sum = gathered(kf[0], c * p.group);
+    if (there && g == 0) {
       weight[j] = sum;
       if (p.pos) p.pos[((size_t)b * p.H_kv + kh) * p.kv_cap + j] = p.next_pos[b] + c;
     }
@@ -169,15 +192,20 @@ __global__ __launch_bounds__(256) void kv_weight_kernel(KvWeightParams p) {
 }
 
 template <bool F32, int DHP>
-static hipError_t launch_kv_weight(const KvWeightParams& p, dim3 grid, bool one, size_t lds, hipStream_t stream) {
-  if (one) hipLaunchKernelGGL((kv_weight_kernel<F32, DHP, true>), grid, dim3(256), lds, stream, p);
-  else hipLaunchKernelGGL((kv_weight_kernel<F32, DHP, false>), grid, dim3(256), lds, stream, p);
+static hipError_t launch_kv_weight(const KvWeightParams& p, dim3 grid, int blocks, hipStream_t stream) {
+  const size_t lds = (size_t)blocks * 16 * 8;
+  // rows of 256 and 512 bytes: five blocks and one are what the registers hold beside two tiles of keys
+  constexpr int kMost = F32 ? (DHP == 64 ? 3 : 1) : 5;
+  if (blocks == 1) hipLaunchKernelGGL((kv_weight_kernel<F32, DHP, 1>), grid, dim3(256), lds, stream, p);
+  else if (blocks <= 3 && kMost >= 3) hipLaunchKernelGGL((kv_weight_kernel<F32, DHP, kMost >= 3 ? 3 : 1>), grid, dim3(256), lds, stream, p);
+  else if (blocks <= kMost) hipLaunchKernelGGL((kv_weight_kernel<F32, DHP, kMost>), grid, dim3(256), lds, stream, p);
+  else hipLaunchKernelGGL((kv_weight_kernel<F32, DHP, 0>), grid, dim3(256), lds, stream, p);
   return hipGetLastError();
 }
 
 hipError_t prepare_kv_weight() {
   hipFuncAttributes attr;
-  return hipFuncGetAttributes(&attr, (const void*)kv_weight_kernel<false, 128, true>);
+  return hipFuncGetAttributes(&attr, (const void*)kv_weight_kernel<false, 128, 1>);
 }
 
 }  // namespace ctcspec
@@ -213,13 +241,12 @@ extern "C" int kv_weight_update(ctcspec_ctx* ctx, ctcspec_dtype dt, const void* 
   p.weight = weight; p.pos = pos; p.next_pos = next_pos;
   p.T = T; p.kv_cap = kv_cap; p.H = H; p.H_kv = H_kv; p.group = H / H_kv; p.dh = dh; p.max_nodes = max_nodes;
   p.sl2 = scale * 1.4426950408889634f;
-  const int rows = (T + 1) * p.group, blocks = (rows + 31) / 32;
-  const dim3 grid((unsigned)(((long long)kv_cap + kKwKeys - 1) / kKwKeys), (unsigned)H_kv, (unsigned)B);
-  const size_t lds = (size_t)blocks * 32 * 8;
-  const bool one = blocks == 1;
+  p.tiles = weight_tiles((long long)B * H_kv * ((kv_cap + 31LL) / 32));
+  const int blocks = ((T + 1) * p.group + 15) / 16;
+  const dim3 grid((unsigned)(((long long)kv_cap + 128 * p.tiles - 1) / (128 * p.tiles)) + 1, (unsigned)H_kv, (unsigned)B);
   hipError_t e;
-  if (dt == CTCSPEC_F32) e = dh <= 64 ? launch_kv_weight<true, 64>(p, grid, one, lds, ctx->stream) : launch_kv_weight<true, 128>(p, grid, one, lds, ctx->stream);
-  else e = dh <= 64 ? launch_kv_weight<false, 64>(p, grid, one, lds, ctx->stream) : launch_kv_weight<false, 128>(p, grid, one, lds, ctx->stream);
+  if (dt == CTCSPEC_F32) e = dh <= 64 ? launch_kv_weight<true, 64>(p, grid, blocks, ctx->stream) : launch_kv_weight<true, 128>(p, grid, blocks, ctx->stream);
+  else e = dh <= 64 ? launch_kv_weight<false, 64>(p, grid, blocks, ctx->stream) : launch_kv_weight<false, 128>(p, grid, blocks, ctx->stream);
   CTCSPEC_HIP(ctx, e);
   return CTCSPEC_OK;
 }
