@@ -31,26 +31,28 @@ constexpr int kEvWaves = 16, kEvThreads = 64 * kEvWaves;
 constexpr int kEvBins = 2048;      // of a digit of up to 11 bits
 constexpr int kEvIndexBits = 20;   // of a row
 constexpr int kEvMaxRows = 1 << 19;
-constexpr int kEvTies = 256;       // rows that are compared with each other
+constexpr int kEvListed = 4096;    // rows that are listed once their number is below that
+constexpr int kEvTies = 256;       // ... and that are compared with each other
 constexpr int kEvList = 8192;      // moved rows per round
-// LDS: the bins, and from then on the list of the moved rows in their place; then for every 64 rows their bits and how many of
-// the kind that counts there lie before them
-constexpr int kEvListBytes = kEvList * 4;
-static_assert(kEvListBytes >= kEvBins * 4 + kEvTies * 8);
+// LDS: the bins and the lists of the search, and from then on the list of the moved rows in their place; then for every 64 rows their
+// bits and how many of the kind that counts there lie before them
+constexpr int kEvListBytes = kEvBins * 4 + kEvTies * 8 + kEvListed * 8;
+static_assert(kEvListBytes >= kEvList * 4 && kEvListed % kEvThreads == 0);
 constexpr size_t evict_lds_bytes(int kv_cap) { return kEvListBytes + (size_t)((kv_cap + 63) / 64) * 12; }
 
 // Order of the rows: larger weight first, then smaller index; rows that stay in any case before all others; a weight that is not
 // a number behind all others.  (fresh: positions from there on stay.)
 __device__ __forceinline__ unsigned int evict_key(float weight, int pos, int sink, int fresh) {
-  const unsigned int key = weight != weight ? 0u : float_to_ordered(weight);
+  const unsigned int u = __float_as_uint(weight + 0.0f);  // (-0 becomes 0)
+  const unsigned int key = weight != weight ? 0u : u ^ ((unsigned)((int)u >> 31) | 0x80000000u);
   return pos < sink || pos >= fresh ? 0xffffffffu : key;
 }
 
-// The order as one number: the key, then the index from the top - no two rows have the same -, searched digit by digit for
-// the n-th largest until the rows that share the digits so far all stay or are few enough to be compared with each other.  Then a
+// The order is that of the key, then of the index from the top - no two rows have the same place -, searched digit by digit for
+// the n-th until the rows that share the digits so far all stay or are few enough to be compared with each other.  Then a
 // bit for every row that stays, and everything else follows from counts of bits.
 // K: a lane holds up to K keys in registers (rows 64 k + lane of its wavefront's range): the passes read memory once.  0: for
-// capacities beyond that; every pass reads the weights again, eight rows of a lane at a time.
+// capacities beyond that; every pass reads the weights again, eight rows of a lane at a time and the next eight under way.
 template <int K>
 __global__ __launch_bounds__(kEvThreads) void kv_evict_select_kernel(KvEvictParams p) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
@@ -71,6 +73,7 @@ __global__ __launch_bounds__(kEvThreads) void kv_evict_select_kernel(KvEvictPara
   }
   unsigned int* hist = (unsigned int*)smem;
   unsigned long long* ties = (unsigned long long*)(smem + kEvBins * 4);
+  unsigned long long* listed = ties + kEvTies;
   int* list = (int*)smem;
   const int words = (L + 63) / 64;
   unsigned long long* bits = (unsigned long long*)(smem + kEvListBytes);
@@ -81,76 +84,74 @@ __global__ __launch_bounds__(kEvThreads) void kv_evict_select_kernel(KvEvictPara
   const int sink = pos ? p.sink : -0x7fffffff - 1, fresh = p.recent > 0 ? p.next_pos[b] - p.recent : 0x7fffffff;
   const int range = (words + kEvWaves - 1) / kEvWaves * 64, j0 = wave * range;  // this wavefront's rows
   const int rows = j0 < L ? (L - j0 < range ? L - j0 : range) : 0;
-  // keys of rows j0 + 64 (k0 + i) + lane, i < N; rows that are none get the smallest
-  auto load = [&]<int N>(int k0, unsigned int (&key)[N]) __attribute__((always_inline)) {
-    float v[N];
-    int at[N];
+  // weights and positions of rows j0 + 64 (k0 + i) + lane, i < N (behind the last row: the last one again), and their keys
+  auto load = [&]<int N>(int k0, float (&v)[N], int (&at)[N]) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int j = j0 + 64 * (k0 + i) + lane;
-      v[i] = w[j < L ? j : L - 1];
+      const unsigned int j = (unsigned)(j0 + 64 * (k0 + i) + lane), last = (unsigned)L - 1u, off = (j < last ? j : last) * 4u;
+      v[i] = *(const float*)((const char*)w + off);
+      at[i] = pos ? *(const int32_t*)((const char*)pos + off) : 0;
     }
-#pragma unroll
-    for (int i = 0; i < N; ++i) at[i] = 0;
-    if (pos) {
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const int j = j0 + 64 * (k0 + i) + lane;
-        at[i] = pos[j < L ? j : L - 1];
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < N; ++i) key[i] = evict_key(v[i], at[i], sink, fresh);
   };
   unsigned int mine[K ? K : 1];
   if constexpr (K > 0) {
     constexpr int N = K < 16 ? K : 16;
 #pragma unroll
     for (int k = 0; k < K; k += N) {
-      unsigned int some[N];
-      load(k, some);
+      float v[N];
+      int at[N];
+      load(k, v, at);
 #pragma unroll
-      for (int i = 0; i < N; ++i) mine[k + i] = some[i];
+      for (int i = 0; i < N; ++i) mine[k + i] = evict_key(v[i], at[i], sink, fresh);
     }
   }
-  // f(k, whether the row exists, its place in the order)
+  // f(k, whether the row exists, its key)
   auto each = [&](auto&& f) __attribute__((always_inline)) {
-    auto order = [&](unsigned int key, int k) __attribute__((always_inline)) {
-      return (unsigned long long)key << kEvIndexBits | (unsigned)((1 << kEvIndexBits) - 1 - (j0 + 64 * k + lane));
-    };
     if constexpr (K > 0) {
 #pragma unroll
       for (int k = 0; k < K; ++k)
-        if (64 * k < rows) f(k, 64 * k + lane < rows, order(mine[k], k));
+        if (64 * k < rows) f(k, 64 * k + lane < rows, mine[k]);
     } else {
-      for (int k0 = 0; 64 * k0 < rows; k0 += 8) {
-        unsigned int some[8];
-        load(k0, some);
+      constexpr int N = 8;  // with as many more under way
+      float v[N], next_v[N];
+      int at[N], next_at[N];
+      if (rows > 0) load(0, v, at);
+      for (int k0 = 0; 64 * k0 < rows; k0 += N) {
+        load(k0 + N, next_v, next_at);
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (64 * (k0 + i) < rows) f(k0 + i, 64 * (k0 + i) + lane < rows, order(some[i], k0 + i));
+        for (int i = 0; i < N; ++i)
+          if (64 * (k0 + i) < rows) f(k0 + i, 64 * (k0 + i) + lane < rows, evict_key(v[i], at[i], sink, fresh));
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          v[i] = next_v[i];
+          at[i] = next_at[i];
+        }
       }
     }
   };
+  // a row's index from the top (formed where it is needed: K of them would take as many registers as the keys)
+  auto from_top = [&](int k) __attribute__((always_inline)) {
+    int l = lane;
+    asm volatile("" : "+v"(l));
+    return (unsigned)((1 << kEvIndexBits) - 1 - (j0 + 64 * k + l));
+  };
 
-  // ---- the search: `want` of the `same` rows whose place begins with `prefix` (the bits from `shift` on) stay, and all before them ----
-  unsigned long long prefix = 0ull;
-  int want = n, same = L, shift = 32 + kEvIndexBits;
-  while (same > want && same > kEvTies) {
-    const int bits_left = shift, digit = bits_left > 30 ? 11 : 10;
-    shift -= digit;
+  // ---- the search: `want` of the `same` rows that share the digits so far stay, and all before them --------------------------------------
+  // (keys in registers cost little to go over again)
+  constexpr int kMost = K ? kEvTies : kEvListed;
+  int want = n, same = L;
+  // one digit: counts(f): f(whether a row counts, its digit)
+  auto digit = [&](auto&& counts) __attribute__((always_inline)) {
     hist[tid] = hist[tid + kEvThreads] = 0u;
     __syncthreads();
-    each([&](int, bool there, unsigned long long at) __attribute__((always_inline)) {
-      const bool counts = there && (at >> (shift + digit)) == prefix;
-      const unsigned int bin = (unsigned)(at >> shift) & ((1u << digit) - 1u);
+    counts([&](bool here, unsigned int bin) __attribute__((always_inline)) {
       // (equal weights are common - rows that nobody looked at -, and 64 additions to one place follow one another)
-      const unsigned long long m = __builtin_amdgcn_ballot_w64(counts);
+      const unsigned long long m = __builtin_amdgcn_ballot_w64(here);
       if (m == 0ull) return;
       const unsigned int one = (unsigned)__builtin_amdgcn_readlane((int)bin, __builtin_ctzll(m));
-      if (__builtin_amdgcn_ballot_w64(counts && bin != one) == 0ull) {
+      if (__builtin_amdgcn_ballot_w64(bin == one && here) == m) {
         if (lane == 0) atomicAdd(&hist[one], (unsigned)__builtin_popcountll(m));
-      } else if (counts) {
+      } else if (here) {
         atomicAdd(&hist[bin], 1u);
       }
     });
@@ -171,9 +172,36 @@ __global__ __launch_bounds__(kEvThreads) void kv_evict_select_kernel(KvEvictPara
     if (above < want && want <= above + c1) { found[0] = hi; found[1] = above; found[2] = c1; }
     else if (above + c1 < want && want <= above + c1 + c0) { found[0] = hi - 1; found[1] = above + c1; found[2] = c0; }
     __syncthreads();
-    prefix = prefix << digit | (unsigned)found[0];
     want -= found[1];
     same = found[2];
+    return (unsigned)found[0];
+  };
+  // the key's digits: 11, 11 and 10 bits
+  unsigned int prefix = 0u;
+  int shift = 32;
+  while (shift > 0 && same > want && same > kMost) {
+    const int bits_of = shift == 10 ? 10 : 11, above = shift;
+    shift -= bits_of;
+    const unsigned int d = digit([&](auto&& f) __attribute__((always_inline)) {
+      each([&](int, bool there, unsigned int key) __attribute__((always_inline)) {
+        f(there && (above == 32 || key >> (above & 31) == prefix), (key >> shift) & ((1u << bits_of) - 1u));
+      });
+    });
+    prefix = prefix << bits_of | d;
+  }
+  // (equal keys) the index's digits: 10 bits each
+  unsigned int iprefix = 0u;
+  int ishift = kEvIndexBits;
+  while (ishift > 0 && same > want && same > kMost) {
+    const int above = ishift;
+    ishift -= 10;
+    const unsigned int d = digit([&](auto&& f) __attribute__((always_inline)) {
+      each([&](int k, bool there, unsigned int key) __attribute__((always_inline)) {
+        const unsigned int at = from_top(k);
+        f(there && key == prefix && at >> above == iprefix, (at >> ishift) & 1023u);
+      });
+    });
+    iprefix = iprefix << 10 | d;
   }
   // ---- a bit for every row that stays -----------------------------------------------------------------------------------------------
   const bool compare = same > want;
@@ -182,22 +210,65 @@ __global__ __launch_bounds__(kEvThreads) void kv_evict_select_kernel(KvEvictPara
     if (tid == 0) found[0] = 0;
     __syncthreads();
   }
-  each([&](int k, bool there, unsigned long long at) __attribute__((always_inline)) {
-    const unsigned long long top = at >> shift;
-    const unsigned long long m = __builtin_amdgcn_ballot_w64(there && (top > prefix || (top == prefix && !compare)));
+  each([&](int k, bool there, unsigned int key) __attribute__((always_inline)) {
+    const unsigned int top = shift == 32 ? 0u : key >> shift;  // (no digit was looked at: all rows share what there is)
+    bool sure = there && top > prefix, tie = there && top == prefix;
+    if (ishift < kEvIndexBits) {
+      const unsigned int at = from_top(k) >> ishift;
+      sure |= tie && at > iprefix;
+      tie &= at == iprefix;
+    }
+    const unsigned long long m = __builtin_amdgcn_ballot_w64(sure || (tie && !compare));
     if (lane == 0) bits[j0 / 64 + k] = m;
-    if (compare && there && top == prefix) ties[atomicAdd(&found[0], 1)] = at;
+    if (compare) {
+      const unsigned long long tm = __builtin_amdgcn_ballot_w64(tie);
+      if (tm != 0ull) {
+        int at = 0;
+        if (lane == 0) at = atomicAdd(&found[0], __builtin_popcountll(tm));
+        at = __builtin_amdgcn_readfirstlane(at) + __builtin_popcountll(tm & ((1ull << lane) - 1ull));
+        if (tie) listed[at] = (unsigned long long)key << kEvIndexBits | from_top(k);
+      }
+    }
   });
   __syncthreads();
-  if (compare) {
-    if (tid < same) {
+  if (compare) {  // among those that are listed now: the rest of the digits, then with each other
+    constexpr int kMine = K ? 1 : kEvListed / kEvThreads;
+    unsigned long long place[kMine];
+    const int entries = same;
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) place[i] = tid + i * kEvThreads < entries ? listed[tid + i * kEvThreads] : 0ull;
+    int low = ishift < kEvIndexBits ? ishift : shift + kEvIndexBits;  // the bits below are still to be looked at
+    unsigned long long first = listed[0] >> low;
+    while (same > want && same > kEvTies) {  // (no two places are the same)
+      const int above = low, bits_of = low < 11 ? low : 11;
+      low -= bits_of;
+      const unsigned int d = digit([&](auto&& f) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < kMine; ++i)
+          f(tid + i * kEvThreads < entries && place[i] >> above == first, (unsigned)(place[i] >> low) & ((1u << bits_of) - 1u));
+      });
+      first = first << bits_of | d;
+    }
+    auto stays = [&](unsigned long long at) __attribute__((always_inline)) {
+      const int j = (1 << kEvIndexBits) - 1 - (int)(at & ((1u << kEvIndexBits) - 1u));
+      atomicOr((unsigned int*)bits + j / 32, 1u << (j & 31));
+    };
+    __syncthreads();
+    if (tid == 0) found[0] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+      if (tid + i * kEvThreads >= entries) continue;
+      const unsigned long long top = place[i] >> low;
+      if (top > first || (top == first && same == want)) stays(place[i]);
+      else if (top == first) ties[atomicAdd(&found[0], 1)] = place[i];
+    }
+    __syncthreads();
+    if (same > want && tid < same) {
       const unsigned long long at = ties[tid];
       int rank = 0;
       for (int i = 0; i < same; ++i) rank += ties[i] > at ? 1 : 0;
-      if (rank < want) {
-        const int j = (1 << kEvIndexBits) - 1 - (int)(at & ((1u << kEvIndexBits) - 1u));
-        atomicOr((unsigned int*)bits + j / 32, 1u << (j & 31));
-      }
+      if (rank < want) stays(at);
     }
     __syncthreads();
   }
