@@ -463,13 +463,18 @@ __global__ __launch_bounds__(64 * SH::NW, SH::WPE) void prefix_attn_kernel(Prefi
               // P is rounded to bf16, as the values are and as the result will be; FINE: P = hi + lo, within 2^-17 of it
               const float p0 = __builtin_amdgcn_exp2f(fmaf(s[qt][2 * j], p.sl2, -ms[qt]));
               const float p1 = __builtin_amdgcn_exp2f(fmaf(s[qt][2 * j + 1], p.sl2, -ms[qt]));
-              sum[qt] += p0 + p1;
-              asm volatile("" : "+v"(sum[qt]));  // (here, not at the end of the tile)
               const unsigned int h = __builtin_bit_cast(unsigned int, bf16x2{(__bf16)p0, (__bf16)p1});
               hi[qt][j / 4][j % 4] = h;
-              if constexpr (SH::FINE)
-                lo[qt][j / 4][j % 4] = __builtin_bit_cast(
-                    unsigned int, bf16x2{(__bf16)(p0 - __uint_as_float(h << 16)), (__bf16)(p1 - __uint_as_float(h & 0xffff0000u))});
+              if constexpr (SH::FINE) {
+                // (the sum is that of the rounded weights: what both are off by in common goes - all of it where one key has the weight)
+                const float h0 = __uint_as_float(h << 16), h1 = __uint_as_float(h & 0xffff0000u);
+                const unsigned int r = __builtin_bit_cast(unsigned int, bf16x2{(__bf16)(p0 - h0), (__bf16)(p1 - h1)});
+                lo[qt][j / 4][j % 4] = r;
+                sum[qt] += (h0 + __uint_as_float(r << 16)) + (h1 + __uint_as_float(r & 0xffff0000u));
+              } else {
+                sum[qt] += p0 + p1;
+              }
+              asm volatile("" : "+v"(sum[qt]));  // (here, not at the end of the tile)
             }
         };
         constexpr int kReads = 4 * DT / QU;
