@@ -29,16 +29,19 @@ struct KvEvictParams {
 
 constexpr int kEvWaves = 16, kEvThreads = 64 * kEvWaves;
 constexpr int kEvBins = 2048;      // of a digit of up to 11 bits
+constexpr int kEvCopies = 4;       // of every bin, for lanes next to each other: equal digits are common, and additions to one place follow one another
 constexpr int kEvIndexBits = 20;   // of a row
 constexpr int kEvMaxRows = 1 << 19;
 constexpr int kEvListed = 4096;    // rows that are listed once their number is below that
 constexpr int kEvTies = 256;       // ... and that are compared with each other
 constexpr int kEvList = 8192;      // moved rows per round
-// LDS: the bins and the lists of the search, and from then on the list of the moved rows in their place; then for every 64 rows their
-// bits and how many of the kind that counts there lie before them
-constexpr int kEvListBytes = kEvBins * 4 + kEvTies * 8 + kEvListed * 8;
-static_assert(kEvListBytes >= kEvList * 4 && kEvListed % kEvThreads == 0);
-constexpr size_t evict_lds_bytes(int kv_cap) { return kEvListBytes + (size_t)((kv_cap + 63) / 64) * 12; }
+// LDS, one after the other in the same place: the bins of the search; for every 64 rows the bits of those that are still to be
+// decided; the bins and the list of those rows; the rows that are compared; for every 64 rows how many of the kind that counts there
+// lie before them, and the list of the moved rows.  Behind that, for every 64 rows, the bits of those that stay.
+constexpr int kEvBinBytes = kEvBins * kEvCopies * 4, kEvListBytes = kEvBinBytes + kEvList * 4;
+static_assert(kEvMaxRows / 64 * 8 <= kEvListBytes && kEvMaxRows / 64 * 4 <= kEvBinBytes);
+static_assert(kEvListed <= kEvList && kEvTies * 8 <= kEvBinBytes && kEvListed % kEvThreads == 0 && kEvTies % 64 == 0 && kEvTies <= 64 * kEvWaves);
+constexpr size_t evict_lds_bytes(int kv_cap) { return kEvListBytes + (size_t)((kv_cap + 63) / 64) * 8; }
 
 // Order of the rows: larger weight first, then smaller index; rows that stay in any case before all others; a weight that is not
 // a number behind all others.  (fresh: positions from there on stay.)
@@ -52,7 +55,12 @@ __device__ __forceinline__ unsigned int evict_key(float weight, int pos, int sin
 // the n-th until the rows that share the digits so far all stay or are few enough to be compared with each other.  Then a
 // bit for every row that stays, and everything else follows from counts of bits.
 // K: a lane holds up to K keys in registers (rows 64 k + lane of its wavefront's range): the passes read memory once.  0: for
-// capacities beyond that; every pass reads the weights again, eight rows of a lane at a time and the next eight under way.
+// capacities beyond that; every pass reads the weights again, eight rows of a lane at a time and the next eight under way.  (The
+// call in us with the keys in registers / read again: 700 rows 12.3 / 18.3, 2304 rows 27.1 / 35.7, 4000 rows 27.3 / 37.4, 12000 rows
+// 59.8 / 66.1; with 96 rows in registers 65536 rows 91 / 74: they leave none for the rows of a step.)
+// What bounds it: up to some thousand rows the steps' latencies, one workgroup behind each other's barriers; beyond, instructions - a
+// compute unit takes a cycle for one on 64 rows -, of which a row takes about 20 in each of the two or three passes.  (32 heads of
+// 65536 rows to 4096: 43 us; 256 heads of 2304 rows to 2048: 10.5 us.)
 template <int K>
 __global__ __launch_bounds__(kEvThreads) void kv_evict_select_kernel(KvEvictParams p) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
@@ -72,12 +80,12 @@ __global__ __launch_bounds__(kEvThreads) void kv_evict_select_kernel(KvEvictPara
     return;
   }
   unsigned int* hist = (unsigned int*)smem;
-  unsigned long long* ties = (unsigned long long*)(smem + kEvBins * 4);
-  unsigned long long* listed = ties + kEvTies;
-  int* list = (int*)smem;
+  unsigned long long* ties = (unsigned long long*)smem;
+  int* count = (int*)smem;
+  unsigned long long* open = (unsigned long long*)smem;
+  int* list = (int*)(smem + kEvBinBytes);
   const int words = (L + 63) / 64;
   unsigned long long* bits = (unsigned long long*)(smem + kEvListBytes);
-  int* count = (int*)(bits + words);
 
   const float* w = p.weight + head * p.kv_cap;
   const int32_t* pos = p.pos ? p.pos + head * p.kv_cap : nullptr;
@@ -86,11 +94,21 @@ __global__ __launch_bounds__(kEvThreads) void kv_evict_select_kernel(KvEvictPara
   const int rows = j0 < L ? (L - j0 < range ? L - j0 : range) : 0;
   // weights and positions of rows j0 + 64 (k0 + i) + lane, i < N (behind the last row: the last one again), and their keys
   auto load = [&]<int N>(int k0, float (&v)[N], int (&at)[N]) __attribute__((always_inline)) {
+    if (64 * (k0 + N) <= rows) {
+      const unsigned int off = lane * 4u;
+      const char *wk = (const char*)(w + j0 + 64 * k0), *pk = (const char*)(pos + j0 + 64 * k0);
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const unsigned int j = (unsigned)(j0 + 64 * (k0 + i) + lane), last = (unsigned)L - 1u, off = (j < last ? j : last) * 4u;
-      v[i] = *(const float*)((const char*)w + off);
-      at[i] = pos ? *(const int32_t*)((const char*)pos + off) : 0;
+      for (int i = 0; i < N; ++i) {
+        v[i] = *(const float*)(wk + off + i * 256);
+        at[i] = pos ? *(const int32_t*)(pk + off + i * 256) : 0;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const unsigned int j = (unsigned)(j0 + 64 * (k0 + i) + lane), last = (unsigned)L - 1u, off = (j < last ? j : last) * 4u;
+        v[i] = *(const float*)((const char*)w + off);
+        at[i] = pos ? *(const int32_t*)((const char*)pos + off) : 0;
+      }
     }
   };
   unsigned int mine[K ? K : 1];
@@ -103,26 +121,46 @@ __global__ __launch_bounds__(kEvThreads) void kv_evict_select_kernel(KvEvictPara
       load(k, v, at);
 #pragma unroll
       for (int i = 0; i < N; ++i) mine[k + i] = evict_key(v[i], at[i], sink, fresh);
+#pragma unroll
+      for (int i = 0; i < N; ++i) asm volatile("" : "+v"(mine[k + i]));
     }
   }
-  // f(k, whether the row exists, its key)
+  // f(k, whether the rows exist, their keys) for G of the lane's rows at a time, from row k on.  (Nothing but instructions bounds a
+  // pass over many rows - one costs a compute unit a cycle for every 64 of them -, so rows that all exist are not asked.)
+  constexpr int G = K && K < 8 ? K : 8;
+  auto some = [&](int k, const unsigned int (&key)[G], auto&& f) __attribute__((always_inline)) {
+    bool there[G];
+    if (64 * (k + G) <= rows) {
+#pragma unroll
+      for (int i = 0; i < G; ++i) there[i] = true;
+      f(k, there, key);
+    } else {
+#pragma unroll
+      for (int i = 0; i < G; ++i) there[i] = 64 * (k + i) + lane < rows;
+      f(k, there, key);
+    }
+  };
   auto each = [&](auto&& f) __attribute__((always_inline)) {
+    unsigned int key[G];
     if constexpr (K > 0) {
 #pragma unroll
-      for (int k = 0; k < K; ++k)
-        if (64 * k < rows) f(k, 64 * k + lane < rows, mine[k]);
+      for (int k = 0; k < K; k += G) {
+        if (64 * k >= rows) continue;
+#pragma unroll
+        for (int i = 0; i < G; ++i) key[i] = mine[k + i];
+        some(k, key, f);
+      }
     } else {
-      constexpr int N = 8;  // with as many more under way
-      float v[N], next_v[N];
-      int at[N], next_at[N];
+      float v[G], next_v[G];  // with as many more under way
+      int at[G], next_at[G];
       if (rows > 0) load(0, v, at);
-      for (int k0 = 0; 64 * k0 < rows; k0 += N) {
-        load(k0 + N, next_v, next_at);
+      for (int k = 0; 64 * k < rows; k += G) {
+        load(k + G, next_v, next_at);
 #pragma unroll
-        for (int i = 0; i < N; ++i)
-          if (64 * (k0 + i) < rows) f(k0 + i, 64 * (k0 + i) + lane < rows, evict_key(v[i], at[i], sink, fresh));
+        for (int i = 0; i < G; ++i) key[i] = evict_key(v[i], at[i], sink, fresh);
+        some(k, key, f);
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
+        for (int i = 0; i < G; ++i) {
           v[i] = next_v[i];
           at[i] = next_at[i];
         }
@@ -142,23 +180,18 @@ __global__ __launch_bounds__(kEvThreads) void kv_evict_select_kernel(KvEvictPara
   int want = n, same = L;
   // one digit: counts(f): f(whether a row counts, its digit)
   auto digit = [&](auto&& counts) __attribute__((always_inline)) {
-    hist[tid] = hist[tid + kEvThreads] = 0u;
+#pragma unroll
+    for (int i = 0; i < kEvBins * kEvCopies / kEvThreads / 4; ++i) ((u32x4*)hist)[tid + i * kEvThreads] = u32x4{0u, 0u, 0u, 0u};
     __syncthreads();
     counts([&](bool here, unsigned int bin) __attribute__((always_inline)) {
-      // (equal weights are common - rows that nobody looked at -, and 64 additions to one place follow one another)
-      const unsigned long long m = __builtin_amdgcn_ballot_w64(here);
-      if (m == 0ull) return;
-      const unsigned int one = (unsigned)__builtin_amdgcn_readlane((int)bin, __builtin_ctzll(m));
-      if (__builtin_amdgcn_ballot_w64(bin == one && here) == m) {
-        if (lane == 0) atomicAdd(&hist[one], (unsigned)__builtin_popcountll(m));
-      } else if (here) {
-        atomicAdd(&hist[bin], 1u);
-      }
+      if (here) atomicAdd(&hist[bin * kEvCopies + (lane & (kEvCopies - 1))], 1u);
     });
     __syncthreads();
     // thread t: bins 2 t and 2 t + 1 from the top; how many rows lie in the bins above
     const int hi = kEvBins - 1 - 2 * tid;
-    const int c1 = (int)hist[hi], c0 = (int)hist[hi - 1];
+    static_assert(kEvCopies == 4 && kEvBins == 2 * kEvThreads);
+    const u32x4 h1 = ((const u32x4*)hist)[hi], h0 = ((const u32x4*)hist)[hi - 1];
+    const int c1 = (int)(h1[0] + h1[1] + h1[2] + h1[3]), c0 = (int)(h0[0] + h0[1] + h0[2] + h0[3]);
     int sum = c0 + c1;
 #pragma unroll
     for (int o = 1; o < 64; o *= 2) {
@@ -179,12 +212,22 @@ __global__ __launch_bounds__(kEvThreads) void kv_evict_select_kernel(KvEvictPara
   // the key's digits: 11, 11 and 10 bits
   unsigned int prefix = 0u;
   int shift = 32;
+  if (same > kMost) {
+    shift = 21;
+    prefix = digit([&](auto&& f) __attribute__((always_inline)) {
+      each([&](int, const bool (&there)[G], const unsigned int (&key)[G]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < G; ++i) f(there[i], key[i] >> 21);
+      });
+    });
+  }
   while (shift > 0 && same > want && same > kMost) {
-    const int bits_of = shift == 10 ? 10 : 11, above = shift;
+    const int bits_of = shift == 21 ? 11 : 10, above = shift;
     shift -= bits_of;
     const unsigned int d = digit([&](auto&& f) __attribute__((always_inline)) {
-      each([&](int, bool there, unsigned int key) __attribute__((always_inline)) {
-        f(there && (above == 32 || key >> (above & 31) == prefix), (key >> shift) & ((1u << bits_of) - 1u));
+      each([&](int, const bool (&there)[G], const unsigned int (&key)[G]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < G; ++i) f(there[i] && key[i] >> above == prefix, (key[i] >> shift) & ((1u << bits_of) - 1u));
       });
     });
     prefix = prefix << bits_of | d;
@@ -196,79 +239,121 @@ __global__ __launch_bounds__(kEvThreads) void kv_evict_select_kernel(KvEvictPara
     const int above = ishift;
     ishift -= 10;
     const unsigned int d = digit([&](auto&& f) __attribute__((always_inline)) {
-      each([&](int k, bool there, unsigned int key) __attribute__((always_inline)) {
-        const unsigned int at = from_top(k);
-        f(there && key == prefix && at >> above == iprefix, (at >> ishift) & 1023u);
+      each([&](int k, const bool (&there)[G], const unsigned int (&key)[G]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < G; ++i) {
+          const unsigned int at = from_top(k + i);
+          f(there[i] && key[i] == prefix && at >> above == iprefix, (at >> ishift) & 1023u);
+        }
       });
     });
     iprefix = iprefix << 10 | d;
   }
-  // ---- a bit for every row that stays -----------------------------------------------------------------------------------------------
+  // ---- a bit for every row that stays; the others that share the digits so far ---------------------------------------------------------
   const bool compare = same > want;
-  if (compare) {
-    __syncthreads();
-    if (tid == 0) found[0] = 0;
-    __syncthreads();
-  }
-  each([&](int k, bool there, unsigned int key) __attribute__((always_inline)) {
-    const unsigned int top = shift == 32 ? 0u : key >> shift;  // (no digit was looked at: all rows share what there is)
-    bool sure = there && top > prefix, tie = there && top == prefix;
-    if (ishift < kEvIndexBits) {
-      const unsigned int at = from_top(k) >> ishift;
-      sure |= tie && at > iprefix;
-      tie &= at == iprefix;
-    }
-    const unsigned long long m = __builtin_amdgcn_ballot_w64(sure || (tie && !compare));
-    if (lane == 0) bits[j0 / 64 + k] = m;
-    if (compare) {
-      const unsigned long long tm = __builtin_amdgcn_ballot_w64(tie);
-      if (tm != 0ull) {
-        int at = 0;
-        if (lane == 0) at = atomicAdd(&found[0], __builtin_popcountll(tm));
-        at = __builtin_amdgcn_readfirstlane(at) + __builtin_popcountll(tm & ((1ull << lane) - 1ull));
-        if (tie) listed[at] = (unsigned long long)key << kEvIndexBits | from_top(k);
+  auto place_of = [&](unsigned int key, unsigned int from_top) __attribute__((always_inline)) {  // key, index from the top
+    return (unsigned long long)(key >> (32 - kEvIndexBits)) << 32 | (key << kEvIndexBits | from_top);
+  };
+  if (tid == 0) found[0] = 0;
+  __syncthreads();
+  each([&](int k, const bool (&there)[G], const unsigned int (&key)[G]) __attribute__((always_inline)) {
+    unsigned long long stay = 0ull, tied = 0ull;  // lane i: the bits of rows 64 (k + i) ..
+#pragma unroll
+    for (int i = 0; i < G; ++i) {
+      const unsigned int top = shift == 32 ? 0u : key[i] >> (shift & 31);  // (no digit was looked at: all rows share what there is)
+      bool sure = there[i] && top > prefix, tie = there[i] && top == prefix;
+      if (ishift < kEvIndexBits) {
+        const unsigned int at = from_top(k + i) >> ishift;
+        sure |= tie && at > iprefix;
+        tie &= at == iprefix;
       }
+      const unsigned long long m = __builtin_amdgcn_ballot_w64(sure), tm = __builtin_amdgcn_ballot_w64(tie);
+      stay = lane == i ? m : stay;
+      tied = lane == i ? tm : tied;
+      if constexpr (K > 0) {
+        if (compare && tm != 0ull) {
+          int at = 0;
+          if (lane == 0) at = atomicAdd(&found[0], __builtin_popcountll(tm));
+          at = __builtin_amdgcn_readfirstlane(at) + __builtin_popcountll(tm & ((1ull << lane) - 1ull));
+          if (tie) ties[at] = place_of(key[i], from_top(k + i));
+        }
+      }
+    }
+    if (lane < G && 64 * (k + lane) < rows) {
+      bits[j0 / 64 + k + lane] = compare ? stay : stay | tied;
+      if (K == 0 && compare) open[j0 / 64 + k + lane] = tied;
     }
   });
   __syncthreads();
-  if (compare) {  // among those that are listed now: the rest of the digits, then with each other
-    constexpr int kMine = K ? 1 : kEvListed / kEvThreads;
-    unsigned long long place[kMine];
-    const int entries = same;
-#pragma unroll
-    for (int i = 0; i < kMine; ++i) place[i] = tid + i * kEvThreads < entries ? listed[tid + i * kEvThreads] : 0ull;
-    int low = ishift < kEvIndexBits ? ishift : shift + kEvIndexBits;  // the bits below are still to be looked at
-    unsigned long long first = listed[0] >> low;
-    while (same > want && same > kEvTies) {  // (no two places are the same)
-      const int above = low, bits_of = low < 11 ? low : 11;
-      low -= bits_of;
-      const unsigned int d = digit([&](auto&& f) __attribute__((always_inline)) {
-#pragma unroll
-        for (int i = 0; i < kMine; ++i)
-          f(tid + i * kEvThreads < entries && place[i] >> above == first, (unsigned)(place[i] >> low) & ((1u << bits_of) - 1u));
-      });
-      first = first << bits_of | d;
-    }
-    auto stays = [&](unsigned long long at) __attribute__((always_inline)) {
-      const int j = (1 << kEvIndexBits) - 1 - (int)(at & ((1u << kEvIndexBits) - 1u));
+  if (compare) {
+    auto stays = [&](unsigned long long place) __attribute__((always_inline)) {
+      const int j = (1 << kEvIndexBits) - 1 - (int)(place & ((1u << kEvIndexBits) - 1u));
       atomicOr((unsigned int*)bits + j / 32, 1u << (j & 31));
     };
-    __syncthreads();
-    if (tid == 0) found[0] = 0;
-    __syncthreads();
+    if constexpr (K == 0) {  // more than can be compared: a list of them, and the rest of the digits
+      constexpr int kMine = kEvListed / kEvThreads, kWords = kEvMaxRows / 64 / kEvThreads;
+      unsigned long long tied[kWords];
 #pragma unroll
-    for (int i = 0; i < kMine; ++i) {
-      if (tid + i * kEvThreads >= entries) continue;
-      const unsigned long long top = place[i] >> low;
-      if (top > first || (top == first && same == want)) stays(place[i]);
-      else if (top == first) ties[atomicAdd(&found[0], 1)] = place[i];
+      for (int i = 0; i < kWords; ++i) tied[i] = tid + i * kEvThreads < words ? open[tid + i * kEvThreads] : 0ull;
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < kWords; ++i)
+        if (tied[i]) {
+          int at = atomicAdd(&found[0], __builtin_popcountll(tied[i]));
+          for (unsigned long long left = tied[i]; left; left &= left - 1ull) list[at++] = 64 * (tid + i * kEvThreads) + __builtin_ctzll(left);
+        }
+      __syncthreads();
+      unsigned long long place[kMine];
+      const int entries = same;
+#pragma unroll
+      for (int i = 0; i < kMine; ++i) {
+        place[i] = 0ull;
+        if (tid + i * kEvThreads < entries) {
+          const int j = list[tid + i * kEvThreads];
+          place[i] = place_of(evict_key(w[j], pos ? pos[j] : 0, sink, fresh), (unsigned)((1 << kEvIndexBits) - 1 - j));
+        }
+      }
+      int low = ishift < kEvIndexBits ? ishift : shift + kEvIndexBits;  // the bits below are still to be looked at
+      unsigned long long first = ishift < kEvIndexBits ? (unsigned long long)prefix << (kEvIndexBits - ishift) | iprefix : prefix;
+      while (same > want && same > kEvTies) {  // (no two places are the same)
+        const int above = low, bits_of = low < 11 ? low : 11;
+        low -= bits_of;
+        const unsigned int d = digit([&](auto&& f) __attribute__((always_inline)) {
+#pragma unroll
+          for (int i = 0; i < kMine; ++i)
+            f(tid + i * kEvThreads < entries && place[i] >> above == first, (unsigned)(place[i] >> low) & ((1u << bits_of) - 1u));
+        });
+        first = first << bits_of | d;
+      }
+      __syncthreads();
+      if (tid == 0) found[0] = 0;
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < kMine; ++i) {
+        if (tid + i * kEvThreads >= entries) continue;
+        const unsigned long long top = place[i] >> low;
+        if (top > first || (top == first && same == want)) stays(place[i]);
+        else if (top == first) ties[atomicAdd(&found[0], 1)] = place[i];
+      }
+      __syncthreads();
     }
-    __syncthreads();
-    if (same > want && tid < same) {
-      const unsigned long long at = ties[tid];
+    if (same > want && wave < same) {  // `want` of these: wavefront v counts those before number v, v + 16 .., 64 at a time
+      unsigned long long all[kEvTies / 64];
+#pragma unroll
+      for (int i = 0; i < kEvTies / 64; ++i) all[i] = 64 * i + lane < same ? ties[64 * i + lane] : 0ull;
+      const int own = wave + lane * kEvWaves;
+      const unsigned long long place = own < same ? ties[own] : 0ull;
       int rank = 0;
-      for (int i = 0; i < same; ++i) rank += ties[i] > at ? 1 : 0;
-      if (rank < want) stays(at);
+      for (int i = 0; wave + i * kEvWaves < same; ++i) {
+        const unsigned long long at = (unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)(place >> 32), i) << 32 |
+                                      (unsigned)__builtin_amdgcn_readlane((int)place, i);
+        int before = 0;
+#pragma unroll
+        for (int v = 0; v < kEvTies / 64; ++v)
+          if (64 * v < same) before += __builtin_popcountll(__builtin_amdgcn_ballot_w64(all[v] > at));
+        rank = lane == i ? before : rank;
+      }
+      if (own < same && rank < want) stays(place);
     }
     __syncthreads();
   }
@@ -313,12 +398,12 @@ __global__ __launch_bounds__(kEvThreads) void kv_evict_select_kernel(KvEvictPara
   const int nword = n / 64;  // words from here on may have moving rows; their counts begin behind `total` free places
   for (int from = 0; from == 0 || from < total; from += kEvList) {
     if (from) __syncthreads();
-    for (int x = nword + wave; x < words; x += kEvWaves) {
+    for (int y = nword * 8 + tid; y < words * 8; y += kEvThreads) {  // eight rows
+      const int x = y / 8, at = y % 8 * 8;
       const unsigned long long m = moving_of(x);
-      if ((m >> lane) & 1ull) {
-        const int rank = count[x] + (x == nword ? __builtin_popcountll(free_of(x)) : 0) - total + __builtin_popcountll(m & ((1ull << lane) - 1ull)) - from;
-        if (rank >= 0 && rank < kEvList) list[rank] = 64 * x + lane;
-      }
+      int rank = count[x] + (x == nword ? __builtin_popcountll(free_of(x)) : 0) - total + __builtin_popcountll(m & ((1ull << at) - 1ull)) - from;
+      for (unsigned int left = (unsigned)(m >> at) & 255u; left; left &= left - 1u, ++rank)
+        if (rank >= 0 && rank < kEvList) list[rank] = 64 * x + at + __builtin_ctz(left);
     }
     __syncthreads();
     for (int j = tid; j < n; j += kEvThreads) {
@@ -380,7 +465,14 @@ static hipError_t with_select(int kv_cap, F&& f) {
 }
 
 hipError_t prepare_kv_evict() {
-  return hipFuncSetAttribute((const void*)kv_evict_select_kernel<0>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)evict_lds_bytes(kEvMaxRows));
+  hipError_t e = hipSuccess;
+  for (int cap : {4 * kEvThreads, 16 * kEvThreads, kEvMaxRows}) {
+    if (e != hipSuccess) break;
+    e = with_select(cap, [&](auto kernel) {
+      return hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)evict_lds_bytes(cap));
+    });
+  }
+  return e;
 }
 
 }  // namespace ctcspec
