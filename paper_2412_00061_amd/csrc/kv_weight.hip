@@ -25,7 +25,7 @@ struct KvWeightParams {
   int32_t* pos;                  // [B][H_kv][kv_cap] or null
   const int32_t* next_pos;       // [B] or null
   int T, kv_cap, H, H_kv, group, dh, max_nodes, tiles;
-  float sl2;                     // scale * log2(e)
+  float scale;
 };
 
 constexpr int kKwMaxRows = 9 * 256;  // rows of a group: (T + 1) heads
@@ -73,7 +73,7 @@ __global__ __launch_bounds__(256, 2) void kv_weight_kernel(KvWeightParams p) {
   u32x4 kf[2][QS];
   if (!fresh) load_keys(key0, kf);  // (first of all: nothing else is as far away)
 
-  // ---- the rows: row r is head r % group of path entry r / group; its lse in the log2 domain (infinite: counts for nothing) and
+  // ---- the rows: row r is head r % group of path entry r / group; its lse (infinite: counts for nothing) and
   // where its query begins -------------------------------------------------------------------------------------------------------
   int len = __builtin_amdgcn_readfirstlane(p.accept_len[b]);
   len = len < 0 ? 0 : (len > p.T ? p.T : len);
@@ -90,7 +90,7 @@ __global__ __launch_bounds__(256, 2) void kv_weight_kernel(KvWeightParams p) {
       if (node >= 0 && node < p.max_nodes) {
         at = (r - i * p.group) * p.max_nodes + node;
         const float s = p.lse[head0 * p.max_nodes + at];
-        v = s == -INFINITY ? INFINITY : s * 1.4426950408889634f;
+        v = s == -INFINITY ? INFINITY : s;
       }
     }
     row_lse[r] = v;
@@ -125,7 +125,8 @@ __global__ __launch_bounds__(256, 2) void kv_weight_kernel(KvWeightParams p) {
     float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float w = __builtin_amdgcn_exp2f(fmaf(s[i], p.sl2, -lse[i]));
+      // (the difference first, rounded once: score and lse are large against it, and so are their roundings)
+      const float w = __builtin_amdgcn_exp2f(fmaf(s[i], p.scale, -lse[i]) * 1.4426950408889634f);
       // (a row that counts for nothing: its score may be anything)
       sum += lse[i] == INFINITY || row0 + 4 * g + i < from ? 0.f : w;
     }
@@ -240,7 +241,7 @@ extern "C" int kv_weight_update(ctcspec_ctx* ctx, ctcspec_dtype dt, const void* 
   p.k_tree = (const unsigned char*)k_tree; p.accept_len = accept_len; p.accept_nodes = accept_nodes;
   p.weight = weight; p.pos = pos; p.next_pos = next_pos;
   p.T = T; p.kv_cap = kv_cap; p.H = H; p.H_kv = H_kv; p.group = H / H_kv; p.dh = dh; p.max_nodes = max_nodes;
-  p.sl2 = scale * 1.4426950408889634f;
+  p.scale = scale;
   p.tiles = weight_tiles((long long)B * H_kv * ((kv_cap + 31LL) / 32));
   const int blocks = ((T + 1) * p.group + 15) / 16;
   const dim3 grid((unsigned)(((long long)kv_cap + 128 * p.tiles - 1) / (128 * p.tiles)) + 1, (unsigned)H_kv, (unsigned)B);
