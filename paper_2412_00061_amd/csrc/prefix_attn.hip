@@ -66,11 +66,13 @@ struct Work {
   int punits, pitems, units;  // units and blocks of the prefix over all key heads; all units
 };
 // units of a block of rows
-__device__ __forceinline__ int own_units(int iters) { return kPrefixBlockUnits + iters * kPrefixOwnWeight; }
-template <int R>
-__device__ __forceinline__ int prefix_units(int iters) { return kPrefixBlockUnits + iters * prefix_shared_weight(R); }
-template <int R, int TPI>
+template <typename SH>
+__device__ __forceinline__ int own_units(int iters) { return prefix_block_units(SH::F32) + iters * kPrefixOwnWeight; }
+template <typename SH>
+__device__ __forceinline__ int prefix_units(int iters) { return prefix_block_units(SH::F32) + iters * prefix_shared_weight(SH::R); }
+template <typename SH>
 __device__ __forceinline__ Work read_work(const PrefixAttnParams& p) {
+  constexpr int R = SH::R, TPI = SH::TPI;
   const int lane = threadIdx.x & 63;
   Work t{};
   const int P = *p.prefix_len;
@@ -82,7 +84,7 @@ __device__ __forceinline__ Work read_work(const PrefixAttnParams& p) {
   }
   t.blocks = (t.n * p.group + R - 1) / R;
   t.iters = t.n ? ((t.ctx + 31) / 32 + (t.n + 31) / 32 + TPI - 1) / TPI : 0;
-  const int mine = t.blocks * own_units(t.iters);
+  const int mine = t.blocks * own_units<SH>(t.iters);
   int n = t.n, b = t.blocks, u = mine;
   for (int d = 1; d < p.B; d *= 2) {
     const int nb = __shfl_up(n, d, 64), bb = __shfl_up(b, d, 64), ub = __shfl_up(u, d, 64);
@@ -98,7 +100,7 @@ __device__ __forceinline__ Work read_work(const PrefixAttnParams& p) {
   t.piters = ((t.prefix + 31) / 32 + TPI - 1) / TPI;
   t.pblocks = uniform((t.all * p.group + R - 1) / R);
   t.pitems = t.piters ? p.H_kv * t.pblocks : 0;
-  t.punits = t.pitems * prefix_units<R>(t.piters);
+  t.punits = t.pitems * prefix_units<SH>(t.piters);
   t.units = t.punits + p.H_kv * t.head_units;
   return t;
 }
@@ -155,7 +157,7 @@ __global__ __launch_bounds__(64 * SH::NW, SH::WPE) void prefix_attn_kernel(Prefi
   const int c = lane & 31, h2 = lane >> 5;
   const int rb = p.dh * SH::ES;  // bytes of a row
 
-  const Work t = read_work<R, TPI>(p);
+  const Work t = read_work<SH>(p);
   const Deal d = prefix_deal(t.units, SH::GROUPS);
   // Workgroups go to the 8 XCDs in turn, each with an L2 of its own: consecutive shares - the row blocks of a key head, which
   // read the same keys - go to the same one.
@@ -214,7 +216,7 @@ __global__ __launch_bounds__(64 * SH::NW, SH::WPE) void prefix_attn_kernel(Prefi
       const int in_head = rel - kh * head_units;
       // (sequences without nodes have no units: the last sequence that starts at or before the unit and has some)
       b = 63 - __builtin_clzll(__builtin_amdgcn_ballot_w64(table[kIters][seg_lane] > 0 && table[kUnit0][seg_lane] <= in_head));
-      units = own_units(of(kIters, b));
+      units = own_units<SH>(of(kIters, b));
       weight = kPrefixOwnWeight;
       const int in_seq = in_head - of(kUnit0, b);
       blk = uniform(in_seq / units);
@@ -228,7 +230,7 @@ __global__ __launch_bounds__(64 * SH::NW, SH::WPE) void prefix_attn_kernel(Prefi
       kc = p.k_cache + at; vc = p.v_cache + at;
       kt = p.k_tree + ta; vt = p.v_tree + ta;
     } else {
-      units = prefix_units<R>(piters);
+      units = prefix_units<SH>(piters);
       weight = prefix_shared_weight(R);
       const int item = uniform(u / units);
       at_unit = u - item * units;
@@ -245,7 +247,7 @@ __global__ __launch_bounds__(64 * SH::NW, SH::WPE) void prefix_attn_kernel(Prefi
     u += share;
     // the iterations that begin in the share
     auto iterations = [&](int units) __attribute__((always_inline)) {
-      const int x = units - kPrefixBlockUnits;
+      const int x = units - prefix_block_units(SH::F32);
       return uniform(x > 0 ? (x + weight - 1) / weight : 0);
     };
     const int it0 = iterations(at_unit), niter = iterations(at_unit + share) - it0;
@@ -419,38 +421,56 @@ __global__ __launch_bounds__(64 * SH::NW, SH::WPE) void prefix_attn_kernel(Prefi
       // A value that is no number or infinite must not reach the rows that do not see its key, and 0 times it is no number: in a
       // tile of tree nodes such values take part as 0, and the join adds them where they are seen.
       if constexpr (SH::F32) {
+        constexpr int kGroups = 2 * DT;  // of eight values, read one group ahead
+        float x[2][8];
+        auto read_values = [&](int g) __attribute__((always_inline)) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[g % 2][i] = lds_read<float>((va ^ (g / 2 << 7)) + (16 * (g % 2) + 8 * (i / 4) + i % 4) * ROWB);
+        };
 #pragma unroll
         for (int i = 0; i < QU; ++i) {
+          __builtin_amdgcn_sched_barrier(0);
           score(i, sn);
           if (i + kAhead < QU) a[i % kAhead] = lds_read<u32x4>(ka ^ ((i + kAhead) << 5));
+          if (i == QU - 1) read_values(0);
+#pragma unroll
+          for (int j = i * 16 / QU; j < (i + 1) * 16 / QU; ++j)
+#pragma unroll
+            for (int qt = 0; qt < QT; ++qt) {
+              s[qt][j] = __builtin_amdgcn_exp2f(fmaf(s[qt][j], p.sl2, -ms[qt]));
+              sum[qt] += s[qt][j];
+              asm volatile("" : "+v"(sum[qt]));  // (here, not at the end of the tile)
+            }
         }
 #pragma unroll
-        for (int qt = 0; qt < QT; ++qt)
+        for (int g = 0; g < kGroups; ++g) {
+          __builtin_amdgcn_sched_barrier(0);
+          if (g + 1 < kGroups) read_values(g + 1);
+          if (tree) {
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            s[qt][i] = __builtin_amdgcn_exp2f(fmaf(s[qt][i], p.sl2, -ms[qt]));
-            sum[qt] += s[qt][i];
-          }
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            float x = lds_read<float>((va ^ (dt << 7)) + (8 * (i / 4) + i % 4) * ROWB);
-            if (tree) {
-              const bool bad = (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u;
+            for (int i = 0; i < 8; ++i) {
+              const bool bad = (__float_as_uint(x[g % 2][i]) & 0x7f800000u) == 0x7f800000u;
               odd |= bad;
-              x = bad ? 0.f : x;
+              x[g % 2][i] = bad ? 0.f : x[g % 2][i];
             }
-#pragma unroll
-            for (int qt = 0; qt < QT; ++qt) o[qt][dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, s[qt][i], o[qt][dt], 0, 0, 0);
           }
-        read_next();
-        hide(k1, any1, sn, mw0, mw1);
 #pragma unroll
-        for (int qt = 0; qt < QT; ++qt) {
-          mx[qt] = sn[qt][0];
+          for (int i = 0; i < 8; ++i)
 #pragma unroll
-          for (int i = 1; i < 16; ++i) mx[qt] = fmaxf(mx[qt], sn[qt][i]);
+            for (int qt = 0; qt < QT; ++qt)
+              o[qt][g / 2] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[g % 2][i], s[qt][8 * (g % 2) + i], o[qt][g / 2], 0, 0, 0);
+          if (g == 0) {
+            __builtin_amdgcn_sched_barrier(0);
+            read_next();
+            hide(k1, any1, sn, mw0, mw1);
+          } else {
+#pragma unroll
+            for (int qt = 0; qt < QT; ++qt) {
+#pragma unroll
+              for (int i = (g - 1) * 16 / (kGroups - 1); i < g * 16 / (kGroups - 1); ++i) mx[qt] = i == 0 ? sn[qt][0] : fmaxf(mx[qt], sn[qt][i]);
+              asm volatile("" : "+v"(mx[qt]));
+            }
+          }
         }
       } else {
         u32x4 hi[QT][2], lo[QT][2];
@@ -683,7 +703,7 @@ __global__ __launch_bounds__(2 * SH::DHP) void prefix_join_kernel(PrefixJoinPara
   constexpr int DT = SH::DT, R = SH::R;
   const int lane = threadIdx.x & 63, dt = threadIdx.x >> 6, c = lane & 31, h2 = lane >> 5;
   const int kh = blockIdx.y, b = blockIdx.z, r = blockIdx.x * 32 + c;
-  const Work t = read_work<R, SH::TPI>(p.a);
+  const Work t = read_work<SH>(p.a);
   const int n = __builtin_amdgcn_readlane(t.n, b);
   if ((int)blockIdx.x * 32 >= n * p.a.group) return;
   const bool live = r < n * p.a.group;
@@ -730,12 +750,12 @@ __global__ __launch_bounds__(2 * SH::DHP) void prefix_join_kernel(PrefixJoinPara
   };
   if (t.piters > 0) {
     const int item = kh * t.pblocks + rp / R;
-    const int first = item * prefix_units<R>(t.piters) + kPrefixBlockUnits;
+    const int first = item * prefix_units<SH>(t.piters) + prefix_block_units(SH::F32);
     gather(item, d.owner(first), d.owner(first + (t.piters - 1) * prefix_shared_weight(R)), rp);
   }
   const int oi = __builtin_amdgcn_readlane(t.iters, b), blk = rr / R;
   const int ou = t.punits + kh * t.head_units + __builtin_amdgcn_readlane(t.unit0, b) +
-                 blk * own_units(oi) + kPrefixBlockUnits;
+                 blk * own_units<SH>(oi) + prefix_block_units(SH::F32);
   const int oitem = t.pitems + kh * t.head_blocks + __builtin_amdgcn_readlane(t.block0, b) + blk;
   const int x0 = d.owner(ou), x1 = d.owner(ou + (oi - 1) * kPrefixOwnWeight);
   gather(oitem, x0, x1, rr);

@@ -27,8 +27,11 @@ inline int prefix_block_rows(long long rows, bool f32) {
 // 64 keys against the sequence's rows: the keys' way in), and a block of rows besides its iterations (the rows' way in, the
 // first keys' way, what it leaves).  8 sequences x 64 nodes behind 2048 keys with 256 to 2048 of their own, us for 2 : 2 / 3 : 2 /
 // 4 : 2 with 256 rows 98 / 82 / 84; 256 short blocks of their own behind 32768 keys take 855 us if a block costs nothing, 312 with 8.
+// A float iteration is 32 keys or 64, bound by its products, and costs more: 4 sequences x 100 nodes, 12 heads, behind 1500 keys, us with
+// 8 / 4 / 3 units a block: 46.5 / 45.1 / 45.6, twice as wide heads 78.5 / 75.9 / 75.7.
 CTCSPEC_BOTH constexpr int prefix_shared_weight(int rows) { return rows == 256 ? 3 : 2; }
-constexpr int kPrefixOwnWeight = 2, kPrefixBlockUnits = 8;
+constexpr int kPrefixOwnWeight = 2;
+CTCSPEC_BOTH constexpr int prefix_block_units(bool f32) { return f32 ? 4 : 8; }
 
 // The work is units in a row - iterations over the keys, for block of rows after block of rows -, and workgroup w has
 // those from begin(w) to begin(w + 1).  Where its share crosses into another block, it leaves a partial result for each; that
@@ -55,8 +58,8 @@ CTCSPEC_BOTH Deal prefix_deal(int units, int groups) {
 }
 // units are counted in 32 bits: whether that is enough for the largest lengths
 inline bool prefix_units_fit(long long B, int H_kv, long long seq_rows, int prefix_cap, int kv_cap, int max_nodes) {
-  const double own = (double)B * ((seq_rows + 31) / 32) * (kPrefixOwnWeight * ((kv_cap + 31LL) / 32 + max_nodes / 32 + 1) + kPrefixBlockUnits);
-  const double prefix = (double)((B * seq_rows + 31) / 32) * (3 * ((prefix_cap + 31LL) / 32) + kPrefixBlockUnits);
+  const double own = (double)B * ((seq_rows + 31) / 32) * (kPrefixOwnWeight * ((kv_cap + 31LL) / 32 + max_nodes / 32 + 1) + prefix_block_units(false));
+  const double prefix = (double)((B * seq_rows + 31) / 32) * (3 * ((prefix_cap + 31LL) / 32) + prefix_block_units(false));
   return (own + prefix) * H_kv < 2147483647.0;
 }
 
