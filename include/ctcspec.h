@@ -471,7 +471,7 @@ int ctc_loss(ctcspec_ctx* ctx, const float* logits, const int32_t* labels, const
  * k_cache, v_cache, kv_off, ctx_len, kv_cap   as for tree_verify_attn, with [H_kv][kv_cap][dh] per sequence
  * k_tree, v_tree [B,H_kv,max_nodes,dh]
  * n_nodes, anc_mask   as for tree_verify_attn
- * scale         positive and finite
+ * scale         positive, at most 2e38
  * workspace     device scratch of at least prefix_verify_attn_workspace_bytes(B, H, H_kv, dh, max_nodes) bytes, owned by the
  *               caller, contents undefined afterwards; calls that share it must not overlap.  Bytes for some B and max_nodes
  *               serve every smaller B and max_nodes
@@ -479,8 +479,8 @@ int ctc_loss(ctcspec_ctx* ctx, const float* logits, const int32_t* labels, const
  *               bf16 operands (weights rounded to bf16 as well: a third less work)
  * lse           [B,H,max_nodes] float out or NULL: what kv_weight_update takes
  * Pointers 16-byte aligned (prefix_len, ctx_len, n_nodes, kv_off, anc_mask and lse as their types are).
- * Limits: dh % 8 == 0, dh <= CTCSPEC_MAX_HEAD_DIM, max_nodes <= CTCSPEC_MAX_NODES; B, H, dh, max_nodes within the context's
- * limits; H % H_kv == 0.  The same bits on every run.
+ * Limits: dh % 8 == 0, dh <= CTCSPEC_MAX_HEAD_DIM, max_nodes <= CTCSPEC_MAX_NODES, B <= 64; B, H, dh, max_nodes within the
+ * context's limits; H % H_kv == 0; kv_cap, prefix_cap and B * max_nodes * H / H_kv <= 2^30.  The same bits on every run.
  */
 size_t prefix_verify_attn_workspace_bytes(int B, int H, int H_kv, int dh, int max_nodes);
 
@@ -512,7 +512,8 @@ int prefix_verify_attn(ctcspec_ctx* ctx, ctcspec_dtype dt, const void* q, const 
  * weight        [B,H_kv,kv_cap] float, in and out
  * pos           [B,H_kv,kv_cap] int32, in and out, or NULL: the position of every cached row in its sequence
  * next_pos      [B] int32 in: the position of the root; NULL only without pos
- * Limits: as for prefix_verify_attn, T <= CTCSPEC_MAX_SLOTS, (T + 1) * H / H_kv <= 2304.  The same bits on every run.
+ * Limits: dh, max_nodes, H, H_kv as for prefix_verify_attn, kv_cap <= 2^30, T <= CTCSPEC_MAX_SLOTS, (T + 1) * H / H_kv <= 2304;
+ * B within the context's limits.  The same bits on every run.
  */
 int kv_weight_update(ctcspec_ctx* ctx, ctcspec_dtype dt, const void* q, const float* lse, const void* k_cache,
                      const int64_t* kv_off, const int32_t* ctx_len, int kv_cap, const void* k_tree,
@@ -522,7 +523,8 @@ int kv_weight_update(ctcspec_ctx* ctx, ctcspec_dtype dt, const void* q, const fl
 /*
  * kv_evict - a layer's cache brought down to `budget` rows per sequence and key head.  Sequences with ctx_len[b] <= budget keep
  * everything.  Of the others every key head keeps, with n = budget:
- *   the rows with pos < sink (the first positions of the sequence) and those with pos >= next_pos[b] - recent (its last ones),
+ *   the rows with pos < sink (the first positions of the sequence) and, with recent > 0, those with
+ *   pos >= next_pos[b] - recent (its last ones),
  *   then those with the largest weight - equal weights: the smaller index; a weight that is not a number: behind all others.
  * (Should positions occur more than once, so that more than n rows are among the first kind, the n of smallest index stay.)
  * Kept rows with an index below n stay where they are; those from n on move, in ascending order, into the places that became
@@ -540,7 +542,7 @@ int kv_weight_update(ctcspec_ctx* ctx, ctcspec_dtype dt, const void* q, const fl
  * sink, recent  >= 0, together <= budget; either needs pos and pos_out, recent needs next_pos
  * kept          [B,H_kv,budget] int32 out
  * weight_out, pos_out, ctx_len_out   out, other buffers than the inputs
- * Limits: kv_cap <= 524288, dh % 8 == 0, dh <= CTCSPEC_MAX_HEAD_DIM, B, H_kv, dh within the context's limits.  The same bits
+ * Limits: kv_cap <= 524288, budget <= 2^30, dh % 8 == 0, dh <= CTCSPEC_MAX_HEAD_DIM, B, H_kv, dh within the context's limits.  The same bits
  * on every run.
  */
 int kv_evict(ctcspec_ctx* ctx, ctcspec_dtype dt, void* k_cache, void* v_cache, const int64_t* kv_off,

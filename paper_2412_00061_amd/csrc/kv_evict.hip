@@ -44,11 +44,11 @@ static_assert(kEvListed <= kEvList && kEvTies * 8 <= kEvBinBytes && kEvListed % 
 constexpr size_t evict_lds_bytes(int kv_cap) { return kEvListBytes + (size_t)((kv_cap + 63) / 64) * 8; }
 
 // Order of the rows: larger weight first, then smaller index; rows that stay in any case before all others; a weight that is not
-// a number behind all others.  (fresh: positions from there on stay.)
-__device__ __forceinline__ unsigned int evict_key(float weight, int pos, int sink, int fresh) {
+// a number behind all others.  (last: positions behind it stay.)
+__device__ __forceinline__ unsigned int evict_key(float weight, int pos, int sink, int last) {
   const unsigned int u = __float_as_uint(weight + 0.0f);  // (-0 becomes 0)
   const unsigned int key = weight != weight ? 0u : u ^ ((unsigned)((int)u >> 31) | 0x80000000u);
-  return pos < sink || pos >= fresh ? 0xffffffffu : key;
+  return pos < sink || pos > last ? 0xffffffffu : key;
 }
 
 // The order is that of the key, then of the index from the top - no two rows have the same place -, searched digit by digit for
@@ -89,7 +89,12 @@ __global__ __launch_bounds__(kEvThreads) void kv_evict_select_kernel(KvEvictPara
 
   const float* w = p.weight + head * p.kv_cap;
   const int32_t* pos = p.pos ? p.pos + head * p.kv_cap : nullptr;
-  const int sink = pos ? p.sink : -0x7fffffff - 1, fresh = p.recent > 0 ? p.next_pos[b] - p.recent : 0x7fffffff;
+  int sink = -0x7fffffff - 1, last = 0x7fffffff;  // (without pos, and without recent: no position is before the one or behind the other)
+  if (pos) sink = p.sink;
+  if (p.recent > 0) {
+    const long long before = (long long)p.next_pos[b] - p.recent - 1;
+    last = before < -0x7fffffffLL - 1 ? -0x7fffffff - 1 : (int)before;
+  }
   const int range = (words + kEvWaves - 1) / kEvWaves * 64, j0 = wave * range;  // this wavefront's rows
   const int rows = j0 < L ? (L - j0 < range ? L - j0 : range) : 0;
   // weights and positions of rows j0 + 64 (k0 + i) + lane, i < N (behind the last row: the last one again), and their keys
@@ -120,7 +125,7 @@ __global__ __launch_bounds__(kEvThreads) void kv_evict_select_kernel(KvEvictPara
       int at[N];
       load(k, v, at);
 #pragma unroll
-      for (int i = 0; i < N; ++i) mine[k + i] = evict_key(v[i], at[i], sink, fresh);
+      for (int i = 0; i < N; ++i) mine[k + i] = evict_key(v[i], at[i], sink, last);
 #pragma unroll
       for (int i = 0; i < N; ++i) asm volatile("" : "+v"(mine[k + i]));
     }
@@ -157,7 +162,7 @@ __global__ __launch_bounds__(kEvThreads) void kv_evict_select_kernel(KvEvictPara
       for (int k = 0; 64 * k < rows; k += G) {
         load(k + G, next_v, next_at);
 #pragma unroll
-        for (int i = 0; i < G; ++i) key[i] = evict_key(v[i], at[i], sink, fresh);
+        for (int i = 0; i < G; ++i) key[i] = evict_key(v[i], at[i], sink, last);
         some(k, key, f);
 #pragma unroll
         for (int i = 0; i < G; ++i) {
@@ -310,7 +315,7 @@ __global__ __launch_bounds__(kEvThreads) void kv_evict_select_kernel(KvEvictPara
         place[i] = 0ull;
         if (tid + i * kEvThreads < entries) {
           const int j = list[tid + i * kEvThreads];
-          place[i] = place_of(evict_key(w[j], pos ? pos[j] : 0, sink, fresh), (unsigned)((1 << kEvIndexBits) - 1 - j));
+          place[i] = place_of(evict_key(w[j], pos ? pos[j] : 0, sink, last), (unsigned)((1 << kEvIndexBits) - 1 - j));
         }
       }
       int low = ishift < kEvIndexBits ? ishift : shift + kEvIndexBits;  // the bits below are still to be looked at
@@ -496,8 +501,8 @@ extern "C" int kv_evict(ctcspec_ctx* ctx, ctcspec_dtype dt, void* k_cache, void*
   CTCSPEC_REQUIRE(ctx, weight_out != weight && (!pos || pos_out != pos) && ctx_len_out != ctx_len, CTCSPEC_EINVAL,
                   "kv_evict: weight_out, pos_out and ctx_len_out must not be the inputs");
   CTCSPEC_REQUIRE(ctx, dh % 8 == 0 && dh <= CTCSPEC_MAX_HEAD_DIM && B <= ctx->lim.max_batch && H_kv <= ctx->lim.max_heads &&
-                           dh <= ctx->lim.max_head_dim && B <= 65535 && H_kv <= 65535 && kv_cap <= kEvMaxRows,
-                  CTCSPEC_EUNSUPPORTED, "kv_evict: dh must be a multiple of 8 and <= %d, kv_cap <= %d, the shape within the context's limits",
+                           dh <= ctx->lim.max_head_dim && B <= 65535 && H_kv <= 65535 && kv_cap <= kEvMaxRows && budget <= (1 << 30),
+                  CTCSPEC_EUNSUPPORTED, "kv_evict: dh must be a multiple of 8 and <= %d, kv_cap <= %d, budget <= 2^30, the shape within the context's limits",
                   CTCSPEC_MAX_HEAD_DIM, kEvMaxRows);
   CTCSPEC_REQUIRE(ctx, aligned16(k_cache) && aligned16(v_cache), CTCSPEC_EINVAL, "kv_evict: the caches must be 16-byte aligned");
   KvEvictParams p;

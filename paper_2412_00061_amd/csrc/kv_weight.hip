@@ -234,6 +234,7 @@ extern "C" int kv_weight_update(ctcspec_ctx* ctx, ctcspec_dtype dt, const void* 
   CTCSPEC_REQUIRE(ctx, B <= ctx->lim.max_batch && B <= 65535 && max_nodes <= ctx->lim.max_nodes && H <= ctx->lim.max_heads &&
                            dh <= ctx->lim.max_head_dim,
                   CTCSPEC_EUNSUPPORTED, "kv_weight_update: shape exceeds the context's limits");
+  CTCSPEC_REQUIRE(ctx, kv_cap <= (1 << 30), CTCSPEC_EUNSUPPORTED, "kv_weight_update: kv_cap must be <= 2^30");
   for (const void* a : {q, k_cache, k_tree})
     CTCSPEC_REQUIRE(ctx, aligned16(a), CTCSPEC_EINVAL, "kv_weight_update: q, k_cache and k_tree must be 16-byte aligned");
   KvWeightParams p;

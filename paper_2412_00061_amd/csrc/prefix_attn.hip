@@ -480,7 +480,7 @@ __global__ __launch_bounds__(64 * SH::NW, SH::WPE) void prefix_attn_kernel(Prefi
           for (int j = from; j < to; ++j)
 #pragma unroll
             for (int qt = 0; qt < QT; ++qt) {
-              // P is rounded to bf16, as the values are and as the result will be; FINE: P = hi + lo, within 2^-17 of it
+              // P is rounded to bf16, as the values are and as the result will be; FINE: P = hi + lo, within 2^-16 of it
               const float p0 = __builtin_amdgcn_exp2f(fmaf(s[qt][2 * j], p.sl2, -ms[qt]));
               const float p1 = __builtin_amdgcn_exp2f(fmaf(s[qt][2 * j + 1], p.sl2, -ms[qt]));
               const unsigned int h = __builtin_bit_cast(unsigned int, bf16x2{(__bf16)p0, (__bf16)p1});
@@ -878,14 +878,14 @@ extern "C" int prefix_verify_attn(ctcspec_ctx* ctx, ctcspec_dtype dt, const void
   CTCSPEC_REQUIRE(ctx, dt == CTCSPEC_F32 || dt == CTCSPEC_BF16, CTCSPEC_EINVAL, "prefix_verify_attn: unknown element type");
   CTCSPEC_REQUIRE(ctx, out_dt == CTCSPEC_F32 || (out_dt == CTCSPEC_BF16 && dt == CTCSPEC_BF16), CTCSPEC_EINVAL,
                   "prefix_verify_attn: the output is float, or bf16 with bf16 operands");
-  CTCSPEC_REQUIRE(ctx, scale > 0.f && scale <= 3.0e38f, CTCSPEC_EINVAL, "prefix_verify_attn: the scale must be positive and finite");
+  CTCSPEC_REQUIRE(ctx, scale > 0.f && scale <= 2.0e38f, CTCSPEC_EINVAL, "prefix_verify_attn: the scale must be positive and at most 2e38");
   CTCSPEC_REQUIRE(ctx, dh % 8 == 0 && dh <= CTCSPEC_MAX_HEAD_DIM && max_nodes <= CTCSPEC_MAX_NODES, CTCSPEC_EUNSUPPORTED,
                   "prefix_verify_attn: dh must be a multiple of 8 and <= %d, max_nodes <= %d", CTCSPEC_MAX_HEAD_DIM, CTCSPEC_MAX_NODES);
   CTCSPEC_REQUIRE(ctx, B <= ctx->lim.max_batch && B <= 64 && max_nodes <= ctx->lim.max_nodes && H <= ctx->lim.max_heads &&
                            dh <= ctx->lim.max_head_dim && H_kv <= 65535,
                   CTCSPEC_EUNSUPPORTED, "prefix_verify_attn: shape exceeds the context's limits");
   CTCSPEC_REQUIRE(ctx, prefix_units_fit(B, H_kv, (long long)max_nodes * (H / H_kv), prefix_cap, kv_cap, max_nodes),
-                  CTCSPEC_EUNSUPPORTED, "prefix_verify_attn: capacities of this size need more than 32 bits for the work's units");
+                  CTCSPEC_EUNSUPPORTED, "prefix_verify_attn: capacities or rows beyond 2^30, or work of more than 2^31 units");
   for (const void* a : {q, k_prefix, v_prefix, k_cache, v_cache, k_tree, v_tree, (const void*)workspace, (const void*)out})
     CTCSPEC_REQUIRE(ctx, aligned16(a), CTCSPEC_EINVAL, "prefix_verify_attn: pointers must be 16-byte aligned");
   const bool f32 = dt == CTCSPEC_F32, fine = out_dt == CTCSPEC_F32;

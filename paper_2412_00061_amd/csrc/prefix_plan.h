@@ -56,11 +56,11 @@ CTCSPEC_BOTH Deal prefix_deal(int units, int groups) {
   d.more = units - d.each * d.groups;
   return d;
 }
-// units are counted in 32 bits: whether that is enough for the largest lengths
+// rows, keys and units are counted in 32 bits: whether that is enough for the largest lengths
 inline bool prefix_units_fit(long long B, int H_kv, long long seq_rows, int prefix_cap, int kv_cap, int max_nodes) {
   const double own = (double)B * ((seq_rows + 31) / 32) * (kPrefixOwnWeight * ((kv_cap + 31LL) / 32 + max_nodes / 32 + 1) + prefix_block_units(false));
   const double prefix = (double)((B * seq_rows + 31) / 32) * (3 * ((prefix_cap + 31LL) / 32) + prefix_block_units(false));
-  return (own + prefix) * H_kv < 2147483647.0;
+  return (own + prefix) * H_kv < 2147483647.0 && B * seq_rows <= 1LL << 30 && prefix_cap <= 1 << 30 && kv_cap <= 1 << 30;
 }
 
 inline int prefix_padded_dim(int dh) { return dh <= 64 ? 64 : 128; }

@@ -92,6 +92,37 @@ def test_ties_and_weights_of_every_kind(weights, L, budget):
     check(c)
 
 
+@pytest.mark.parametrize("weights", ["equal", "few", "signed", "odd", "decades"])
+@pytest.mark.parametrize("L,budget", [(9000, 5000), (16384, 300), (17000, 9000), (70001, 1001)])
+def test_ties_in_long_histories(weights, L, budget):
+    """Thousands of rows with one weight: the search goes on in their indexes."""
+    c = make(L, 1, 2, 8, L, [L], budget, 0, 0, "bf16", weights)
+    check(c)
+    c.update(sink=min(30, budget // 2), recent=budget // 3)
+    check(c)
+
+
+@pytest.mark.parametrize("spread", [1e-7, 1e-4, 1e-2])
+def test_weights_that_share_their_leading_digits(spread):
+    """Thousands of different weights next to each other."""
+    c = make(7, 1, 2, 8, 30000, [30000], 12345, 0, 0, "bf16")
+    c["weight"] = (1.5 + spread * np.random.default_rng(3).random(c["weight"].shape)).astype(np.float32)
+    check(c)
+
+
+def test_positions_at_the_ends_of_their_range():
+    """Without recent rows no position is too high, and a sequence shorter than `recent` keeps what it holds."""
+    top = 2 ** 31 - 1
+    c = make(6, 1, 1, 8, 200, [200], 20, 3, 0, "f32")
+    c["pos"][0, 0, 100:] = top
+    check(c)
+    c.update(sink=0, recent=20, next=np.array([top], dtype=np.int32))
+    check(c)
+    c["next"] = np.array([-(2 ** 31) + 4], dtype=np.int32)
+    c["pos"][0, 0, ::3] = -(2 ** 31) + 1
+    check(c)
+
+
 def test_positions_that_occur_more_than_once():
     """More rows are to stay than the budget holds: those of smallest index."""
     c = make(4, 1, 2, 16, 400, [400], 50, 5, 5, "f32")
@@ -137,6 +168,8 @@ def test_refusals():
     go(-2, "limits", B=3)
     go(-2, "limits", Hkv=3)
     go(-2, "limits", dh=72)
+    go(-2, "limits", cap=524289)
+    go(-2, "limits", budget=(1 << 30) + 1)
     go(-1, "aligned", k=ctypes.c_void_p(t["k"].data_ptr() + 8))
     torch.cuda.synchronize()
     assert not any(t[n].any() for n in ("kept", "weight_out", "pos_out", "ctx_out"))

@@ -72,6 +72,9 @@ SHAPES = [
     (1, 12, 1, 20, 80, 3, [2049], 2060),
     (4, 3, 3, 33, 16, 8, [512, 513, 5, 64], 530),
     (1, 40, 8, 128, 96, 8, [600], 601),
+    (1, 20, 1, 9, 64, 8, [300], 320),                      # 180 rows: more blocks than stay in registers
+    (1, 256, 1, 9, 32, 8, [130], 140),                     # as many rows as a key head may have
+    (1, 8, 8, 9, 16, 8, [40001], 40010),                   # several tiles for a wavefront
 ]
 
 
@@ -145,6 +148,7 @@ def test_refusals():
     for s in (0.0, -2.0, math.inf, math.nan):
         go(-1, "scale", scale=s)
     go(-2, "multiple of 8", dh=12)
+    go(-2, "2^30", cap=(1 << 30) + 1)
     go(-2, "T <=", T=9)
     go(-2, "limits", B=3)
     go(-2, "limits", H=6)
