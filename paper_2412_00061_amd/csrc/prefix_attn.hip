@@ -383,22 +383,23 @@ __global__ __launch_bounds__(64 * SH::NW, SH::WPE) void prefix_attn_kernel(Prefi
         }
       }
     };
-    // The reference only has to be near the maximum: it is moved when a score exceeds it by more than 2^8, so that P stays
-    // below 256; the two lanes of a row then agree on the larger.
+    // The reference (in the log2 domain) only has to be near the maximum: it is moved when a score exceeds it by more than 2^8, so that
+    // P stays below 256; the two lanes of a row then agree on the larger.  What weights, factors and joins take is this one rounded
+    // number, so that its rounding is in all of them alike; and where it is the maximum, the weight 1 is exact in bf16.
     auto reference = [&](const float (&mx)[QT]) __attribute__((always_inline)) {
       bool far = false;
 #pragma unroll
-      for (int qt = 0; qt < QT; ++qt) far |= (mx[qt] - m_run[qt]) * p.sl2 > 8.0f;
+      for (int qt = 0; qt < QT; ++qt) far |= fmaf(mx[qt], p.sl2, -m_run[qt]) > 8.0f;
       if (__builtin_amdgcn_ballot_w64(far) != 0ull) {
 #pragma unroll
         for (int qt = 0; qt < QT; ++qt) {
           const float m = fmaxf(mx[qt], __shfl_xor(mx[qt], 32, 64));
-          if ((m - m_run[qt]) * p.sl2 > 8.0f) {
-            const float alpha = __builtin_amdgcn_exp2f((m_run[qt] - m) * p.sl2);  // 0 on first use
+          if (fmaf(m, p.sl2, -m_run[qt]) > 8.0f) {
+            const float top = m * p.sl2, alpha = __builtin_amdgcn_exp2f(m_run[qt] - top);  // 0 on first use
             l_run[qt] *= alpha;
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt) o[qt][dt] *= alpha;
-            m_run[qt] = m;
+            m_run[qt] = top;
           }
         }
       }
@@ -413,7 +414,7 @@ __global__ __launch_bounds__(64 * SH::NW, SH::WPE) void prefix_attn_kernel(Prefi
       float ms[QT], sum[QT], mx[QT];
 #pragma unroll
       for (int qt = 0; qt < QT; ++qt) {
-        ms[qt] = (m_run[qt] > -INFINITY ? m_run[qt] : 0.f) * p.sl2;
+        ms[qt] = m_run[qt] > -INFINITY ? m_run[qt] : 0.f;
         sum[qt] = 0.f;
 #pragma unroll
         for (int i = 0; i < 16; ++i) sn[qt][i] = 0.f;
@@ -650,7 +651,7 @@ __global__ __launch_bounds__(64 * SH::NW, SH::WPE) void prefix_attn_kernel(Prefi
             const float* its = part + ((q * SH::CW + rg) * QT + qt) * (SH::PART / 4);
             const float mo = its[DT * 1024 + seg_lane], lother = its[DT * 1024 + 64 + seg_lane];
             const float m = fmaxf(m_run[qt], mo), base = m > -INFINITY ? m : 0.f;
-            const float a0 = __builtin_amdgcn_exp2f((m_run[qt] - base) * p.sl2), a1 = __builtin_amdgcn_exp2f((mo - base) * p.sl2);
+            const float a0 = __builtin_amdgcn_exp2f(m_run[qt] - base), a1 = __builtin_amdgcn_exp2f(mo - base);
             l_run[qt] = l_run[qt] * a0 + lother * a1;
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt)
@@ -678,7 +679,7 @@ __global__ __launch_bounds__(64 * SH::NW, SH::WPE) void prefix_attn_kernel(Prefi
             *(f32x4*)(po + (dt * 4 + i) * 256) = f32x4{o[qt][dt][4 * i], o[qt][dt][4 * i + 1], o[qt][dt][4 * i + 2], o[qt][dt][4 * i + 3]};
         if (sh == 0) {
           float* ml = p.pml + (size_t)slot * 2 * R + (rg * QT + qt) * 32 + sc;
-          ml[0] = m_run[qt] * p.sl2;
+          ml[0] = m_run[qt];
           ml[R] = l_run[qt];
         }
       }
