@@ -3,7 +3,8 @@
 //   weight[b,hk,j] += sum over the heads of hk's group and the accepted rows of exp(scale q . k_j - lse)
 //
 // With the rows' lse at hand (prefix_verify_attn) one read of K is all it takes: at most nine rows per head, so the call is bound by
-// that read.  S = Q K^T goes through matrix instructions with 16 rows of the group on one side and 16 keys on the other; a
+// that read (8 sequences x 32 heads of 256 to 2048 keys, 79 MB: 18.2 us, 4.3 TB/s; 4 x 8 key heads of 16384 to 65536, 346 MB: 68.9 us,
+// 5.0 TB/s).  S = Q K^T goes through matrix instructions with 16 rows of the group on one side and 16 keys on the other; a
 // lane then holds four rows of ONE key, and a key's sum is three additions and two exchanges.  (32 x 32 tiles: twice the
 // exponentials for nine rows, and loads of 32 bytes of a key instead of 64.)
 #include <type_traits>
@@ -30,14 +31,18 @@ struct KvWeightParams {
 
 constexpr int kKwMaxRows = 9 * 256;  // rows of a group: (T + 1) heads
 
-// Tiles of 32 keys that a wavefront takes one after the other, each requested under the products of the one before: enough
-// wavefronts to fill the chip come first.
+// Tiles of 32 keys that a wavefront takes one after the other, each requested under the products of the one before: several where
+// there are enough wavefronts for the chip all the same.  (bf16, 128 wide, us with one for every 4096 / 16384 / 32768 tiles there
+// are / with one always: 8 sequences x 32 key heads of 256 to 2048 keys 19.7 / 18.2 / 18.2 / 18.2, of 4096 62.5 / 55.3 / 59.3 / 59.2,
+// of 1000 to 8000 53.0 / 50.4 / 69.5 / 69.6; 4 x 8 of 16384 to 65536 73.8 / 68.9 / 71.5 / 82.8.)
 inline int weight_tiles(long long tiles) {
-  const long long most = tiles / 4096;
+  const long long most = tiles / 16384;
   return most < 1 ? 1 : (most > 8 ? 8 : (int)most);
 }
 
-// DHP: dh padded.  NB: blocks of 16 rows that stay in registers; 0: as many as there are, read again for every tile.
+// DHP: dh padded.  NB: blocks of 16 rows that stay in registers; 0: as many as there are, read again for every tile.  (The smallest
+// that holds them, as few registers as possible: 9 rows a key head 19.7 us with one block, 22.4 with room for five, 25.7 read again; 36
+// rows 73.8 with three, 80.3 with five, 111 read again.)
 template <bool F32, int DHP, int NB>
 __global__ __launch_bounds__(256, 2) void kv_weight_kernel(KvWeightParams p) {
 #if defined(__HIP_DEVICE_COMPILE__)
