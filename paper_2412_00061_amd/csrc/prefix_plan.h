@@ -15,8 +15,10 @@ namespace ctcspec {
 constexpr int kPrefixMaxGroups = 512;  // workgroups: one or two for each compute unit, each with an equal share of the work
 
 // Query rows of a workgroup, by the rows that share the prefix's keys (without one: the rows of a sequence): as many as there
-// are, up to what the registers hold, so that every key is fetched once for all of them.  (8 sequences x 64 nodes, 32 heads, us
-// with 128 / 256: behind 2048 keys 81 / 82, 8192 without history 135 / 98, 32768 445 / 352.)
+// are, up to what the registers hold, so that every key is fetched once for all of them.  (bf16, 32 heads of 128, us.  8 x 64 nodes
+// with 128 / 256: behind 2048 keys 81 / 82, 8192 without history 135 / 98, 32768 445 / 352.  8 x 16 nodes with 128 / 256: behind 16384
+// keys 75.6 / 83.2, 2048 32.4 / 30.9; 100 nodes behind 4000 31.9 / 36.4.  8 single tokens with 32 / 64 / 128 / 256: 26.7 / 27.2 /
+// 28.7 / 30.5; float, 12 heads of 64, with 32 / 128: 25.5 / 28.2.)
 inline int prefix_block_rows(long long rows, bool f32) {
   if (rows <= 32) return 32;
   if (f32) return 128;
