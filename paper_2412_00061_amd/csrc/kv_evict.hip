@@ -259,6 +259,7 @@ __global__ __launch_bounds__(kEvThreads) void kv_evict_select_kernel(KvEvictPara
   auto place_of = [&](unsigned int key, unsigned int from_top) __attribute__((always_inline)) {  // key, index from the top
     return (unsigned long long)(key >> (32 - kEvIndexBits)) << 32 | (key << kEvIndexBits | from_top);
   };
+  __syncthreads();  // (everyone has read what the last digit found)
   if (tid == 0) found[0] = 0;
   __syncthreads();
   each([&](int k, const bool (&there)[G], const unsigned int (&key)[G]) __attribute__((always_inline)) {

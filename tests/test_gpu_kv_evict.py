@@ -72,6 +72,7 @@ SHAPES = [
     (1, 1, 8, 70000, [70000], 69000, 0, 0),
     (2, 2, 64, 300, [300, 1000000], 500, 3, 10),             # a budget beyond the capacity
     (1, 4, 64, 2320, [2304], 2048, 4, 256),
+    (3, 1, 8, 40000, [3000, 17000, 200], 129, 4, 64),        # short histories in a long cache
 ]
 
 
