@@ -117,15 +117,19 @@ __global__ __launch_bounds__(256, 2) void kv_weight_kernel(KvWeightParams p) {
   // a block's weights of this lane's key; rows below `from` do not see it
   auto weigh = [&](const u32x4 (&qf)[QS], f32x4 lse, const u32x4 (&kf)[QS], int row0, int from) __attribute__((always_inline)) {
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
+    if constexpr (F32) {
+      // (sums side by side: a long one's every addition is rounded at the size of the whole)
+      f32x4 part[4] = {s, s, s, s};
 #pragma unroll
-    for (int u = 0; u < QS; ++u) {
-      if constexpr (F32) {
+      for (int u = 0; u < QS; ++u)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          s = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(qf[u][e]), __uint_as_float(kf[u][e]), s, 0, 0, 0);
-      } else {
+          part[u % 4] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(qf[u][e]), __uint_as_float(kf[u][e]), part[u % 4], 0, 0, 0);
+      s = (part[0] + part[1]) + (part[2] + part[3]);
+    } else {
+#pragma unroll
+      for (int u = 0; u < QS; ++u)
         s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, qf[u]), __builtin_bit_cast(bf16x8, kf[u]), s, 0, 0, 0);
-      }
     }
     float sum = 0.f;
 #pragma unroll
