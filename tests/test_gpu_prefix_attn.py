@@ -87,7 +87,7 @@ def allowed(c, b, bf16_out):
     output.  A score is a sum of dh products, each exact (bf16) or rounded once, added in float32: off by at most
     (dh + 2) 2^-24 sum |q k| scale, and as much again where it is scaled; a weight by twice that (numerator and sum), by 2^-22
     for the exponential and its argument's rounding, 2^-24 per addition of up to 32 keys' tiles in a lane and of the joins; bf16
-    weights are two numbers whose sum is within 2^-15 of them, or one within 2^-8."""
+    weights are two numbers or three whose sum is within 2^-15 of them, or one within 2^-8."""
     n, L, P = c["n"][b], c["ctx"][b], c["P"]
     group = c["H"] // c["Hkv"]
     mean, score = np.zeros((c["H"], n)), np.zeros((c["H"], n))
