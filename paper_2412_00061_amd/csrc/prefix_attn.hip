@@ -265,7 +265,10 @@ __global__ __launch_bounds__(64 * SH::NW, SH::WPE) void prefix_attn_kernel(Prefi
     // ---- the tiles of iteration i of this segment into their stage -----------------------------------------------------------
     // (The bases are parameters: captured, the choice between them becomes one between their addresses, in scratch memory.  The
     // instruction is written out because the compiler would let every transposing read wait for all requests that it knows of;
-    // it has no register for a result, and the loop below waits for it.)
+    // it has no register for a result, and the loop below waits for it.  The compiler counts no wait states for what is written
+    // out, so they stand inside: a vector instruction that writes a scalar register - v_readfirstlane for the descriptor, v_readlane
+    // where it comes back from a spill - has to lie five wait states before the load that reads it: one for s_mov, four for s_nop 3.
+    // m0 needs one of them.)
     auto request = [&](int i, const unsigned char* kc, const unsigned char* vc, const unsigned char* kt, const unsigned char* vt)
         __attribute__((always_inline)) {
       const unsigned int stage = lds0 + i % SH::NS * SH::STAGE + wave * NREQ * 1024;
@@ -282,7 +285,7 @@ __global__ __launch_bounds__(64 * SH::NW, SH::WPE) void prefix_attn_kernel(Prefi
         const u32x4 rsrc = {(unsigned)uniform((int)at), (unsigned)uniform((int)(at >> 32)) & 0xffffu, (unsigned)uniform(left * rb), 0x00020000u};
 #pragma unroll
         for (int j = q * kRun; j < (q + 1) * kRun; ++j)
-          asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(stage + j * 1024), "v"(voff[j]), "s"(rsrc)
+          asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(stage + j * 1024), "v"(voff[j]), "s"(rsrc)
                        : "memory", "m0");
       }
     };
