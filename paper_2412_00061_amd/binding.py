@@ -237,6 +237,13 @@ def _out(out, name, shape, dtype, device):
     return torch.empty(shape, dtype=dtype, device=device)
 
 
+def _workspace(ctx, nbytes, device):
+    """Scratch of one call, from the pool of the stream that its kernels run on.  The block goes back there when the call returns, while
+    they may still use it: whoever has it next comes behind them."""
+    with torch.cuda.stream(ctx.stream):
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
 def ctc_draft_topk(ctx, hidden, w, bias, k, *, want_logits=False, out=None):
     """hidden [B,T,D], w [V+1,D] (same dtype), bias [V+1] f32 or None -> dict(topk_id, topk_logp, lse[, logits])."""
     B, T, D = hidden.shape
@@ -414,7 +421,7 @@ def draft_layer_forward(ctx, x, weights, pos0, k_cache, v_cache, kv_off, ctx_len
     B, T, D = x.shape
     dev = x.device
     if workspace is None:
-        workspace = torch.empty(draft_layer_workspace_bytes(B, T, D, H, F), dtype=torch.uint8, device=dev)
+        workspace = _workspace(ctx, draft_layer_workspace_bytes(B, T, D, H, F), dev)
     res = {"out": _out(out, "out", (B, T, D), torch.bfloat16, dev),
            "k_new": _out(out, "k_new", (B, H, T, D // H), torch.bfloat16, dev),
            "v_new": _out(out, "v_new", (B, H, T, D // H), torch.bfloat16, dev)}
@@ -456,7 +463,7 @@ def ctc_loss(ctx, logits, labels, label_len, frame_len, blank_id, *, want_grad=T
     dev = logits.device
     need = ctc_loss_workspace_bytes(B, T, Lmax)
     if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+        workspace = _workspace(ctx, need, dev)
     res = {"loss": _out(out, "loss", (B,), torch.float32, dev)}
     if want_grad:
         res["grad"] = _out(out, "grad", (B, T, Vp1), torch.float32, dev)
@@ -499,7 +506,7 @@ def prefix_verify_attn(ctx, q, k_prefix, v_prefix, prefix_len, k_cache, v_cache,
     for name, t in (("kv_off", kv_off), ("ctx_len", ctx_len), ("n_nodes", n_nodes)):
         _shaped(name, t, (B,))
     if workspace is None:
-        workspace = torch.empty(prefix_verify_attn_workspace_bytes(B, H, H_kv, dh, N), dtype=torch.uint8, device=dev)
+        workspace = _workspace(ctx, prefix_verify_attn_workspace_bytes(B, H, H_kv, dh, N), dev)
     res = {"out": _out(out, "out", (B, H, N, dh), out_dtype, dev)}
     if want_lse:
         res["lse"] = _out(out, "lse", (B, H, N), torch.float32, dev)
