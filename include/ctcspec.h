@@ -475,7 +475,7 @@ int ctc_loss(ctcspec_ctx* ctx, const float* logits, const int32_t* labels, const
  * workspace     device scratch of at least prefix_verify_attn_workspace_bytes(B, H, H_kv, dh, max_nodes) bytes, owned by the
  *               caller, contents undefined afterwards; calls that share it must not overlap.  Bytes for some B and max_nodes
  *               serve every smaller B and max_nodes
- * out_dt, out   [B,H,max_nodes,dh] out: CTCSPEC_F32 (weights carried with 16 or more bits of mantissa), or CTCSPEC_BF16 with
+ * out_dt, out   [B,H,max_nodes,dh] out: CTCSPEC_F32 (weights carried with 24 bits), or CTCSPEC_BF16 with
  *               bf16 operands (weights rounded to bf16 as well: a third to a half less work)
  * lse           [B,H,max_nodes] float out or NULL: what kv_weight_update takes
  * Pointers 16-byte aligned (prefix_len, ctx_len, n_nodes, kv_off, anc_mask and lse as their types are).

@@ -16,7 +16,7 @@
 // the matrix units' cycles (0.75 PFLOP/s of the call's own products, 0.94 of those on whole blocks); a tile's exponentials take as long
 // as its products and only partly run beside them.  Long histories: their bytes - an iteration over own keys takes 32 KB into a compute
 // unit in 3.7 k cycles, 4.7 TB/s over the chip.  Short calls: the first keys' way in (about 6 k cycles for 64 KB a compute unit, all at
-// once) and the second kernel (6 us, most of it latency).  8 x 64 nodes behind 2048 keys with 256 to 2048 of their own: 90 us, 203 MB;
+// once) and the second kernel (6 us, most of it latency).  8 x 64 nodes behind 2048 keys with 256 to 2048 of their own: 97 us, 203 MB;
 // one token for each of 8 sequences behind 2048: 30 us, 52 MB.
 #include <type_traits>
 #include <utility>
@@ -415,12 +415,6 @@ __global__ __launch_bounds__(64 * SH::NW, SH::WPE) void prefix_attn_kernel(Prefi
       }
     };
 
-    // A float result's weights: three parts where the products are not what the time goes by, two for 256 rows that share a prefix.
-    // (8 sequences x 64 nodes behind 2048 keys, off from the exact result by, relative to it: two parts everywhere 84.4 us, 1.1e-6;
-    // so 90.4 us, 8.7e-7; three everywhere 95 us, 4.4e-7.  Single tokens: 29.5 us, 1.1e-6; 29.9 us, 3.5e-7.)
-    const bool three = R < 256 || own;
-    const float left_out = three ? 0.f : 1.f;
-
     // Tile k at `tile`, its scores in s and the reference set for them; the next tile k1 at `next` (any1: it is part of the
     // segment), whose scores go to sn; read_next() requests the first fragments of the tile behind it.
     auto step = [&](int k, unsigned int tile, int k1, bool any1, unsigned int next, f32x16 (&s)[QT], f32x16 (&sn)[QT], auto&& read_next,
@@ -497,8 +491,9 @@ __global__ __launch_bounds__(64 * SH::NW, SH::WPE) void prefix_attn_kernel(Prefi
           for (int j = from; j < to; ++j)
 #pragma unroll
             for (int qt = 0; qt < QT; ++qt) {
-              // P is rounded to bf16, as the values are and as the result will be; FINE: P = hi + lo, within 2^-16 of it, or
-              // hi + lo + rest, within 2^-24
+              // P is rounded to bf16, as the values are and as the result will be; FINE: P = hi + lo + rest, within 2^-24 of it.
+              // (Two parts, within 2^-16, where 256 rows share a prefix: 8 sequences x 64 nodes behind 2048 keys 93 us instead of 97,
+              // and a weight off by up to 2^-17 as soon as more than 128 rows are in the batch.)
               const float p0 = __builtin_amdgcn_exp2f(fmaf(s[qt][2 * j], p.sl2, -ms[qt]));
               const float p1 = __builtin_amdgcn_exp2f(fmaf(s[qt][2 * j + 1], p.sl2, -ms[qt]));
               const unsigned int h = __builtin_bit_cast(unsigned int, bf16x2{(__bf16)p0, (__bf16)p1});
@@ -509,11 +504,8 @@ __global__ __launch_bounds__(64 * SH::NW, SH::WPE) void prefix_attn_kernel(Prefi
                 lo[qt][j / 4][j % 4] = r;
                 const float r0 = (p0 - h0) - __uint_as_float(r << 16), r1 = (p1 - h1) - __uint_as_float(r & 0xffff0000u);
                 rest[qt][j / 4][j % 4] = __builtin_bit_cast(unsigned int, bf16x2{(__bf16)r0, (__bf16)r1});
-                // (the sum is that of the weights as they are multiplied: what both are off by in common goes)
-                sum[qt] += R < 256 ? p0 + p1 : fmaf(-left_out, r0 + r1, p0 + p1);
-              } else {
-                sum[qt] += p0 + p1;
               }
+              sum[qt] += p0 + p1;
               asm volatile("" : "+v"(sum[qt]));  // (here, not at the end of the tile)
             }
         };
@@ -562,10 +554,8 @@ __global__ __launch_bounds__(64 * SH::NW, SH::WPE) void prefix_attn_kernel(Prefi
         if constexpr (SH::FINE) {
 #pragma unroll
           for (int dt = 0; dt < DT; ++dt) value(dt, 0, lo);
-          if (three) {
 #pragma unroll
-            for (int dt = 0; dt < DT; ++dt) value(dt, 0, rest);
-          }
+          for (int dt = 0; dt < DT; ++dt) value(dt, 0, rest);
         }
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) {
@@ -581,10 +571,8 @@ __global__ __launch_bounds__(64 * SH::NW, SH::WPE) void prefix_attn_kernel(Prefi
         if constexpr (SH::FINE) {
 #pragma unroll
           for (int dt = 0; dt < DT; ++dt) value(dt, 1, lo);
-          if (three) {
 #pragma unroll
-            for (int dt = 0; dt < DT; ++dt) value(dt, 1, rest);
-          }
+          for (int dt = 0; dt < DT; ++dt) value(dt, 1, rest);
         }
       }
 #pragma unroll
