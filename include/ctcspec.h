@@ -480,7 +480,9 @@ int ctc_loss(ctcspec_ctx* ctx, const float* logits, const int32_t* labels, const
  * lse           [B,H,max_nodes] float out or NULL: what kv_weight_update takes
  * Pointers 16-byte aligned (prefix_len, ctx_len, n_nodes, kv_off, anc_mask and lse as their types are).
  * Limits: dh % 8 == 0, dh <= CTCSPEC_MAX_HEAD_DIM, max_nodes <= CTCSPEC_MAX_NODES, B <= 64; B, H, dh, max_nodes within the
- * context's limits; H % H_kv == 0; kv_cap, prefix_cap and B * max_nodes * H / H_kv <= 2^30.  The same bits on every run.
+ * context's limits; H % H_kv == 0; kv_cap, prefix_cap and B * max_nodes * H / H_kv <= 2^30; iterations over the keys (of 32 or 64, for a
+ * block of 32 to 256 rows) are counted in 32 bits: 64 sequences x 128 nodes x 32 heads may have 4e7 rows of prefix, or of their own 3e7,
+ * and a call that could need more is refused (CTCSPEC_EUNSUPPORTED).  The same bits on every run.
  */
 size_t prefix_verify_attn_workspace_bytes(int B, int H, int H_kv, int dh, int max_nodes);
 

@@ -127,6 +127,7 @@ struct PrefixShape {
   static constexpr int LDS = (NS * STAGE > JOIN ? NS * STAGE : JOIN) + kPrefixTable;
   // what 256 compute units hold at once
   static constexpr int GROUPS = WPE * 4 >= 2 * NW && 2 * LDS <= 160 * 1024 ? 512 : 256;
+  static_assert(TPI == prefix_tiles(R, DHP, F32));
   static_assert(TPI * 2 * RQ % NW == 0 && LDS <= 160 * 1024, "requests in equal shares; fits the LDS");
   // 16-byte chunk c of row r lies at chunk c ^ f(r).  K: the LDS serves lanes l .. l+7 with l+16 .. l+23 together, which read
   // the same chunk of rows r .. r+7 and r+16 .. r+23 - 16 places of 16 bytes.  V, bf16: 32 lanes read 8 bytes each of four
@@ -900,12 +901,12 @@ extern "C" int prefix_verify_attn(ctcspec_ctx* ctx, ctcspec_dtype dt, const void
   CTCSPEC_REQUIRE(ctx, B <= ctx->lim.max_batch && B <= 64 && max_nodes <= ctx->lim.max_nodes && H <= ctx->lim.max_heads &&
                            dh <= ctx->lim.max_head_dim && H_kv <= 65535,
                   CTCSPEC_EUNSUPPORTED, "prefix_verify_attn: shape exceeds the context's limits");
-  CTCSPEC_REQUIRE(ctx, prefix_units_fit(B, H_kv, (long long)max_nodes * (H / H_kv), prefix_cap, kv_cap, max_nodes),
+  const bool f32 = dt == CTCSPEC_F32, fine = out_dt == CTCSPEC_F32;
+  const PrefixWorkspace ws = prefix_workspace(B, H, H_kv, dh, max_nodes, prefix_cap > 0, f32);
+  CTCSPEC_REQUIRE(ctx, prefix_units_fit(ws.rows, B, H_kv, (long long)max_nodes * (H / H_kv), prefix_padded_dim(dh), prefix_cap, kv_cap, max_nodes, f32),
                   CTCSPEC_EUNSUPPORTED, "prefix_verify_attn: capacities or rows beyond 2^30, or work of more than 2^31 units");
   for (const void* a : {q, k_prefix, v_prefix, k_cache, v_cache, k_tree, v_tree, (const void*)workspace, (const void*)out})
     CTCSPEC_REQUIRE(ctx, aligned16(a), CTCSPEC_EINVAL, "prefix_verify_attn: pointers must be 16-byte aligned");
-  const bool f32 = dt == CTCSPEC_F32, fine = out_dt == CTCSPEC_F32;
-  const PrefixWorkspace ws = prefix_workspace(B, H, H_kv, dh, max_nodes, prefix_cap > 0, f32);
   CTCSPEC_REQUIRE(ctx, workspace_bytes >= ws.total, CTCSPEC_EINVAL, "prefix_verify_attn: workspace of %zu bytes needed, %zu given",
                   ws.total, workspace_bytes);
 

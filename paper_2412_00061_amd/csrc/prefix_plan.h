@@ -58,14 +58,24 @@ CTCSPEC_BOTH Deal prefix_deal(int units, int groups) {
   d.more = units - d.each * d.groups;
   return d;
 }
-// rows, keys and units are counted in 32 bits: whether that is enough for the largest lengths
-inline bool prefix_units_fit(long long B, int H_kv, long long seq_rows, int prefix_cap, int kv_cap, int max_nodes) {
-  const double own = (double)B * ((seq_rows + 31) / 32) * (kPrefixOwnWeight * ((kv_cap + 31LL) / 32 + max_nodes / 32 + 1) + prefix_block_units(false));
-  const double prefix = (double)((B * seq_rows + 31) / 32) * (3 * ((prefix_cap + 31LL) / 32) + prefix_block_units(false));
-  return (own + prefix) * H_kv < 2147483647.0 && B * seq_rows <= 1LL << 30 && prefix_cap <= 1 << 30 && kv_cap <= 1 << 30;
-}
-
 inline int prefix_padded_dim(int dh) { return dh <= 64 ? 64 : 128; }
+
+// Tiles of 32 keys that an iteration takes: one for each of a shape's key parts, two where a wavefront has all keys of 256 rows.
+CTCSPEC_BOTH constexpr int prefix_tiles(int rows, int padded_dim, bool f32) { return f32 && (rows > 32 || padded_dim > 64) ? 1 : 2; }
+
+// The most units that a call can have whose workgroups take `rows` rows.
+inline double prefix_most_units(int rows, long long B, int H_kv, long long seq_rows, int padded_dim, int prefix_cap, int kv_cap, int max_nodes, bool f32) {
+  const long long tiles = prefix_tiles(rows, padded_dim, f32), block = prefix_block_units(f32);
+  auto up = [](long long a, long long b) { return (a + b - 1) / b; };
+  const long long own = block + kPrefixOwnWeight * up(up(kv_cap, 32) + up(max_nodes, 32), tiles);
+  const long long prefix = prefix_cap ? block + prefix_shared_weight(rows) * up(up(prefix_cap, 32), tiles) : 0;
+  return ((double)B * up(seq_rows, rows) * own + (double)up(B * seq_rows, rows) * prefix) * H_kv;
+}
+// Rows, keys and units are counted in 32 bits: whether that is enough for the largest lengths.
+inline bool prefix_units_fit(int rows, long long B, int H_kv, long long seq_rows, int padded_dim, int prefix_cap, int kv_cap, int max_nodes, bool f32) {
+  return B * seq_rows <= 1LL << 30 && prefix_cap <= 1 << 30 && kv_cap <= 1 << 30 &&
+         prefix_most_units(rows, B, H_kv, seq_rows, padded_dim, prefix_cap, kv_cap, max_nodes, f32) < 2147483647.0;
+}
 
 struct PrefixWorkspace {
   int rows;  // of a workgroup
