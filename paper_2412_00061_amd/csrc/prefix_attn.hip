@@ -254,11 +254,8 @@ __global__ __launch_bounds__(64 * SH::NW, SH::WPE) void prefix_attn_kernel(Prefi
     const int share = uniform(units - at_unit < u1 - u ? units - at_unit : u1 - u);
     u += share;
     // the iterations that begin in the share
-    auto iterations = [&](int units) __attribute__((always_inline)) {
-      const int x = units - prefix_block_units(SH::F32);
-      return uniform(x > 0 ? (x + weight - 1) / weight : 0);
-    };
-    const int it0 = iterations(at_unit), niter = iterations(at_unit + share) - it0;
+    const int it0 = uniform(prefix_iterations(at_unit, weight, SH::F32));
+    const int niter = uniform(prefix_iterations(at_unit + share, weight, SH::F32)) - it0;
     if (niter <= 0) continue;
     kc = uniform(kc); vc = uniform(vc); kt = uniform(kt); vt = uniform(vt);
     const int ctx_tiles = own ? (L + 31) / 32 : 0x7fffffff;  // the tiles from here on are tree nodes

@@ -47,8 +47,17 @@ struct Deal {
     return u < big ? u / (each + 1) : more + (u - big) / each;
   }
 };
-// A share is at least kPrefixMinUnits.
+// As few workgroups as need at most kPrefixMinUnits each, up to those there are: all work is one share, or each has at least
+// half as many units (7 units are two shares, 4 and 3).  The join reads a partial result from every workgroup between the owners of
+// a block's first and last iteration, so each of these has to begin an iteration there: no share may be shorter than one.
 constexpr int kPrefixMinUnits = 6;
+static_assert((kPrefixMinUnits + 1) / 2 >= prefix_shared_weight(256) && (kPrefixMinUnits + 1) / 2 >= prefix_shared_weight(32) &&
+              (kPrefixMinUnits + 1) / 2 >= kPrefixOwnWeight);
+// Iterations that begin in the first `units` units of a block of rows, an iteration being `weight` of them.
+CTCSPEC_BOTH int prefix_iterations(int units, int weight, bool f32) {
+  const int x = units - prefix_block_units(f32);
+  return x > 0 ? (x + weight - 1) / weight : 0;
+}
 CTCSPEC_BOTH Deal prefix_deal(int units, int groups) {
   Deal d;
   const int most = (int)(((unsigned)units + kPrefixMinUnits - 1) / kPrefixMinUnits);
