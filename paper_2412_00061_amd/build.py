@@ -20,8 +20,6 @@ HIPCC_FLAGS = [
     # keep the compiler from emitting packed fp32 VALU ops
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-Wall", "-Wno-unused-function", "-Wno-unused-command-line-argument",
-    # prefix_attn.hip's requests write m0, a reserved register, and say so
-    "-Wno-inline-asm",
 ]
 
 

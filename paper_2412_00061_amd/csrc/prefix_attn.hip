@@ -281,10 +281,13 @@ __global__ __launch_bounds__(64 * SH::NW, SH::WPE) void prefix_attn_kernel(Prefi
         const int from = left > 0 ? row0 : 0;
         const unsigned long long at = (unsigned long long)base + (size_t)from * rb;
         const u32x4 rsrc = {(unsigned)uniform((int)at), (unsigned)uniform((int)(at >> 32)) & 0xffffu, (unsigned)uniform(left * rb), 0x00020000u};
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"  // (that m0 is reserved: nothing else here uses it)
 #pragma unroll
         for (int j = q * kRun; j < (q + 1) * kRun; ++j)
           asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(stage + j * 1024), "v"(voff[j]), "s"(rsrc)
                        : "memory", "m0");
+#pragma clang diagnostic pop
       }
     };
     constexpr int kEarly = SH::NS > 2 ? 2 : 1;  // stages in front of the rows, which everything waits for together

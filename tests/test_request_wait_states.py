@@ -17,8 +17,9 @@ def kernels(tmp_path_factory):
     """{name of a prefix_attn_kernel: its instructions, labels among them as ''}."""
     csrc, at = os.path.join(build.HERE, "csrc"), tmp_path_factory.mktemp("asm") / "p.s"
     flags = [f for f in build.HIPCC_FLAGS if f not in ("-shared", "-fPIC")]
-    subprocess.run([os.environ.get("HIPCC", "/opt/rocm/bin/hipcc"), *flags, "-I", os.path.join(build.ROOT, "include"), "-I", csrc,
-                    "--cuda-device-only", "-S", os.path.join(csrc, "prefix_attn.hip"), "-o", str(at)], check=True, capture_output=True)
+    said = subprocess.run([os.environ.get("HIPCC", "/opt/rocm/bin/hipcc"), *flags, "-I", os.path.join(build.ROOT, "include"), "-I", csrc,
+                           "--cuda-device-only", "-S", os.path.join(csrc, "prefix_attn.hip"), "-o", str(at)], check=True, capture_output=True, text=True).stderr
+    assert "-Winline-asm" not in said and not any("inline-asm" in f for f in flags)  # (silent where m0 is written, and only there)
     found = {}
     for name, body in re.findall(r"; -- Begin function (\S+)(.*?); -- End function", at.read_text(), re.S):
         if "prefix_attn_kernel" not in name:
