@@ -109,6 +109,35 @@ def test_weights(shape, dtype, out):
     ctx.close()
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,out", [("bf16", "f32"), ("bf16", "bf16"), ("f32", "f32")])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "x".join(map(str, s[:6])))
+def test_sums(shape, dtype, out):
+    """lse: the sum takes the weights before they are rounded to bf16, so it has a float's bits whatever the result's type.  Off by the sum's
+    relative error (what `limits` allows a weight without its parts), the reference's two roundings (a score in the log2 domain: of log2(e)
+    and of the product), two steps of the logarithm, which is below 8 (half a step of that: 4 U), and the roundings of the sum of
+    both, of ln 2 and of the last product."""
+    import torch
+    from test_gpu_prefix_attn import call, context, upload
+    c = exact_case(7, *shape, dtype)
+    ctx = context(c)
+    res = call(ctx, c, upload(c), torch.bfloat16 if out == "bf16" else torch.float32)["lse"].double().cpu().numpy()
+    for b in range(c["B"]):
+        n = c["n"][b]
+        if not n:
+            continue
+        L, P = c["ctx"][b], c["P"]
+        weights, lse = oracle.prefix_attention(c["q"][b, :, :n], c["kp"], c["vp"], c["kc"][b, :, :L], c["vc"][b, :, :L], c["kt"][b], c["vt"][b], n,
+                                               c["seen"][b, :n, :n], SCALE)
+        low = np.where(weights > 0, weights, np.inf).min(-1)
+        spread = float(np.log2(weights.max(-1) / low).max())
+        top = np.abs(lse + np.log(weights.max(-1))) + spread  # the reference is a score within that
+        lim = limits(spread, 0.0, False)[0] + 2 * top * U + 4 * 4 * U + 3 * (np.abs(lse) + top + 8) * U
+        off = np.abs(res[b, :, :n] - lse)
+        assert np.all(off <= lim), (b, float((off / lim).max()))
+    ctx.close()
+
+
 def bf16(x):
     import torch
     return torch.from_numpy(x).bfloat16().float().numpy()
