@@ -459,7 +459,8 @@ int ctc_loss(ctcspec_ctx* ctx, const float* logits, const int32_t* labels, const
  *   lse[b,h,i]   = log sum_{j in keys} exp(scale * q[b,h,i,:] . key_j)
  *   out[b,h,i,:] = sum_{j in keys} exp(scale * q[b,h,i,:] . key_j - lse[b,h,i]) * value_j
  *
- * A row that sees no key at all (no prefix, no cached row, an empty mask row) has out = 0 and lse = -inf.  Rows
+ * A row that sees no key at all (no prefix, no cached row, an empty mask row), or none whose score is above -infinity, has out = 0
+ * and lse = -inf.  Rows
  * i >= n_nodes[b] are not written; n_nodes[b] may be 0 (a place of the batch that is not in use).  No positional encoding is
  * applied.  The lengths are read on the device; those beyond their capacity count as the capacity, negative ones as 0.
  * A value that is infinite or not a number reaches the rows that see its key and no other row; a score that is, likewise.

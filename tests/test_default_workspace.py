@@ -88,3 +88,37 @@ def test_two_streams_in_turn():
         assert all(torch.equal(a, b) for a, b in zip(row, want))
     for ctx in (alone, *ctxs):
         ctx.close()
+
+
+@pytest.mark.gpu
+def test_captured_without_a_workspace():
+    """Two calls in a graph, both with scratch of their own making; other tensors come and go between the replays."""
+    g = torch.Generator().manual_seed(4)
+    f = lambda *s: torch.randn(s, generator=g).bfloat16().cuda()  # noqa: E731
+    i = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    B, H, N, dh, P, cap = 3, 4, 33, 64, 200, 100
+    args = [(f(B, H, N, dh), f(2, P, dh), f(2, P, dh), i(P), f(B * 2 * cap * dh), f(B * 2 * cap * dh), torch.arange(B, device="cuda") * (2 * cap * dh),
+             i(cap, 0, 7), cap, f(B, 2, N, dh), f(B, 2, N, dh), i(N, 1, 20), torch.full((B, N, 1), -1, dtype=torch.int64, device="cuda"), 0.125)
+            for _ in range(2)]
+    out = [{"out": torch.zeros((B, H, N, dh), device="cuda")} for _ in args]
+    stream = torch.cuda.Stream()
+    ctx = pkg.Context(max_batch=B, max_slots=1, max_topk=1, max_vocab_rows=16, max_nodes=N, max_heads=H, max_head_dim=dh, stream=stream)
+    torch.cuda.synchronize()
+    for a, o in zip(args, out):
+        pkg.prefix_verify_attn(ctx, *a, out=o)
+    torch.cuda.synchronize()
+    want = [o["out"].clone() for o in out]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        for a, o in zip(args, out):
+            pkg.prefix_verify_attn(ctx, *a, out=o)
+    for _ in range(4):
+        other = [torch.full((1 << 20,), 7.0, device="cuda") for _ in range(8)]
+        for o in out:
+            o["out"].zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(o["out"], w) for o, w in zip(out, want)) and all((x == 7).all() for x in other)
+        del other
+    ctx.close()

@@ -41,3 +41,26 @@ def test_more_work_than_it_counts_is_refused():
     torch.cuda.synchronize()
     assert not ws.any()  # nothing was launched
     ctx.close()
+
+
+@pytest.mark.parametrize("dtype,out", [("bf16", "f32"), ("bf16", "bf16"), ("f32", "f32")])
+def test_rows_whose_scores_are_all_minus_infinity(dtype, out):
+    """They give no key a weight: as rows that see none."""
+    import torch
+    t, od = (torch.bfloat16 if x == "bf16" else torch.float32 for x in (dtype, out))
+    B, H, N, dh, P, L = 2, 2, 5, 64, 37, 9
+    ctx = pkg.Context(max_batch=B, max_slots=1, max_topk=1, max_vocab_rows=16, max_nodes=N, max_heads=H, max_head_dim=dh)
+    z = lambda *s: torch.zeros(s, dtype=t, device="cuda")  # noqa: E731
+    i = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    q, kp, kc, kt = z(B, H, N, dh), z(H, P, dh), z(B * H * L, dh), z(B, H, N, dh)
+    for k in (kp, kc, kt):
+        k[..., 0] = -1
+    q[0, 1, 2, 0] = float("inf")
+    v = [torch.ones_like(k) for k in (kp, kc, kt)]
+    res = pkg.prefix_verify_attn(ctx, q, kp, v[0], i(P), kc.view(-1), v[1].view(-1), torch.arange(B, device="cuda") * (H * L * dh), i(L, L), L, kt,
+                                 v[2], i(N, N), torch.full((B, N, 1), -1, dtype=torch.int64, device="cuda"), 0.125, out_dtype=od, want_lse=True)
+    some = torch.ones((B, H, N), dtype=torch.bool, device="cuda")
+    some[0, 1, 2] = False
+    assert (res["out"][~some] == 0).all() and torch.isneginf(res["lse"][~some]).all()
+    assert ((res["out"][some].float() - 1).abs() <= 2.0 ** -8).all() and torch.isfinite(res["lse"][some]).all()
+    ctx.close()
