@@ -477,7 +477,8 @@ int ctc_loss(ctcspec_ctx* ctx, const float* logits, const int32_t* labels, const
  *               caller, contents undefined afterwards; calls that share it must not overlap.  Bytes for some B and max_nodes
  *               serve every smaller B and max_nodes
  * out_dt, out   [B,H,max_nodes,dh] out: CTCSPEC_F32 (weights carried with 24 bits), or CTCSPEC_BF16 with
- *               bf16 operands (weights rounded to bf16 as well: a third to a half less work)
+ *               bf16 operands (weights rounded to bf16 as well: a third to a half less work.  A bf16 result of fine weights
+ *               is the float one rounded)
  * lse           [B,H,max_nodes] float out or NULL: what kv_weight_update takes
  * Pointers 16-byte aligned (prefix_len, ctx_len, n_nodes, kv_off, anc_mask and lse as their types are).
  * Limits: dh % 8 == 0, dh <= CTCSPEC_MAX_HEAD_DIM, max_nodes <= CTCSPEC_MAX_NODES, B <= 64; B, H, dh, max_nodes within the

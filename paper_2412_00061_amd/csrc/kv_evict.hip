@@ -57,7 +57,8 @@ __device__ __forceinline__ unsigned int evict_key(float weight, int pos, int sin
 // K: a lane holds up to K keys in registers (rows 64 k + lane of its wavefront's range): the passes read memory once.  0: for
 // capacities beyond that; every pass reads the weights again, eight rows of a lane at a time and the next eight under way.  (The
 // call in us with the keys in registers / read again: 700 rows 12.3 / 18.3, 2304 rows 27.1 / 35.7, 4000 rows 27.3 / 37.4, 12000 rows
-// 59.8 / 66.1; with 96 rows in registers 65536 rows 91 / 74: they leave none for the rows of a step.)
+// 59.8 / 66.1; with 96 rows in registers 65536 rows 91 / 74: they leave none for the rows of a step.  It goes by the capacity, as the host
+// does not know the lengths: 8 x 32 heads from 700 rows to 512 take 15.7 us with room for 704, 17.2 for 16384 and 21.5 for 20000.)
 // What bounds it: up to some thousand rows the steps' latencies, one workgroup behind each other's barriers; beyond, instructions - a
 // compute unit takes a cycle for one on 64 rows -, of which a row takes about 20 in each of the two or three passes.  (32 heads of
 // 65536 rows to 4096: 43 us; 256 heads of 2304 rows to 2048: 10.5 us.)

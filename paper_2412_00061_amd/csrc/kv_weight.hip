@@ -3,8 +3,8 @@
 //   weight[b,hk,j] += sum over the heads of hk's group and the accepted rows of exp(scale q . k_j - lse)
 //
 // With the rows' lse at hand (prefix_verify_attn) one read of K is all it takes: at most nine rows per head, so the call is bound by
-// that read (8 sequences x 32 heads of 256 to 2048 keys, 79 MB: 18.2 us, 4.3 TB/s; 4 x 8 key heads of 16384 to 65536, 346 MB: 68.9 us,
-// 5.0 TB/s).  S = Q K^T goes through matrix instructions with 16 rows of the group on one side and 16 keys on the other; a
+// that read (8 sequences x 32 heads of 256 to 2048 keys, 79 MB: 18 to 21 us from card to card, 3.8 to 4.4 TB/s; 4 x 8 key heads of 16384
+// to 65536, 346 MB: 69 to 78 us, 4.4 to 5.0 TB/s).  S = Q K^T goes through matrix instructions with 16 rows of the group on one side and 16 keys on the other; a
 // lane then holds four rows of ONE key, and a key's sum is three additions and two exchanges.  (32 x 32 tiles: twice the
 // exponentials for nine rows, and loads of 32 bytes of a key instead of 64.)
 #include <type_traits>
@@ -34,7 +34,9 @@ constexpr int kKwMaxRows = 9 * 256;  // rows of a group: (T + 1) heads
 // Tiles of 32 keys that a wavefront takes one after the other, each requested under the products of the one before: several where
 // there are enough wavefronts for the chip all the same.  (bf16, 128 wide, us with one for every 4096 / 16384 / 32768 tiles there
 // are / with one always: 8 sequences x 32 key heads of 256 to 2048 keys 19.7 / 18.2 / 18.2 / 18.2, of 4096 62.5 / 55.3 / 59.3 / 59.2,
-// of 1000 to 8000 53.0 / 50.4 / 69.5 / 69.6; 4 x 8 of 16384 to 65536 73.8 / 68.9 / 71.5 / 82.8.)
+// of 1000 to 8000 53.0 / 50.4 / 69.5 / 69.6; 4 x 8 of 16384 to 65536 73.8 / 68.9 / 71.5 / 82.8.)  The tiles are those of the capacity, as the
+// host does not know the lengths: in a cache with much room few wavefronts take many tiles each (8 x 32 heads of 500 keys: 11.0 us with
+// room for 516, 11.9 for 4096, 15.8 for 16384; of 2000: 28.9 with room for 2016, 33.6 for 16384).
 inline int weight_tiles(long long tiles) {
   const long long most = tiles / 16384;
   return most < 1 ? 1 : (most > 8 ? 8 : (int)most);

@@ -14,10 +14,12 @@
 //
 // What bounds it.  Many rows over a long prefix: the products - 8 x 64 nodes, 32 heads of 128, behind 32768 keys, bf16: 332 us, 0.41 of
 // the matrix units' cycles (0.75 PFLOP/s of the call's own products, 0.94 of those on whole blocks); a tile's exponentials take as long
-// as its products and only partly run beside them.  Long histories: their bytes - an iteration over own keys takes 32 KB into a compute
-// unit in 3.7 k cycles, 4.7 TB/s over the chip.  Short calls: the first keys' way in (about 6 k cycles for 64 KB a compute unit, all at
-// once) and the second kernel (6 us, most of it latency).  8 x 64 nodes behind 2048 keys with 256 to 2048 of their own: 97 us, 203 MB;
-// one token for each of 8 sequences behind 2048: 30 us, 52 MB.
+// as its products and only partly run beside them.  Long histories: their bytes where a sequence's rows fill a block; where more rows
+// share a prefix, a block has more than a sequence's rows, and on own keys only the wavefronts that have rows multiply - two of eight for
+// 64 nodes: 8 x 64 nodes, 32 heads, each further 2048 own keys (268 MB) take 47 us (5.7 TB/s) in blocks of 64 rows, without a prefix,
+// and 57 us (4.7 TB/s) in blocks of 256, behind one of a single key.  Short calls: the first keys' way in (about 6 k cycles for 64 KB a
+// compute unit, all at once) and the second kernel (6 us, most of it latency).  8 x 64 nodes behind 2048 keys with 256 to 2048 of their
+// own: 95 to 102 us, 203 MB; one token for each of 8 sequences behind 2048: 30 us, 52 MB.
 #include <type_traits>
 #include <utility>
 
@@ -492,9 +494,10 @@ __global__ __launch_bounds__(64 * SH::NW, SH::WPE) void prefix_attn_kernel(Prefi
           for (int j = from; j < to; ++j)
 #pragma unroll
             for (int qt = 0; qt < QT; ++qt) {
-              // P is rounded to bf16, as the values are and as the result will be; FINE: P = hi + lo + rest, within 2^-24 of it.
-              // (Two parts, within 2^-16, where 256 rows share a prefix: 8 sequences x 64 nodes behind 2048 keys 93 us instead of 97,
-              // and a weight off by up to 2^-17 as soon as more than 128 rows are in the batch.)
+              // P is rounded to bf16, as the values are and as the result will be: 8 x 64 nodes behind 32768 keys 350 us, off from the
+              // exact result by 1.88e-3 of it; with another part 440 us and 1.66e-3, which is the result's own rounding.  FINE: P = hi + lo
+              // + rest, within 2^-24 of it.  (Two parts, within 2^-16, where 256 rows share a prefix: 8 x 64 nodes behind 2048 keys
+              // 89 to 101 us instead of 95 to 102, and a weight off by up to 2^-17 as soon as more than 128 rows are in the batch.)
               const float p0 = __builtin_amdgcn_exp2f(fmaf(s[qt][2 * j], p.sl2, -ms[qt]));
               const float p1 = __builtin_amdgcn_exp2f(fmaf(s[qt][2 * j + 1], p.sl2, -ms[qt]));
               const unsigned int h = __builtin_bit_cast(unsigned int, bf16x2{(__bf16)p0, (__bf16)p1});
