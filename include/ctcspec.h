@@ -554,6 +554,68 @@ int kv_evict(ctcspec_ctx* ctx, ctcspec_dtype dt, void* k_cache, void* v_cache, c
              int H_kv, int dh, int budget, int sink, int recent, int32_t* kept, float* weight_out, int32_t* pos_out,
              int32_t* ctx_len_out);
 
+/*
+ * A cache held in 4 bits.  A layer's keys and values as 4-bit codes with one scale byte for every 32 elements: 17 bytes where bf16 takes
+ * 64.  A row of dh elements is blocks = ceil(dh / 32) blocks, the last one filled up with zeros; an element x of a block stands for
+ *
+ *   x^ = c * 2^(s - 127)     c: sign (bit 3) and 0 0.5 1 1.5 2 3 4 6 (bits 0 to 2), the even element in the low half of its byte
+ *                            s: the block's scale byte (the E2M1 and E8M0 formats of the OCP microscaling specification)
+ *
+ * The calls that fill the cache choose for s the smallest of 2 to 252 with |x| <= 7 * 2^(s - 127) in the block, for c the nearest value -
+ * of two the even code; beyond 6: 6; no sign on what rounds to 0 -: x^ is off by at most 2^(s - 127) (for magnitudes up to 7 * 2^125) and
+ * exact in bf16.  A block with an infinity or NaN has s = 255 and stands for NaN in all its elements.
+ *
+ *   k_codes, v_codes    bytes, 16-byte aligned: a sequence's block is [H_kv][kv_cap][16 * blocks]
+ *   k_scales, v_scales  bytes, 4-byte aligned:  a sequence's block is [H_kv][kv_cap][blocks]
+ *   kv_off              [B] int64 device: sequence b's block starts kv_off[b] ROWS behind the base pointers - in all four buffers
+ *   ctx_len             [B] int32 device: rows of every head that are filled; those behind may hold anything
+ *
+ * The struct and its pointers are read during the call; only what they point to has to live on.
+ */
+typedef struct {
+  void* k_codes;
+  void* k_scales;
+  void* v_codes;
+  void* v_scales;
+} ctcspec_q4_cache;
+
+/*
+ * kv_append_q4 - the rows of a prompt, or those of a cache that was held in full so far, join a layer's 4-bit cache:
+ *   for j = 0..n_rows[b]-1:  cache row ctx_len[b] + j of every key head  <-  row j
+ *   ctx_len_out[b] = min(ctx_len[b] + n_rows[b], kv_cap)
+ * Rows that would fall beyond kv_cap are dropped, as in kv_commit; no other byte of the cache is written.
+ *
+ * dt              element type of the rows
+ * k_rows, v_rows  [B,H_kv,max_rows,dh] 16-byte aligned; rows from n_rows[b] on are not read
+ * n_rows          [B] int32 device (counts beyond max_rows count as max_rows, negative ones as 0)
+ * ctx_len_out     [B] int32 out or NULL; must not be the ctx_len buffer itself
+ *
+ * kv_commit_q4 - the accepted path's keys and values join it: kv_commit for such a cache, with its arguments.  Entries of accept_nodes that
+ * are no node write nothing; ctx_len_out counts their rows, as there.
+ *
+ * k_tree, v_tree  [B,H_kv,max_nodes,dh] 16-byte aligned
+ *
+ * kv_read_q4 - rows of the cache as what they stand for, for the calls that take keys and values in full:
+ *   for j = 0..n_rows[b]-1:  row j  <-  cache row first[b] + j of every key head, where 0 <= first[b] + j < kv_cap
+ * No other row of k_rows and v_rows is written.
+ *
+ * first, n_rows   [B] int32 device (counts beyond max_rows count as max_rows)
+ * out_dt          element type of k_rows, v_rows [B,H_kv,max_rows,dh], 16-byte aligned (either type holds the values exactly)
+ *
+ * Limits of the three: dh % 8 == 0, dh <= CTCSPEC_MAX_HEAD_DIM; B, H_kv (max_heads), dh, and max_nodes of kv_commit_q4 within the
+ * context's limits; kv_cap, max_rows <= 2^30; T <= CTCSPEC_MAX_SLOTS.
+ */
+int kv_append_q4(ctcspec_ctx* ctx, ctcspec_dtype dt, const void* k_rows, const void* v_rows, const int32_t* n_rows, int max_rows,
+                 const ctcspec_q4_cache* cache, const int64_t* kv_off, const int32_t* ctx_len, int kv_cap, int B, int H_kv,
+                 int dh, int32_t* ctx_len_out);
+
+int kv_commit_q4(ctcspec_ctx* ctx, ctcspec_dtype dt, const void* k_tree, const void* v_tree, const int32_t* accept_len,
+                 const int32_t* accept_nodes, int T, const ctcspec_q4_cache* cache, const int64_t* kv_off, const int32_t* ctx_len,
+                 int kv_cap, int B, int H_kv, int dh, int max_nodes, int32_t* ctx_len_out);
+
+int kv_read_q4(ctcspec_ctx* ctx, const ctcspec_q4_cache* cache, const int64_t* kv_off, const int32_t* first, const int32_t* n_rows,
+               int max_rows, int kv_cap, int B, int H_kv, int dh, ctcspec_dtype out_dt, void* k_rows, void* v_rows);
+
 #ifdef __cplusplus
 }
 #endif

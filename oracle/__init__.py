@@ -25,6 +25,7 @@ from .draft_layer import draft_layer, draft_layer_qkv, draft_layer_attend, rms_n
 from .sum_score import ctc_sequence_logprob, sum_scores, ranks_desc  # noqa: F401
 from .ctc_loss import ctc_alpha_beta, ctc_loss_and_grad  # noqa: F401
 from .long_history import prefix_attention, weight_update, evict  # noqa: F401
+from .q4_cache import q4_decode, q4_encode, window_attention  # noqa: F401
 from .sampling import (  # noqa: F401
     target_probs,
     sample_token,

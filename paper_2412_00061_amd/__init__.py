@@ -19,8 +19,11 @@ from .binding import (  # noqa: F401
     ctc_sum_score,
     draft_layer_forward,
     draft_layer_workspace_bytes,
+    kv_append_q4,
     kv_commit,
+    kv_commit_q4,
     kv_evict,
+    kv_read_q4,
     kv_weight_update,
     layer_weights,
     library_path,
@@ -28,6 +31,7 @@ from .binding import (  # noqa: F401
     prefix_verify_attn,
     prefix_verify_attn_workspace_bytes,
     prepared,
+    q4_cache,
     tree_verify_attn,
     verify_head_argmax,
 )

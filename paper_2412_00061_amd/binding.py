@@ -19,6 +19,7 @@ EXPORTS = (
     "ctc_sum_score", "ctc_raw_tree", "ctc_loss_workspace_bytes", "ctc_loss", "verify_sample_tokens",
     "ctc_draft_topk_noalloc", "ctcspec_defer_topk_merge", "ctcspec_flush", "ctcspec_stream_probe",
     "prefix_verify_attn_workspace_bytes", "prefix_verify_attn", "kv_weight_update", "kv_evict",
+    "kv_append_q4", "kv_commit_q4", "kv_read_q4",
 )
 
 CTCSPEC_F32, CTCSPEC_BF16 = 0, 1
@@ -35,6 +36,10 @@ class _Limits(ctypes.Structure):
 
 class _LayerWeights(ctypes.Structure):
     _fields_ = [(n, c_void_p) for n in ("ln1", "wqkv", "wo", "ln2", "wgu", "wd")]
+
+
+class _Q4Cache(ctypes.Structure):
+    _fields_ = [(n, c_void_p) for n in ("k_codes", "k_scales", "v_codes", "v_scales")]
 
 
 def library_path() -> str:
@@ -117,6 +122,14 @@ def load_library():
                                      [c_float] + [c_void_p] * 3)
     lib.kv_evict.restype = c_int
     lib.kv_evict.argtypes = [c_void_p, c_int] + [c_void_p] * 4 + [c_int] + [c_void_p] * 3 + [c_int] * 6 + [c_void_p] * 4
+    lib.kv_append_q4.restype = c_int
+    lib.kv_append_q4.argtypes = ([c_void_p, c_int] + [c_void_p] * 3 + [c_int, POINTER(_Q4Cache)] + [c_void_p] * 2 + [c_int] * 4 +
+                                 [c_void_p])
+    lib.kv_commit_q4.restype = c_int
+    lib.kv_commit_q4.argtypes = ([c_void_p, c_int] + [c_void_p] * 4 + [c_int, POINTER(_Q4Cache)] + [c_void_p] * 2 + [c_int] * 5 +
+                                 [c_void_p])
+    lib.kv_read_q4.restype = c_int
+    lib.kv_read_q4.argtypes = [c_void_p, POINTER(_Q4Cache)] + [c_void_p] * 3 + [c_int] * 6 + [c_void_p] * 2
     _LIB = lib
     return lib
 
@@ -563,4 +576,60 @@ def kv_evict(ctx, k_cache, v_cache, kv_off, ctx_len, kv_cap, dh, weight, budget,
         kv_cap, _ptr(weight, torch.float32), _ptr(pos, torch.int32), _ptr(next_pos, torch.int32), B, H_kv, dh, budget, sink, recent,
         _ptr(res["kept"]), _ptr(res["weight"]), _ptr(res.get("pos")), _ptr(res["ctx_len"]))
     ctx._check(rc, "kv_evict")
+    return res
+
+
+def q4_cache(k_codes, k_scales, v_codes, v_scales):
+    """The C struct of device pointers that the calls on a 4-bit cache take, from four uint8 tensors: codes of 16 bytes and scales of one
+    for every 32 elements of a row (see ctcspec.h), any number of rows."""
+    tensors = (k_codes, k_scales, v_codes, v_scales)
+    st = _Q4Cache(*[_ptr(t, torch.uint8).value for t in tensors])
+    if not k_codes.numel() == v_codes.numel() == 16 * k_scales.numel() == 16 * v_scales.numel():
+        raise CtcspecError("a 4-bit cache has 16 bytes of codes for every scale, as many of keys as of values")
+    st._keep = tensors
+    return st
+
+
+def _q4_ref(cache):
+    if not isinstance(cache, _Q4Cache):
+        raise CtcspecError("expected a cache made by q4_cache()")
+    return ctypes.byref(cache)
+
+
+def kv_append_q4(ctx, k_rows, v_rows, n_rows, cache, kv_off, ctx_len, kv_cap, *, ctx_len_out=None):
+    """Append rows 0..n_rows[b]-1 of k_rows/v_rows [B,H_kv,max_rows,dh] to the 4-bit cache in place; ctx_len_out [B] int32 receives
+    the new lengths."""
+    B, H_kv, max_rows, dh = k_rows.shape
+    _shaped("v_rows", v_rows, k_rows.shape)
+    for name, t in (("n_rows", n_rows), ("kv_off", kv_off), ("ctx_len", ctx_len)) + ((("ctx_len_out", ctx_len_out),) if ctx_len_out is not None else ()):
+        _shaped(name, t, (B,))
+    rc = ctx.lib.kv_append_q4(ctx.handle, _dtype_code(k_rows), _ptr(k_rows), _ptr(v_rows, k_rows.dtype), _ptr(n_rows, torch.int32), max_rows,
+                              _q4_ref(cache), _ptr(kv_off, torch.int64), _ptr(ctx_len, torch.int32), kv_cap, B, H_kv, dh,
+                              _ptr(ctx_len_out, torch.int32))
+    ctx._check(rc, "kv_append_q4")
+
+
+def kv_commit_q4(ctx, k_tree, v_tree, accept_len, accept_nodes, cache, kv_off, ctx_len, kv_cap, *, ctx_len_out=None):
+    """Append the accepted path's rows of k_tree/v_tree [B,H_kv,max_nodes,dh] to the 4-bit cache in place."""
+    B, H_kv, max_nodes, dh = k_tree.shape
+    _shaped("v_tree", v_tree, k_tree.shape)
+    T = _shaped("accept_nodes", accept_nodes, (B, accept_nodes.shape[-1])).shape[1] - 1
+    for name, t in (("accept_len", accept_len), ("kv_off", kv_off), ("ctx_len", ctx_len)) + ((("ctx_len_out", ctx_len_out),) if ctx_len_out is not None else ()):
+        _shaped(name, t, (B,))
+    rc = ctx.lib.kv_commit_q4(ctx.handle, _dtype_code(k_tree), _ptr(k_tree), _ptr(v_tree, k_tree.dtype), _ptr(accept_len, torch.int32),
+                              _ptr(accept_nodes, torch.int32), T, _q4_ref(cache), _ptr(kv_off, torch.int64), _ptr(ctx_len, torch.int32), kv_cap,
+                              B, H_kv, dh, max_nodes, _ptr(ctx_len_out, torch.int32))
+    ctx._check(rc, "kv_commit_q4")
+
+
+def kv_read_q4(ctx, cache, kv_off, first, n_rows, max_rows, kv_cap, H_kv, dh, *, out_dtype=torch.bfloat16, out=None):
+    """Rows first[b]..first[b]+n_rows[b]-1 of the 4-bit cache as what they stand for -> dict(k, v [B,H_kv,max_rows,dh]); other rows of
+    these are left as they are."""
+    B = kv_off.shape[0]
+    for name, t in (("kv_off", kv_off), ("first", first), ("n_rows", n_rows)):
+        _shaped(name, t, (B,))
+    res = {n: _out(out, n, (B, H_kv, max_rows, dh), out_dtype, kv_off.device) for n in ("k", "v")}
+    rc = ctx.lib.kv_read_q4(ctx.handle, _q4_ref(cache), _ptr(kv_off, torch.int64), _ptr(first, torch.int32), _ptr(n_rows, torch.int32), max_rows,
+                            kv_cap, B, H_kv, dh, _dtype_code(res["k"]), _ptr(res["k"]), _ptr(res["v"]))
+    ctx._check(rc, "kv_read_q4")
     return res

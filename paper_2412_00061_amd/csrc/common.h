@@ -106,6 +106,7 @@ hipError_t prepare_verify_sample();
 hipError_t prepare_prefix_attn();
 hipError_t prepare_kv_weight();
 hipError_t prepare_kv_evict();
+hipError_t prepare_kv_q4();
 
 #define CTCSPEC_REQUIRE(ctx, cond, code, ...) \
   do {                                        \

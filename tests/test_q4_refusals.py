@@ -1,0 +1,67 @@
+"""What the calls on a 4-bit cache refuse, before anything reaches the GPU."""
+import ctypes
+
+import pytest
+import torch
+
+import paper_2412_00061_amd as pkg
+from host_context import HostContext
+from paper_2412_00061_amd import binding
+
+P = 4096  # an address, 16-byte aligned: never read on the host
+INVALID, UNSUPPORTED = -1, -2
+
+
+def cache(k_codes=P, k_scales=P, v_codes=P, v_scales=P):
+    return ctypes.byref(binding._Q4Cache(k_codes, k_scales, v_codes, v_scales))
+
+
+APPEND = dict(dt=1, k=P, v=P, n=P, max_rows=10, cache=cache(), off=P, ctx=P, cap=100, B=2, H=4, dh=64, out=None)
+COMMIT = dict(dt=1, k=P, v=P, alen=P, path=P, T=4, cache=cache(), off=P, ctx=P, cap=100, B=2, H=4, dh=64, N=20, out=None)
+READ = dict(cache=cache(), off=P, first=P, n=P, max_rows=10, cap=100, B=2, H=4, dh=64, dt=1, k=P, v=P)
+CALLS = {"kv_append_q4": APPEND, "kv_commit_q4": COMMIT, "kv_read_q4": READ}
+
+BAD = [(name, key, None, INVALID, "null pointer") for name, args in CALLS.items() for key in args
+       if key in ("k", "v", "n", "alen", "path", "cache", "off", "ctx", "first")]
+BAD += [(name, "cache", cache(**{part: None}), INVALID, "null pointer") for name in CALLS for part in ("k_codes", "k_scales", "v_codes", "v_scales")]
+BAD += [(name, key, value, INVALID, "positive") for name, args in CALLS.items() for key in ("B", "H", "dh", "cap", "max_rows", "N", "T") if key in args
+        for value in (0, -3)]
+BAD += [(name, "dt", 2, INVALID, "element type") for name in CALLS]
+BAD += [(name, "dh", value, UNSUPPORTED, "multiple of 8") for name in CALLS for value in (12, 136)]
+BAD += [(name, key, value, UNSUPPORTED, "limits") for name, args in CALLS.items()
+        for key, value in (("B", 9), ("H", 9), ("dh", 128), ("cap", (1 << 30) + 1), ("max_rows", (1 << 30) + 1), ("N", 65)) if key in args]
+BAD += [(name, key, P + 8, INVALID, "aligned") for name in CALLS for key in ("k", "v")]
+BAD += [(name, "cache", cache(**{part: P + 4}), INVALID, "aligned") for name in CALLS for part in ("k_codes", "v_codes")]
+BAD += [("kv_commit_q4", "T", 9, UNSUPPORTED, "T <= 8"), ("kv_append_q4", "out", P, INVALID, "ctx_len_out"), ("kv_commit_q4", "out", P, INVALID, "ctx_len_out")]
+
+
+@pytest.mark.parametrize("name,key,value,code,text", BAD)
+def test_refusals(name, key, value, code, text):
+    args = dict(CALLS[name], **{key: value})
+    HostContext(max_head_dim=64 if key == "dh" else 128).refuses(name, list(args.values()), code, text)
+
+
+def test_no_context():
+    lib = pkg.load_library()
+    for name, args in CALLS.items():
+        assert getattr(lib, name)(None, *args.values()) == INVALID
+
+
+def test_the_binding_looks_at_shapes(monkeypatch):
+    monkeypatch.setattr(binding, "_ptr", lambda t, dtype=None: None if t is None else ctypes.c_void_p(t.data_ptr()))
+    u8 = lambda n: torch.zeros(n, dtype=torch.uint8)  # noqa: E731
+    i32 = lambda n: torch.zeros(n, dtype=torch.int32)  # noqa: E731
+    with pytest.raises(pkg.CtcspecError, match="16 bytes of codes"):
+        pkg.q4_cache(u8(64), u8(4), u8(64), u8(5))
+    c, off = pkg.q4_cache(u8(64), u8(4), u8(64), u8(4)), torch.zeros(2, dtype=torch.int64)
+    rows = torch.zeros((2, 1, 1, 32))
+    with pytest.raises(pkg.CtcspecError, match="n_rows"):
+        pkg.kv_append_q4(None, rows, rows, i32(3), c, off, i32(2), 2)
+    with pytest.raises(pkg.CtcspecError, match="v_rows"):
+        pkg.kv_append_q4(None, rows, rows[:1], i32(2), c, off, i32(2), 2)
+    with pytest.raises(pkg.CtcspecError, match="q4_cache"):
+        pkg.kv_append_q4(type("C", (), {"lib": type("L", (), {"kv_append_q4": None}), "handle": None}), rows, rows, i32(2), u8(64), off, i32(2), 2)
+    with pytest.raises(pkg.CtcspecError, match="accept_len"):
+        pkg.kv_commit_q4(None, rows, rows, i32(1), torch.zeros((2, 5), dtype=torch.int32), c, off, i32(2), 2)
+    with pytest.raises(pkg.CtcspecError, match="first"):
+        pkg.kv_read_q4(None, c, off, i32(1), i32(2), 1, 2, 1, 32)
