@@ -19,7 +19,7 @@
  *      ctc_collapse_tree, ctc_raw_tree
  *      tree_verify_attn, draft_layer_forward
  *      verify_head_argmax
- *      calls of prefix_verify_attn that share a workspace
+ *      calls of prefix_verify_attn, of q4_verify_attn that share a workspace
  *    Two calls of one of these lines race on it.  Every other call uses none.  (Ordering a call behind those
  *    whose outputs it reads is the caller's part, as everywhere.)
  *  - Row-major, innermost index last, no padding unless stated.  bf16 is the upper half of an IEEE
@@ -615,6 +615,50 @@ int kv_commit_q4(ctcspec_ctx* ctx, ctcspec_dtype dt, const void* k_tree, const v
 
 int kv_read_q4(ctcspec_ctx* ctx, const ctcspec_q4_cache* cache, const int64_t* kv_off, const int32_t* first, const int32_t* n_rows,
                int max_rows, int kv_cap, int B, int H_kv, int dh, ctcspec_dtype out_dt, void* k_rows, void* v_rows);
+
+/*
+ * q4_verify_attn - one attention layer of the verification pass (as tree_verify_attn) over a cache held in 4 bits, with grouped heads as
+ * prefix_verify_attn has them, and where the caller wants it with a sliding window: with window > 0 a row sees the last `window`
+ * positions, its own among them, and the first `sink` of its sequence; with window = 0 all.  Cached row j has position j, node i of
+ * sequence b position ctx_len[b] + node_depth[b,i].
+ *
+ *   keys(b, i) = the cached rows j < ctx_len[b], and the tree nodes j < n_nodes[b] with bit j of anc_mask row i set; of these with a window
+ *                those at positions above (ctx_len[b] + node_depth[b,i]) - window or below sink
+ *   lse[b,h,i]   = log sum_{j in keys} exp(scale * q[b,h,i,:] . key_j)
+ *   out[b,h,i,:] = sum_{j in keys} exp(scale * q[b,h,i,:] . key_j - lse[b,h,i]) * value_j
+ *
+ * - keys and values of cached rows being what their codes stand for.  A window skips the cached rows that no row sees; its cost does not
+ * grow with the history.  max_nodes = 1 is plain decoding.
+ * A row that sees no key (no cached row, an empty mask row), or none whose score is above -infinity, has out = 0 and lse = -inf.  Rows
+ * i >= n_nodes[b] are not written; n_nodes[b] may be 0.  No positional encoding is applied.  The lengths are read on the device; those
+ * beyond their capacity count as the capacity, negative ones as 0.  A value that is infinite or not a number reaches the rows that see its
+ * key and no other row; a score that is, likewise.
+ *
+ * dt            element type of q, k_tree, v_tree: CTCSPEC_BF16
+ * q             [B,H,max_nodes,dh]; k_tree, v_tree [B,H_kv,max_nodes,dh]
+ * cache, kv_off, ctx_len, kv_cap   the 4-bit cache as kv_append_q4 and kv_commit_q4 leave it; its pointers may be NULL with kv_cap 0
+ * n_nodes, anc_mask   as for tree_verify_attn
+ * node_depth    [B,max_nodes] int32 device, as written by ctc_collapse_tree (depths outside 0..max_nodes-1 count as the nearer end); NULL
+ *               only without a window
+ * scale         positive, at most 2e38
+ * window, sink  >= 0
+ * workspace     device scratch of at least q4_verify_attn_workspace_bytes(B, H, H_kv, dh, max_nodes) bytes, owned by the caller, contents
+ *               undefined afterwards; calls that share it must not overlap.  Bytes for some B and max_nodes serve every smaller B and
+ *               max_nodes
+ * out_dt, out   [B,H,max_nodes,dh] out: CTCSPEC_F32 (weights carried with 24 bits) or CTCSPEC_BF16 (weights rounded to bf16 as well)
+ * lse           [B,H,max_nodes] float out or NULL
+ * Pointers 16-byte aligned (scales, ctx_len, n_nodes, node_depth, kv_off, anc_mask and lse as their types are).
+ * Limits: dh % 8 == 0, dh <= CTCSPEC_MAX_HEAD_DIM, max_nodes <= CTCSPEC_MAX_NODES, B <= 64; B, H, dh, max_nodes within the context's
+ * limits; H % H_kv == 0; kv_cap and max_nodes * H / H_kv <= 2^30; iterations over the keys (of 128, for a block of 32 or 64 rows) are
+ * counted in 32 bits: 64 sequences x 128 nodes x 32 heads may have 3e7 cached rows, and a call that could need more is refused
+ * (CTCSPEC_EUNSUPPORTED).  The same bits on every run.
+ */
+size_t q4_verify_attn_workspace_bytes(int B, int H, int H_kv, int dh, int max_nodes);
+
+int q4_verify_attn(ctcspec_ctx* ctx, ctcspec_dtype dt, const void* q, const ctcspec_q4_cache* cache, const int64_t* kv_off,
+                   const int32_t* ctx_len, int kv_cap, const void* k_tree, const void* v_tree, const int32_t* n_nodes,
+                   const int32_t* node_depth, const uint64_t* anc_mask, int B, int H, int H_kv, int dh, int max_nodes, float scale,
+                   int window, int sink, void* workspace, size_t workspace_bytes, ctcspec_dtype out_dt, void* out, float* lse);
 
 #ifdef __cplusplus
 }

@@ -32,6 +32,8 @@ from .binding import (  # noqa: F401
     prefix_verify_attn_workspace_bytes,
     prepared,
     q4_cache,
+    q4_verify_attn,
+    q4_verify_attn_workspace_bytes,
     tree_verify_attn,
     verify_head_argmax,
 )

@@ -19,7 +19,7 @@ EXPORTS = (
     "ctc_sum_score", "ctc_raw_tree", "ctc_loss_workspace_bytes", "ctc_loss", "verify_sample_tokens",
     "ctc_draft_topk_noalloc", "ctcspec_defer_topk_merge", "ctcspec_flush", "ctcspec_stream_probe",
     "prefix_verify_attn_workspace_bytes", "prefix_verify_attn", "kv_weight_update", "kv_evict",
-    "kv_append_q4", "kv_commit_q4", "kv_read_q4",
+    "kv_append_q4", "kv_commit_q4", "kv_read_q4", "q4_verify_attn_workspace_bytes", "q4_verify_attn",
 )
 
 CTCSPEC_F32, CTCSPEC_BF16 = 0, 1
@@ -130,6 +130,11 @@ def load_library():
                                  [c_void_p])
     lib.kv_read_q4.restype = c_int
     lib.kv_read_q4.argtypes = [c_void_p, POINTER(_Q4Cache)] + [c_void_p] * 3 + [c_int] * 6 + [c_void_p] * 2
+    lib.q4_verify_attn_workspace_bytes.restype = c_size_t
+    lib.q4_verify_attn_workspace_bytes.argtypes = [c_int] * 5
+    lib.q4_verify_attn.restype = c_int
+    lib.q4_verify_attn.argtypes = ([c_void_p, c_int, c_void_p, POINTER(_Q4Cache)] + [c_void_p] * 2 + [c_int] + [c_void_p] * 5 + [c_int] * 5 +
+                                   [c_float, c_int, c_int, c_void_p, c_size_t, c_int] + [c_void_p] * 2)
     _LIB = lib
     return lib
 
@@ -632,4 +637,34 @@ def kv_read_q4(ctx, cache, kv_off, first, n_rows, max_rows, kv_cap, H_kv, dh, *,
     rc = ctx.lib.kv_read_q4(ctx.handle, _q4_ref(cache), _ptr(kv_off, torch.int64), _ptr(first, torch.int32), _ptr(n_rows, torch.int32), max_rows,
                             kv_cap, B, H_kv, dh, _dtype_code(res["k"]), _ptr(res["k"]), _ptr(res["v"]))
     ctx._check(rc, "kv_read_q4")
+    return res
+
+
+def q4_verify_attn_workspace_bytes(B, H, H_kv, dh, max_nodes) -> int:
+    return int(load_library().q4_verify_attn_workspace_bytes(B, H, H_kv, dh, max_nodes))
+
+
+def q4_verify_attn(ctx, q, cache, kv_off, ctx_len, kv_cap, k_tree, v_tree, n_nodes, anc_mask, scale, *, node_depth=None, window=0, sink=0,
+                   out_dtype=torch.float32, want_lse=False, workspace=None, out=None):
+    """q [B,H,max_nodes,dh], k_tree/v_tree [B,H_kv,max_nodes,dh] bf16, a 4-bit cache; with window > 0 (which needs node_depth [B,max_nodes])
+    rows see the last `window` positions and the first `sink` -> dict(out [B,H,max_nodes,dh][, lse [B,H,max_nodes]])."""
+    B, H, N, dh = q.shape
+    H_kv, dev = k_tree.shape[1], q.device
+    _shaped("k_tree", k_tree, (B, H_kv, N, dh)), _shaped("v_tree", v_tree, (B, H_kv, N, dh))
+    _shaped("anc_mask", anc_mask, (B, N, (N + 63) // 64))
+    for name, t in (("kv_off", kv_off), ("ctx_len", ctx_len), ("n_nodes", n_nodes)):
+        _shaped(name, t, (B,))
+    if node_depth is not None:
+        _shaped("node_depth", node_depth, (B, N))
+    if workspace is None:
+        workspace = _workspace(ctx, q4_verify_attn_workspace_bytes(B, H, H_kv, dh, N), dev)
+    res = {"out": _out(out, "out", (B, H, N, dh), out_dtype, dev)}
+    if want_lse:
+        res["lse"] = _out(out, "lse", (B, H, N), torch.float32, dev)
+    rc = ctx.lib.q4_verify_attn(
+        ctx.handle, _dtype_code(q), _ptr(q), _q4_ref(cache), _ptr(kv_off, torch.int64), _ptr(ctx_len, torch.int32), kv_cap,
+        _ptr(k_tree, q.dtype), _ptr(v_tree, q.dtype), _ptr(n_nodes, torch.int32), _ptr(node_depth, torch.int32), _ptr(anc_mask, torch.int64),
+        B, H, H_kv, dh, N, c_float(scale), window, sink, _ptr(workspace, torch.uint8), workspace.numel(), _dtype_code(res["out"]),
+        _ptr(res["out"]), _ptr(res.get("lse")))
+    ctx._check(rc, "q4_verify_attn")
     return res

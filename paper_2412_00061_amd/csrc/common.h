@@ -107,6 +107,7 @@ hipError_t prepare_prefix_attn();
 hipError_t prepare_kv_weight();
 hipError_t prepare_kv_evict();
 hipError_t prepare_kv_q4();
+hipError_t prepare_q4_attn();
 
 #define CTCSPEC_REQUIRE(ctx, cond, code, ...) \
   do {                                        \

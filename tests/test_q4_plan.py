@@ -1,0 +1,67 @@
+"""q4_plan.h, asked on the CPU: which tiles of keys a window leaves, and that partial results lie inside the workspace."""
+import functools
+import os
+import subprocess
+import tempfile
+
+import launch_plans
+
+PROGRAM = r"""
+#include <stdio.h>
+#include "q4_plan.h"
+using namespace ctcspec;
+int main() {
+  char what;
+  long long a, b, c, d, e;
+  while (scanf(" %c %lld %lld %lld %lld %lld", &what, &a, &b, &c, &d, &e) == 6) {
+    if (what == 't') {
+      const Q4Tiles t = q4_tiles(a, b, c);
+      printf("%d %d %d\n", t.lead, t.gap, t.count);
+    } else if (what == 'f') {
+      printf("%d 0 0\n", (int)q4_units_fit(a, b, c, d, e));
+    } else {
+      const Q4Workspace w = q4_workspace(a, b, c, d, e);
+      printf("%d %zu %zu\n", w.rows, w.o, w.total);
+    }
+  }
+}
+"""
+
+
+@functools.lru_cache(maxsize=None)
+def _program():
+    at = tempfile.mkdtemp(prefix="q4_plan")
+    with open(os.path.join(at, "plan.cpp"), "w") as f:
+        f.write(PROGRAM)
+    subprocess.run(["g++", "-std=c++17", "-O1", "-I", launch_plans.CSRC, os.path.join(at, "plan.cpp"), "-o", os.path.join(at, "plan")], check=True)
+    return os.path.join(at, "plan")
+
+
+def ask(lines):
+    text = "\n".join(" ".join(map(str, line)) for line in lines)
+    out = subprocess.run([_program()], input=text, capture_output=True, text=True, check=True).stdout
+    return [tuple(map(int, line.split())) for line in out.split("\n") if line]
+
+
+def test_a_window_keeps_every_tile_that_a_row_sees():
+    cases = [(L, W, S) for L in (0, 1, 31, 32, 33, 64, 100, 999, 1024) for W in (0, 1, 2, 31, 32, 33, 500, 999, 1000, 5000) for S in (0, 1, 32, 33, 700, 9999)]
+    for (L, W, S), (lead, gap, count) in zip(cases, ask([("t", *c, 0, 0) for c in cases])):
+        tiles = {x if x < lead else x + gap for x in range(count)}
+        seen = {j // 32 for j in range(L) if not W or j > L - W or j < S}  # (a row at a later position sees fewer)
+        assert seen <= tiles <= set(range((L + 31) // 32)), (L, W, S)
+        assert len(tiles) == count <= len(seen) + 1  # (a window of 1 sees no cached row, its tile is kept)
+
+
+def test_units_are_counted_for_the_largest_lengths():
+    fits = ask([("f", 64, 32, 128, 30_000_000, 128), ("f", 64, 32, 128, 40_000_000, 128), ("f", 1, 1, 1, 1 << 30, 1), ("f", 1, 1, 1, (1 << 30) + 1, 1),
+                ("f", 1, 1, (1 << 30) + 1, 8, 128)])
+    assert [f[0] for f in fits] == [1, 0, 1, 0, 0]
+
+
+def test_workspace_has_room_for_every_partial_result():
+    for B, H, Hkv, dh, N in ((1, 1, 1, 8, 1), (8, 32, 32, 128, 64), (64, 40, 8, 96, 128), (3, 32, 1, 64, 1)):
+        (rows, o, total), = ask([("w", B, H, Hkv, dh, N)])
+        seq = N * H // Hkv
+        slots = 512 + Hkv * B * -(-seq // rows)
+        assert rows == (32 if seq <= 32 else 64) and o == 0
+        assert total >= slots * (rows * (max(64, -(-dh // 32) * 32) + 2) + 1) * 4
