@@ -660,6 +660,39 @@ int q4_verify_attn(ctcspec_ctx* ctx, ctcspec_dtype dt, const void* q, const ctcs
                    const int32_t* node_depth, const uint64_t* anc_mask, int B, int H, int H_kv, int dh, int max_nodes, float scale,
                    int window, int sink, void* workspace, size_t workspace_bytes, ctcspec_dtype out_dt, void* out, float* lse);
 
+/*
+ * verify_sample_filtered - verify_sample_tokens under sampling filters, each sequence with its own: the target's token after every node is
+ * drawn from what temperature, top-k, top-p and min-p leave of its distribution.  For sequence b and node i < n_nodes[b], with the
+ * tokens in the order of falling logits - equal ones by their index - and w[v] = exp((logits[b,i,v] - max) / temperature[b]):
+ *
+ *   top_k   keeps the first top_k[b] tokens (0 or less, or V and more: all)
+ *   top_p   of these keeps a token if the weights before it sum up to less than top_p[b] times the sum over the top_k tokens; the first one
+ *           always (1 or more: all)
+ *   min_p   keeps the tokens with w[v] >= min_p[b] (0 or less: all; more than 1 counts as 1)
+ *   target_sampled[b,i] = the first kept v, in vocabulary order, with sum_{kept u <= v} w[u] > uniforms[b,i] * sum_{kept u} w[u]
+ *   n_kept[b,i]  = the number of kept tokens
+ *   logp[b,i]    = log (w[target_sampled] / sum_{kept u} w[u])
+ *
+ * A temperature of 0 or less takes the first token of the order (n_kept 1, logp 0), whatever the filters say.  Weights and sums are held in
+ * 64 bits: cut-offs and token are the exact ones unless a border lies within rounding (about 1e-13 of the sums; for top_p of the weights,
+ * relative to the largest, in whole multiples of 2^-45).  A logit that is -infinity or not a number is never kept; +infinity takes all (equal ones alike); where no
+ * logit is above -infinity the outputs are -1, 0 and -infinity.  Rows i >= n_nodes[b] receive -1, 0 and 0.
+ *
+ * logits         [B,max_nodes,V] float device in, 16-byte aligned
+ * n_nodes        [B] int32 device in
+ * uniforms       [B,max_nodes] float device in: uniform numbers in [0, 1), drawn by the caller
+ * temperature    [B] float device in (not a number counts as 0)
+ * top_k          [B] int32 device in or NULL: no such filter
+ * top_p, min_p   [B] float device in or NULL: no such filter (not a number: none for that sequence)
+ * target_sampled [B,max_nodes] int32 device out
+ * n_kept         [B,max_nodes] int32 device out or NULL
+ * logp           [B,max_nodes] float device out or NULL
+ * Limits: V <= 262144, B <= 65535.  The same bits on every run.
+ */
+int verify_sample_filtered(ctcspec_ctx* ctx, const float* logits, const int32_t* n_nodes, const float* uniforms,
+                           const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p, int B,
+                           int max_nodes, int V, int32_t* target_sampled, int32_t* n_kept, float* logp);
+
 #ifdef __cplusplus
 }
 #endif

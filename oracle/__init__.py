@@ -30,6 +30,8 @@ from .sampling import (  # noqa: F401
     target_probs,
     sample_token,
     sample_nodes,
+    filter_tokens,
+    sample_filtered,
     accept_sampled,
     sec2_rule_distribution,
     sample_and_match_distribution,

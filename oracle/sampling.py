@@ -49,6 +49,47 @@ def sample_nodes(logits, n_nodes, uniforms, temperature):
     return out
 
 
+def filter_tokens(logits_row, temperature, top_k=0, top_p=1.0, min_p=0.0):
+    """Which tokens the sampling filters keep, and the weights of all: (kept, ascending ids; w = exp((logit - max) / temperature)).
+    Each filter keeps a beginning of the order by falling logit (equal ones by id): the first top_k (0 or less: all); of these a token if
+    the weights before it sum up to less than top_p of those of the top_k tokens (the first always; 1 or more: all); those with
+    w >= min_p (more than 1 counts as 1).  A temperature of 0 or less keeps the first alone.  -infinity and NaN are never kept, +infinity
+    takes all."""
+    z = np.asarray(logits_row, dtype=np.float64)
+    z = np.where(np.isnan(z), -np.inf, z)
+    top = z.max()
+    w = np.zeros_like(z)
+    if top == -np.inf:
+        return np.empty(0, dtype=np.int64), w
+    order = np.lexsort((np.arange(len(z)), -z))
+    order = order[z[order] > -np.inf]
+    if not temperature > 0:
+        w[order[0]] = 1.0
+        return order[:1], w
+    w[z == top] = 1.0
+    if top < np.inf:
+        w[order] = np.exp((z[order] - top) / float(temperature))
+    if top_k > 0:
+        order = order[:top_k]
+    if top_p < 1:
+        before = np.cumsum(w[order]) - w[order]
+        order = order[(before < float(top_p) * w[order].sum()) | (np.arange(len(order)) == 0)]
+    order = order[(w[order] >= min(float(min_p), 1.0)) if min_p > 0 else slice(None)]
+    return np.sort(order), w
+
+
+def sample_filtered(logits_row, u, temperature, top_k=0, top_p=1.0, min_p=0.0):
+    """(token, tokens kept, log of its probability among them): the first kept token, in vocabulary order, at which the kept
+    weights so far exceed u of their sum; (-1, 0, -inf) where nothing is kept."""
+    kept, w = filter_tokens(logits_row, temperature, top_k, top_p, min_p)
+    if not len(kept):
+        return -1, 0, -np.inf
+    cum = np.cumsum(w[kept])
+    at = int(np.searchsorted(cum, float(u) * cum[-1], side="right"))
+    at = min(at, int(np.nonzero(w[kept])[0][-1]))
+    return int(kept[at]), len(kept), float(np.log(w[kept[at]] / cum[-1]))
+
+
 def accept_sampled(node_token, node_parent, n_nodes, logits, uniforms, temperature, T):
     """One step's outcome under sampling-based acceptance: the target's token is drawn at every node, then the
     path is followed as in greedy acceptance.  Returns what accept_longest returns."""

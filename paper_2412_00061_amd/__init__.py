@@ -13,6 +13,7 @@ from .binding import (  # noqa: F401
     ctc_draft_topk,
     ctc_draft_topk_noalloc,
     ctc_loss,
+    verify_sample_filtered,
     verify_sample_tokens,
     ctc_loss_workspace_bytes,
     ctc_raw_tree,

@@ -20,6 +20,7 @@ EXPORTS = (
     "ctc_draft_topk_noalloc", "ctcspec_defer_topk_merge", "ctcspec_flush", "ctcspec_stream_probe",
     "prefix_verify_attn_workspace_bytes", "prefix_verify_attn", "kv_weight_update", "kv_evict",
     "kv_append_q4", "kv_commit_q4", "kv_read_q4", "q4_verify_attn_workspace_bytes", "q4_verify_attn",
+    "verify_sample_filtered",
 )
 
 CTCSPEC_F32, CTCSPEC_BF16 = 0, 1
@@ -135,6 +136,8 @@ def load_library():
     lib.q4_verify_attn.restype = c_int
     lib.q4_verify_attn.argtypes = ([c_void_p, c_int, c_void_p, POINTER(_Q4Cache)] + [c_void_p] * 2 + [c_int] + [c_void_p] * 5 + [c_int] * 5 +
                                    [c_float, c_int, c_int, c_void_p, c_size_t, c_int] + [c_void_p] * 2)
+    lib.verify_sample_filtered.restype = c_int
+    lib.verify_sample_filtered.argtypes = [c_void_p] * 8 + [c_int] * 3 + [c_void_p] * 3
     _LIB = lib
     return lib
 
@@ -667,4 +670,26 @@ def q4_verify_attn(ctx, q, cache, kv_off, ctx_len, kv_cap, k_tree, v_tree, n_nod
         B, H, H_kv, dh, N, c_float(scale), window, sink, _ptr(workspace, torch.uint8), workspace.numel(), _dtype_code(res["out"]),
         _ptr(res["out"]), _ptr(res.get("lse")))
     ctx._check(rc, "q4_verify_attn")
+    return res
+
+
+def verify_sample_filtered(ctx, logits, n_nodes, uniforms, temperature, *, top_k=None, top_p=None, min_p=None, want_kept=False,
+                           want_logp=False, out=None):
+    """logits [B,N,V] f32, uniforms [B,N] f32 in [0,1), temperature [B] f32, filters [B] (top_k int32, top_p and min_p f32) or None ->
+    dict(target_sampled [B,N] i32[, n_kept [B,N] i32][, logp [B,N] f32])."""
+    B, N, V = logits.shape
+    _shaped("uniforms", uniforms, (B, N))
+    for name, t in (("n_nodes", n_nodes), ("temperature", temperature), ("top_k", top_k), ("top_p", top_p), ("min_p", min_p)):
+        if t is not None or name in ("n_nodes", "temperature"):
+            _shaped(name, t, (B,))
+    res = {"target_sampled": _out(out, "target_sampled", (B, N), torch.int32, logits.device)}
+    if want_kept:
+        res["n_kept"] = _out(out, "n_kept", (B, N), torch.int32, logits.device)
+    if want_logp:
+        res["logp"] = _out(out, "logp", (B, N), torch.float32, logits.device)
+    rc = ctx.lib.verify_sample_filtered(
+        ctx.handle, _ptr(logits, torch.float32), _ptr(n_nodes, torch.int32), _ptr(uniforms, torch.float32), _ptr(temperature, torch.float32),
+        _ptr(top_k, torch.int32), _ptr(top_p, torch.float32), _ptr(min_p, torch.float32), B, N, V, _ptr(res["target_sampled"]),
+        _ptr(res.get("n_kept")), _ptr(res.get("logp")))
+    ctx._check(rc, "verify_sample_filtered")
     return res

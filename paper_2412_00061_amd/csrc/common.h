@@ -108,6 +108,7 @@ hipError_t prepare_kv_weight();
 hipError_t prepare_kv_evict();
 hipError_t prepare_kv_q4();
 hipError_t prepare_q4_attn();
+hipError_t prepare_sample_filtered();
 
 #define CTCSPEC_REQUIRE(ctx, cond, code, ...) \
   do {                                        \

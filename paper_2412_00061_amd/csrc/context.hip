@@ -110,6 +110,7 @@ extern "C" int ctcspec_create(ctcspec_ctx** out, void* hip_stream, const ctcspec
   if (e == hipSuccess) e = prepare_kv_evict();
   if (e == hipSuccess) e = prepare_kv_q4();
   if (e == hipSuccess) e = prepare_q4_attn();
+  if (e == hipSuccess) e = prepare_sample_filtered();
   if (e != hipSuccess) {
     delete ctx;
     return fail(nullptr, CTCSPEC_EHIP, "preparing the kernels failed: %s", hipGetErrorString(e));
