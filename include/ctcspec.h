@@ -673,10 +673,11 @@ int q4_verify_attn(ctcspec_ctx* ctx, ctcspec_dtype dt, const void* q, const ctcs
  *   n_kept[b,i]  = the number of kept tokens
  *   logp[b,i]    = log (w[target_sampled] / sum_{kept u} w[u])
  *
- * A temperature of 0 or less takes the first token of the order (n_kept 1, logp 0), whatever the filters say.  Weights and sums are held in
- * 64 bits: cut-offs and token are the exact ones unless a border lies within rounding (about 1e-13 of the sums; for top_p of the weights,
- * relative to the largest, in whole multiples of 2^-45).  A logit that is -infinity or not a number is never kept; +infinity takes all (equal ones alike); where no
- * logit is above -infinity the outputs are -1, 0 and -infinity.  Rows i >= n_nodes[b] receive -1, 0 and 0.
+ * A temperature of 0 or less takes the first token of the order (n_kept 1, logp 0), whatever the filters say.  Weights are formed in 64
+ * bits and summed in 64 bits or in whole multiples of 2^-45 of the largest (of a kept token at least one): cut-offs and token are the exact
+ * ones unless a border lies within their roundings, at most V * 2^-45 of the largest weight.  A logit that is -infinity or not a number is
+ * never kept; where one is +infinity, those alone are that are; where none is above -infinity the outputs are -1, 0 and -infinity.  Rows
+ * i >= n_nodes[b] receive -1, 0 and 0.
  *
  * logits         [B,max_nodes,V] float device in, 16-byte aligned
  * n_nodes        [B] int32 device in

@@ -53,10 +53,12 @@ def filter_tokens(logits_row, temperature, top_k=0, top_p=1.0, min_p=0.0):
     """Which tokens the sampling filters keep, and the weights of all: (kept, ascending ids; w = exp((logit - max) / temperature)).
     Each filter keeps a beginning of the order by falling logit (equal ones by id): the first top_k (0 or less: all); of these a token if
     the weights before it sum up to less than top_p of those of the top_k tokens (the first always; 1 or more: all); those with
-    w >= min_p (more than 1 counts as 1).  A temperature of 0 or less keeps the first alone.  -infinity and NaN are never kept, +infinity
-    takes all."""
+    w >= min_p (more than 1 counts as 1).  A temperature of 0 or less keeps the first alone.  -infinity and NaN are never kept; where a
+    logit is +infinity, those are that are."""
     z = np.asarray(logits_row, dtype=np.float64)
     z = np.where(np.isnan(z), -np.inf, z)
+    if z.max() == np.inf:
+        z = np.where(z == np.inf, 0.0, -np.inf)
     top = z.max()
     w = np.zeros_like(z)
     if top == -np.inf:
@@ -66,9 +68,7 @@ def filter_tokens(logits_row, temperature, top_k=0, top_p=1.0, min_p=0.0):
     if not temperature > 0:
         w[order[0]] = 1.0
         return order[:1], w
-    w[z == top] = 1.0
-    if top < np.inf:
-        w[order] = np.exp((z[order] - top) / float(temperature))
+    w[order] = np.exp((z[order] - top) / float(temperature))
     if top_k > 0:
         order = order[:top_k]
     if top_p < 1:

@@ -43,8 +43,8 @@ def check(logits, u, n_nodes=None, t=None, k=None, p=None, m=None, **more):
                 continue
             want = oracle.sample_filtered(logits[b, i], float(np.float32(u[b, i])), f32(t, b, 1.0), 0 if k is None else int(k[b]), f32(p, b, 1.0), f32(m, b, 0.0))
             assert got[:2] == want[:2], (b, i, got, want)
-            # a sum of V weights in 64 bits and one rounding to float
-            assert got[2] == want[2] or abs(got[2] - want[2]) <= 2.0 ** -24 * abs(want[2]) + V * 2.0 ** -50, (b, i, got, want)
+            # each weight in the sum may be off by a unit of 2^-45 of the largest, the sum is at least that; one rounding to float
+            assert got[2] == want[2] or abs(got[2] - want[2]) <= 2.0 ** -24 * abs(want[2]) + V * 2.0 ** -45, (b, i, got, want)
     return res
 
 
