@@ -10,6 +10,8 @@
 //
 // Weights are exp((z - z_max) / t) in 64 bits, relative to the largest: where they are compared with a border they are whole multiples of
 // 2^-45, whose sums do not depend on their order; where the draw sums them they are doubles, in a fixed order.
+#include <type_traits>
+
 #include "common.h"
 
 namespace ctcspec {
@@ -38,21 +40,38 @@ struct FilterParams {
 
 typedef unsigned long long u64;
 
-__device__ __forceinline__ double wave_scan_incl(double v, int lane) {
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const double o = __shfl_up(v, d, 64);
-    if (lane >= d) v += o;
-  }
+// Inclusive sums over the lanes of a wavefront: within the rows of 16 lanes, then each row's end into the next and that of the second into
+// the upper half - all without the LDS.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ unsigned int dpp_shift(unsigned int v) {  // (lanes without a source: 0)
+  return (unsigned int)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false);
+}
+#define CTCSPEC_SCAN_STEPS(STEP) STEP(0x111, 0xf) STEP(0x112, 0xf) STEP(0x114, 0xf) STEP(0x118, 0xf) STEP(0x142, 0xa) STEP(0x143, 0xc)
+__device__ __forceinline__ unsigned int wave_scan_incl(unsigned int v) {
+#define CTCSPEC_STEP(CTRL, ROWS) v += dpp_shift<CTRL, ROWS>(v);
+  CTCSPEC_SCAN_STEPS(CTCSPEC_STEP)
+#undef CTCSPEC_STEP
   return v;
 }
-__device__ __forceinline__ u64 wave_scan_incl(u64 v, int lane) {
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const u64 o = __shfl_up(v, d, 64);
-    if (lane >= d) v += o;
-  }
+__device__ __forceinline__ u64 wave_scan_incl(u64 v) {
+#define CTCSPEC_STEP(CTRL, ROWS) v += (u64)dpp_shift<CTRL, ROWS>((unsigned int)(v >> 32)) << 32 | dpp_shift<CTRL, ROWS>((unsigned int)v);
+  CTCSPEC_SCAN_STEPS(CTCSPEC_STEP)
+#undef CTCSPEC_STEP
   return v;
+}
+__device__ __forceinline__ double wave_scan_incl(double v) {
+#define CTCSPEC_STEP(CTRL, ROWS)                                                                                                     \
+  {                                                                                                                                  \
+    const u64 u = (u64)__double_as_longlong(v);                                                                                      \
+    v += __longlong_as_double((long long)((u64)dpp_shift<CTRL, ROWS>((unsigned int)(u >> 32)) << 32 | dpp_shift<CTRL, ROWS>((unsigned int)u))); \
+  }
+  CTCSPEC_SCAN_STEPS(CTCSPEC_STEP)
+#undef CTCSPEC_STEP
+  return v;
+}
+#undef CTCSPEC_SCAN_STEPS
+__device__ __forceinline__ u64 readlane_u64(u64 v, int lane) {
+  return (u64)readlane_u32((unsigned int)(v >> 32), lane) << 32 | readlane_u32((unsigned int)v, lane);
 }
 
 // p f + c.  (Left to itself the compiler keeps the polynomial's coefficients in vector registers and copies each into place first.)
@@ -235,7 +254,7 @@ __device__ __forceinline__ void sample_streamed(const FilterParams& p, FilterSha
       // -- sums over the bins, one to a thread; the first that reaches the border
       const unsigned int mine = sh.count[tid];
       const u64 mine_weight = sh.weight[tid];
-      const u64 c_incl = wave_scan_incl((u64)mine, lane), w_incl = wave_scan_incl(mine_weight, lane);
+      const u64 c_incl = wave_scan_incl((u64)mine), w_incl = wave_scan_incl(mine_weight);
       if (lane == 63) { sh.wave_u32[wave] = (unsigned int)c_incl; sh.wave_u64[wave] = w_incl; }
       __syncthreads();
       u64 c_before = ahead + c_incl - mine, w_before = ahead_weight + w_incl - mine_weight, w_all = 0ull;
@@ -325,7 +344,7 @@ __device__ __forceinline__ void sample_streamed(const FilterParams& p, FilterSha
         if (w >= 0.0) { s += w; ++mine; }
       }
       double wt = 0.0;
-      if (__ballot(s > 0.0)) wt = wave_scan_incl(s, lane);
+      if (__ballot(s > 0.0)) wt = wave_scan_incl(s);
       if (lane == 63) sh.wave_total[k * kFilterWaves + wave] = wt;
     }
   }
@@ -339,7 +358,7 @@ __device__ __forceinline__ void sample_streamed(const FilterParams& p, FilterSha
       const int j = lane * each_lane + q;
       local += j < entries ? sh.wave_total[j] : 0.0;
     }
-    const double incl = wave_scan_incl(local, lane), total = __shfl(incl, 63, 64);
+    const double incl = wave_scan_incl(local), total = __shfl(incl, 63, 64);
     const double target = fmax((double)p.uniforms[row] * total, 0.0);  // (a number below 0 counts as 0)
     double run = incl - local;
     int found = -1, last = -1;
@@ -379,7 +398,7 @@ __device__ __forceinline__ void sample_streamed(const FilterParams& p, FilterSha
     w[c] = fmax(kept(chunk, c, v[c]), 0.0);
     s += w[c];
   }
-  const double rest = sh.rest, incl = wave_scan_incl(s, lane);
+  const double rest = sh.rest, incl = wave_scan_incl(s);
   const u64 cross = __ballot(s > 0.0 && incl > rest), some = __ballot(s > 0.0);
   const int src = cross ? __ffsll((long long)cross) - 1 : 63 - __clzll((long long)some);
   if (lane != src) return;
@@ -411,9 +430,11 @@ struct ListShared {
   float logit[kFilterCandidates];
   unsigned int index[kFilterCandidates];
   u64 key[kFilterMembers], key_weight[kFilterMembers];
-  double wave_f64[kFilterWaves];
-  u64 wave_u64[kFilterWaves];
-  unsigned int wave_u32[kFilterWaves], wave_u32b[kFilterWaves];
+  // a word for each wavefront: every one of them is written once (block_sum's in turn)
+  double plain_sum[kFilterWaves];
+  u64 bin_sum[kFilterWaves], draw_sum[kFilterWaves], block_sum[2][kFilterWaves];
+  float largest[kFilterWaves], lowest[kFilterWaves];
+  unsigned int part_sum[kFilterWaves], count_sum[kFilterWaves], kept[kFilterWaves];
   u64 ahead_weight, threshold, mass;
   unsigned int candidates, ahead, found, members;
 };
@@ -441,39 +462,24 @@ __device__ __forceinline__ double wave_sum_f64(double v) {
   return (readlane_f64(v, 0) + readlane_f64(v, 16)) + (readlane_f64(v, 32) + readlane_f64(v, 48));
 }
 
-// Sums over the bins before this thread's, and over all: of counts, and of whole weights.  (Two barriers; the second lies behind the reads.)
-__device__ __forceinline__ void bins_before(unsigned int own, unsigned int& before, unsigned int& all, unsigned int* waves, int lane, int wave) {
-  unsigned int incl = own;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const unsigned int o = __shfl_up(incl, d, 64);
-    if (lane >= d) incl += o;
-  }
+// Sums over the threads before this one, and over all: of counts, and of whole weights.  waves: a word for each wavefront; nothing else may
+// be under way with it.  (One barrier: whoever writes to it next has one between.)
+__device__ __forceinline__ void sums_before(unsigned int own, unsigned int& before, unsigned int& all, unsigned int* waves, int lane, int wave) {
+  static_assert(kFilterWaves == 16, "a row of lanes");
+  const unsigned int incl = wave_scan_incl(own);
   if (lane == 63) waves[wave] = incl;
   __syncthreads();
-  before = incl - own;
-  all = 0u;
-#pragma unroll
-  for (int w = 0; w < kFilterWaves; ++w) {
-    const unsigned int v = waves[w];
-    before += w < wave ? v : 0u;
-    all += v;
-  }
-  __syncthreads();
+  const unsigned int of_waves = wave_scan_incl(waves[lane & 15]);  // (the first row's are those of the wavefronts)
+  all = readlane_u32(of_waves, 15);
+  before = incl - own + (wave > 0 ? readlane_u32(of_waves, wave > 0 ? wave - 1 : 0) : 0u);
 }
-__device__ __forceinline__ void bins_before(u64 own, u64& before, u64& all, u64* waves, int lane, int wave) {
-  const u64 incl = wave_scan_incl(own, lane);
+__device__ __forceinline__ void sums_before(u64 own, u64& before, u64& all, u64* waves, int lane, int wave) {
+  const u64 incl = wave_scan_incl(own);
   if (lane == 63) waves[wave] = incl;
   __syncthreads();
-  before = incl - own;
-  all = 0ull;
-#pragma unroll 8
-  for (int w = 0; w < kFilterWaves; ++w) {
-    const u64 v = waves[w];
-    before += w < wave ? v : 0ull;
-    all += v;
-  }
-  __syncthreads();
+  const u64 of_waves = wave_scan_incl(waves[lane & 15]);
+  all = readlane_u64(of_waves, 15);
+  before = incl - own + (wave > 0 ? readlane_u64(of_waves, wave > 0 ? wave - 1 : 0) : 0ull);
 }
 
 // The tokens that may be kept are few, mostly, and a bound below them all is easily had: among the first top_k tokens' logits is none below
@@ -486,7 +492,7 @@ __device__ __forceinline__ void bins_before(u64 own, u64& before, u64& all, u64*
 // is still to be done.
 template <int NV>
 __device__ __forceinline__ bool sample_listed(const FilterParams& p, ListShared& sh) {
-  const int i = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int i = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const size_t row = (size_t)b * p.N + i;
   // Each wavefront has a stretch of the row, 64 groups at a time.  (The row starts `lead` elements past a 16-byte boundary; group g holds
   // its elements 4g - lead .. 4g - lead + 3; what is no number, and what lies outside, counts as -infinity.)
@@ -567,14 +573,10 @@ __device__ __forceinline__ bool sample_listed(const FilterParams& p, ListShared&
   }
   mx = wave_max_f32(mx);
   low = -wave_max_f32(-low);
-  if (lane == 0) { sh.wave_u32[wave] = __float_as_uint(mx); sh.wave_u32b[wave] = __float_as_uint(low); }
-  __syncthreads();
-#pragma unroll 4
-  for (int w = 0; w < kFilterWaves; ++w) {
-    mx = fmaxf(mx, __uint_as_float(sh.wave_u32[w]));
-    low = fminf(low, __uint_as_float(sh.wave_u32b[w]));
-  }
-  __syncthreads();  // (read; and the bins are cleared)
+  if (lane == 0) { sh.largest[wave] = mx; sh.lowest[wave] = low; }
+  __syncthreads();  // (and the bins are cleared)
+  mx = wave_max_f32(sh.largest[lane & 15]);
+  low = -wave_max_f32(-sh.lowest[lane & 15]);
   if (mx == -INFINITY) {  // nothing to draw
     if (tid == 0) leave(p, row, -1, 0, -INFINITY);
     return false;
@@ -609,21 +611,21 @@ __device__ __forceinline__ bool sample_listed(const FilterParams& p, ListShared&
     });
     s = wave_sum_f64(s);
     n = wave_sum_i32(n);
-    if (lane == 0) { sh.wave_f64[wave] = s; sh.wave_u32b[wave] = (unsigned)n; }
+    if (lane == 0) { sh.plain_sum[wave] = s; sh.kept[wave] = (unsigned)n; }
     __syncthreads();
     double total = 0.0;
     int kept = 0, last = 0, at = -1;
 #pragma unroll 4
     for (int w = 0; w < kFilterWaves; ++w) {
-      total += sh.wave_f64[w];
-      kept += (int)sh.wave_u32b[w];
-      last = sh.wave_f64[w] > 0.0 ? w : last;
+      total += sh.plain_sum[w];
+      kept += (int)sh.kept[w];
+      last = sh.plain_sum[w] > 0.0 ? w : last;
     }
     const double target = fmax((double)uniform_number * total, 0.0);  // (a number below 0 counts as 0)
     double run = 0.0, rest = INFINITY;
 #pragma unroll 4
     for (int w = 0; w < kFilterWaves; ++w) {
-      const double v = sh.wave_f64[w];
+      const double v = sh.plain_sum[w];
       if (at < 0 && v > 0.0 && run + v > target) { at = w; rest = target - run; }
       run += v;
     }
@@ -641,7 +643,7 @@ __device__ __forceinline__ bool sample_listed(const FilterParams& p, ListShared&
         w[c] = v[c] > -INFINITY ? y : 0.0;
       }
       const double mine = ((w[0] + w[1]) + w[2]) + w[3];
-      const double incl = before + wave_scan_incl(mine, lane);
+      const double incl = before + wave_scan_incl(mine);
       const u64 cross = __ballot(mine > 0.0 && incl > rest), some = __ballot(mine > 0.0);
       if (some) {  // the token if the row ended here: the last one with any weight; the one that is looked for, where it is
         const int src = cross ? __ffsll((long long)cross) - 1 : 63 - __clzll((long long)some);
@@ -674,7 +676,7 @@ __device__ __forceinline__ bool sample_listed(const FilterParams& p, ListShared&
       if (part[q] > -INFINITY) atomicAdd(&sh.part_count[bin_of(part[q], part_scale)], 1u);
     __syncthreads();
     parts_here = sh.part_count[tid];
-    bins_before(parts_here, parts_before, parts, sh.wave_u32, lane, wave);
+    sums_before(parts_here, parts_before, parts, sh.part_sum, lane, wave);
   }
   // a bound that at least `wanted` of them lie above
   auto below_parts = [&](unsigned int wanted) __attribute__((always_inline)) -> float {
@@ -687,36 +689,54 @@ __device__ __forceinline__ bool sample_listed(const FilterParams& p, ListShared&
     // (one bin further: what rounding moves across a bin's end)
     return found + 2 < (unsigned)kFilterBins && part_scale > 0.f ? mx - (float)(found + 2) / part_scale : -INFINITY;
   };
-  // The candidates, in any order: those with from <= logit < to.
-  auto list = [&](float from, float to, auto&& also) __attribute__((always_inline)) {
-    groups([&](int j, const f32x4& v) __attribute__((always_inline)) {
-      bool in[4];
+  // The candidates, in any order: those with from <= logit, and for more of them logit < to.  Marked group by group, then counted and written a batch of groups at a
+  // time, so that a wavefront asks for its places once a batch.
+  constexpr int kBatch = NV > 0 ? NV : 8;
+  auto list_batch = [&](int j0, const f32x4 (&v)[kBatch], float from, float to, auto&& also, auto more) __attribute__((always_inline)) {
+    constexpr bool MORE = decltype(more)::value;
+    unsigned int marks = 0u;  // bit 4 j + c
 #pragma unroll
-      for (int c = 0; c < 4; ++c) in[c] = v[c] >= from && v[c] < to && v[c] > -INFINITY;
-      if (__ballot(in[0] || in[1] || in[2] || in[3])) {
-        u64 who[4];
-        int all = 0;
+    for (int j = 0; j < kBatch; ++j) {
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          who[c] = __ballot(in[c]);
-          all += __popcll(who[c]);
-        }
-        unsigned int place = 0u;
-        if (lane == 0) place = atomicAdd(&sh.candidates, (unsigned)all);
-        place = (unsigned)__builtin_amdgcn_readfirstlane((int)place);
-        const u64 below = (1ull << lane) - 1;
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          const unsigned int at = place + (unsigned)__popcll(who[c] & below);
-          if (in[c] && at < (unsigned)kFilterCandidates) {
-            sh.logit[at] = v[c];
-            sh.index[at] = (unsigned)(first + 256 * j + c);
-          }
-          place += (unsigned)__popcll(who[c]);
-        }
+      for (int c = 0; c < 4; ++c) {
+        bool in = v[j][c] >= from;
+        if constexpr (MORE) in = in && v[j][c] < to;
+        marks |= in ? 1u << (4 * j + c) : 0u;
       }
-      also(v);
-    });
+      if (j0 + j < nv) also(v[j]);
+      __builtin_amdgcn_sched_barrier(0);  // (group by group: what all of them need at once does not fit the registers)
+    }
+    if (__ballot(marks != 0u) == 0ull) return;
+    const unsigned int incl = wave_scan_incl((unsigned)__popc(marks));
+    unsigned int place = 0u;
+    if (lane == 63) place = atomicAdd(&sh.candidates, incl);
+    place = readlane_u32(place, 63) + incl - (unsigned)__popc(marks);
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j)
+      if ((marks >> (4 * j)) & 15u) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          if ((marks >> (4 * j + c)) & 1u) {
+            if (place < (unsigned)kFilterCandidates) {
+              sh.logit[place] = v[j][c];
+              sh.index[place] = (unsigned)(first + 256 * (j0 + j) + c);
+            }
+            ++place;
+          }
+      }
+  };
+  auto list = [&](float from, float to, auto&& also, auto more) __attribute__((always_inline)) {
+    from = fmaxf(from, -3.402823466e38f);  // (no -infinity)
+    if constexpr (NV > 0) {
+      list_batch(0, x, from, to, also, more);
+    } else {
+      for (int j0 = 0; j0 < nv; j0 += kBatch) {
+        f32x4 v[kBatch];
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) v[j] = load(j0 + j);
+        list_batch(j0, v, from, to, also, more);
+      }
+    }
     __syncthreads();
   };
   const bool of_all = want.by_p && !want.by_k;  // top-p's share is of all tokens
@@ -736,17 +756,13 @@ __device__ __forceinline__ bool sample_listed(const FilterParams& p, ListShared&
         mass += v[c] > -INFINITY ? y : 0ull;
       }
     }
-  });
+  }, std::false_type{});
   unsigned int listed = sh.candidates;
+  int turn = 0;
   auto block_sum = [&](u64 v) __attribute__((always_inline)) -> u64 {
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d, 64);
-    if (lane == 0) sh.wave_u64[wave] = v;
-    __syncthreads();
-    u64 all = 0ull;
-#pragma unroll 8
-    for (int w = 0; w < kFilterWaves; ++w) all += sh.wave_u64[w];
-    __syncthreads();
+    u64 before, all;
+    sums_before(v, before, all, sh.block_sum[turn], lane, wave);
+    turn ^= 1;
     return all;
   };
   if (of_all) {
@@ -764,7 +780,7 @@ __device__ __forceinline__ bool sample_listed(const FilterParams& p, ListShared&
       if ((double)weighs >= enough || bound == -INFINITY || bound == distance) break;
       const float upto = bound;
       bound = fmaxf(round == 1 ? below_parts(parts / 4 * 3) : (round == 2 ? below_parts(parts / 40 * 39) : -INFINITY), distance);
-      list(bound, upto, [](const f32x4&) {});
+      list(bound, upto, [](const f32x4&) {}, std::true_type{});
       listed = sh.candidates;
     }
   }
@@ -787,8 +803,8 @@ __device__ __forceinline__ bool sample_listed(const FilterParams& p, ListShared&
     const u64 own_weight = sh.bin_weight[tid];
     unsigned int before = 0u, all = 0u;
     u64 before_weight = 0ull, all_weight = 0ull;
-    if (want.by_k) bins_before(own, before, all, sh.wave_u32, lane, wave);
-    if (want.by_p) bins_before(own_weight, before_weight, all_weight, sh.wave_u64, lane, wave);
+    if (want.by_k) sums_before(own, before, all, sh.count_sum, lane, wave);
+    if (want.by_p) sums_before(own_weight, before_weight, all_weight, sh.bin_sum, lane, wave);
     // f(key, weight, tokens of the bin before it, their weight) for the tokens of a bin
     auto rank = [&](unsigned int bin, auto&& f) __attribute__((always_inline)) {
       for (int e = tid; e < n; e += kFilterThreads)
@@ -883,11 +899,11 @@ __device__ __forceinline__ bool sample_listed(const FilterParams& p, ListShared&
     if (w != none && w > 0ull) atomicAdd(&sh.bin_weight[sh.index[e] >> shift], w);
   }
   kept = wave_sum_i32(kept);
-  if (lane == 0) sh.wave_u32b[wave] = (unsigned)kept;
+  if (lane == 0) sh.kept[wave] = (unsigned)kept;
   __syncthreads();
   const u64 own = sh.bin_weight[tid];
   u64 before, total;
-  bins_before(own, before, total, sh.wave_u64, lane, wave);
+  sums_before(own, before, total, sh.draw_sum, lane, wave);
   const double wanted = fmax((double)uniform_number * (double)total, 0.0);  // (a number below 0 counts as 0)
   u64 target = total - 1;
   if (wanted < (double)total && (u64)wanted < target) target = (u64)wanted;
@@ -915,7 +931,7 @@ __device__ __forceinline__ bool sample_listed(const FilterParams& p, ListShared&
     if (ahead <= target && ahead + sh.key_weight[tid] > target) {
       int n_kept = 0;
 #pragma unroll 4
-      for (int w = 0; w < kFilterWaves; ++w) n_kept += (int)sh.wave_u32b[w];
+      for (int w = 0; w < kFilterWaves; ++w) n_kept += (int)sh.kept[w];
       leave(p, row, (int)(key >> 32), n_kept, (float)log(weight(__uint_as_float((unsigned)key)) / ((double)total * 0x1p-45)));
     }
   }
