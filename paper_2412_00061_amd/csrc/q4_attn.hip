@@ -34,10 +34,10 @@ struct Q4AttnParams {
   const int32_t* n_nodes;
   const int32_t* depth;           // [B][max_nodes]; null without a window
   const unsigned long long* anc_mask;
-  int kv_cap, B, H, H_kv, group, dh, blocks, max_nodes, window, sink;  // group: heads that share a key head; blocks: of 32 elements, of a row
+  int kv_cap, B, H, H_kv, group, dh, max_nodes, window, sink;  // group: heads that share a key head
   float sl2;                      // scale * log2(e)
-  float* po;                      // partial O: [slot][rows / 32][DT][4][64 lanes][4]
-  float* pml;                     // [slot][2][rows]: maximum in the log2 domain, sum
+  float* po;                      // partial O: [slot][DT][4][64 lanes][4]
+  float* pml;                     // [slot][2][32]: maximum in the log2 domain, sum
   int* odd;                       // [slot]: a value of a tree node is infinite or not a number
   int out_bf16;
   void* out;                      // [B][H][max_nodes][dh]
@@ -45,35 +45,32 @@ struct Q4AttnParams {
 };
 
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
-
-// QT: blocks of 32 rows; DT: blocks of 32 components (at least 2).  FINE: weights in three bf16 parts.
-template <int QT_, int DT_, bool FINE_>
+// DT: blocks of 32 components, of a row of the cache too.  FINE: weights in three bf16 parts.
+template <int DT_, bool FINE_>
 struct Q4Shape {
-  static constexpr int QT = QT_, DT = DT_, R = 32 * QT, NW = kQ4Tiles;
+  static constexpr int DT = DT_, NW = kQ4Tiles;
   static constexpr bool FINE = FINE_;
   static constexpr int KB = (DT + 1) / 2, QU = 4 * KB;        // blocks of a key in a lane; steps of 16 elements of a product
   static constexpr int VB = (DT + 1) / 2;                     // blocks of values in a lane: 32 DT of them in 64 lanes
   static constexpr int ROWB = DT <= 2 ? 128 : 256, TILE = 32 * ROWB;  // values in the LDS
   static constexpr int PART = (DT * 16 + 2) * 64 * 4;         // O, m, l of 32 rows
-  static constexpr int STAGE = NW * TILE > 2 * QT * PART ? NW * TILE : 2 * QT * PART;
+  static constexpr int STAGE = NW * TILE > 2 * PART ? NW * TILE : 2 * PART;
   static constexpr int LDS = STAGE + 6 * 64 * 4;              // and the sequences' table: behind the tiles, whose places are formed by xor
-  static constexpr int WPE = QT == 1 ? 2 : 1, GROUPS = QT == 1 ? 512 : 256;
-  static_assert(2 * LDS <= 160 * 1024 && GROUPS <= kPrefixMaxGroups && GROUPS % 8 == 0);
+  static_assert(kQ4Waves * LDS <= 160 * 1024 && kQ4Groups % 8 == 0);
   // 16-byte chunk c of row r lies at chunk c ^ place(r).  A transposing read of 32 lanes takes four chunks of each of four consecutive
   // rows: these differ in the chunk's upper bits (rows of 128 bytes: in every second row).  A write of eight lanes takes the same chunk of
   // a block from rows that are four apart: these differ in its lower bits.
   static __device__ __forceinline__ int place(int r) { return (ROWB == 256 ? (r & 3) << 2 : ((r >> 1) & 1) << 2) ^ ((r >> 2) & 3); }
-  // the block of values that a lane converts as its u-th: row and block of the row
-  static __device__ __forceinline__ int v_row(int x) {
-    if constexpr (DT == 2) {
-      const int a = x >> 1;
-      return (a & 1) | ((a >> 1) & 7) << 2 | ((a >> 4) & 1) << 1;
-    } else {
-      const int a = x / DT;
-      return (a & 7) << 2 | a >> 3;
-    }
+  // The blocks of values that a lane converts: row and block of the row of its k-th.  (Four blocks a row: two neighbours of a row; else
+  // those 64 further.)
+  static constexpr bool PAIRS = DT == 4;
+  static __device__ __forceinline__ int v_row(int lane, int k) {
+    const int a = PAIRS ? lane / 2 : (lane + 64 * k) / DT;
+    if constexpr (ROWB == 128) return (a & 1) | ((a >> 1) & 7) << 2 | ((a >> 4) & 1) << 1;
+    else return (a & 7) << 2 | a >> 3;
   }
-  static __device__ __forceinline__ int v_block(int x) { return x % DT; }
+  static __device__ __forceinline__ int v_block(int lane, int k) { return PAIRS ? 2 * (lane % 2) + k : (lane + 64 * k) % DT; }
+  static __device__ __forceinline__ bool v_there(int lane, int k) { return DT % 2 == 0 || lane + 64 * k < 32 * DT; }
 };
 
 // What both kernels know about the work: lane b holds sequence b's part (the limits allow 64 sequences), the rest is uniform.
@@ -92,7 +89,7 @@ __device__ __forceinline__ Q4Work q4_read_work(const Q4AttnParams& p) {
     t.n = n < 0 ? 0 : (n > p.max_nodes ? p.max_nodes : n);
     t.ctx = L < 0 ? 0 : (L > p.kv_cap ? p.kv_cap : L);
   }
-  t.blocks = (t.n * p.group + SH::R - 1) / SH::R;
+  t.blocks = (t.n * p.group + kQ4Rows - 1) / kQ4Rows;
   t.iters = t.n ? (q4_tiles(t.ctx, p.window, p.sink).count + (t.n + 31) / 32 + kQ4Tiles - 1) / kQ4Tiles : 0;
   const int mine = t.blocks * q4_units(t.iters);
   int b = t.blocks, u = mine;
@@ -138,20 +135,35 @@ __device__ __forceinline__ Q4Mask q4_tree_mask(const Q4AttnParams& p, int b, int
 
 #if defined(__HIP_DEVICE_COMPILE__)
 typedef __attribute__((address_space(3))) unsigned char lds_byte;
+// of a value of lanes 32 apart, in both
+__device__ __forceinline__ float half_max(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float half_sum(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+// a descriptor of `bytes` bytes at p, both the same in every lane
+__device__ __forceinline__ auto buffer(const unsigned char* p, int bytes) {
+  const unsigned long long at = (unsigned long long)p;
+  const unsigned long long base = (unsigned long long)(unsigned)uniform((int)(at >> 32)) << 32 | (unsigned)uniform((int)at);
+  return __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, (unsigned)uniform(bytes), 0x00020000);
+}
 __device__ __forceinline__ s16x4 lds_read_tr(unsigned int at) {
   return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)at);
 }
 #endif
 
 template <typename SH>
-__global__ __launch_bounds__(64 * SH::NW, SH::WPE) void q4_attn_kernel(Q4AttnParams p) {
+__global__ __launch_bounds__(64 * SH::NW, kQ4Waves) void q4_attn_kernel(Q4AttnParams p) {
 #if defined(__HIP_DEVICE_COMPILE__)
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-  constexpr int R = SH::R, QT = SH::QT, DT = SH::DT, KB = SH::KB, VB = SH::VB, QU = SH::QU, ROWB = SH::ROWB;
-  const int lane = threadIdx.x & 63, c = lane & 31, h2 = lane >> 5;
+  constexpr int DT = SH::DT, KB = SH::KB, VB = SH::VB, QU = SH::QU, ROWB = SH::ROWB;
+  const int lane = threadIdx.x & 63;
   const int wave = uniform(threadIdx.x >> 6);
   const Q4Work t = q4_read_work<SH>(p);
-  const Deal d = prefix_deal(t.units, SH::GROUPS);
+  const Deal d = prefix_deal(t.units, kQ4Groups);
   // (consecutive shares - neighbouring keys - to the same of the 8 XCDs)
   const int per = (d.groups + 7) / 8, w = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
   if ((int)(blockIdx.x >> 3) >= per || w >= d.groups) return;
@@ -173,17 +185,25 @@ __global__ __launch_bounds__(64 * SH::NW, SH::WPE) void q4_attn_kernel(Q4AttnPar
   unsigned char* vtile = smem + wave * SH::TILE;
   const unsigned int vbase = (unsigned int)(size_t)(lds_byte*)vtile;
   // the transposing read: 16 lanes fetch 4 rows x 16 components, 8 bytes each, and lane s of them receives component s of the four rows
-  unsigned int vread;
+  unsigned int vread0;
   {
-    const int s = lane & 15, row = 4 * h2 + (s >> 2), ch = ((c >> 4) << 1) + ((s & 3) >> 1);
-    vread = vbase + row * ROWB + ((ch ^ SH::place(row)) << 4) + (s & 1) * 8;
+    const int s = lane & 15, row = 4 * (lane >> 5) + (s >> 2), ch = (((lane & 31) >> 4) << 1) + ((s & 3) >> 1);
+    vread0 = vbase + row * ROWB + ((ch ^ SH::place(row)) << 4) + (s & 1) * 8;
   }
+  // where this lane's k-th block of values goes in the tile
+  auto vwrite = [&](int k) __attribute__((always_inline)) -> unsigned int {
+    const int row = SH::v_there(lane, k) ? SH::v_row(lane, k) : 0, blk = SH::v_there(lane, k) ? SH::v_block(lane, k) : 0;
+    return vbase + row * ROWB + (((4 * blk) ^ SH::place(row)) << 4);
+  };
+  const unsigned int vwrite0 = vwrite(0);
 
   while (u < u1) {
     // ---- which block of rows, which keys -------------------------------------------------------------------------------
     int seg_lane = lane;  // (as something new: addresses that only a segment's ends need are formed there)
     asm volatile("" : "+v"(seg_lane));
-    const int kh = uniform(u / head_units), in_head = u - kh * head_units;
+    int per_head = head_units, group = p.group;  // (and what divisions by them take)
+    asm volatile("" : "+s"(per_head), "+s"(group));
+    const int kh = uniform(u / per_head), in_head = u - kh * per_head;
     // (sequences without nodes have no units: the last sequence that starts at or before the unit and has some)
     const int b = 63 - __builtin_clzll(__builtin_amdgcn_ballot_w64(table[kIters][seg_lane] > 0 && table[kUnit0][seg_lane] <= in_head));
     const int n = uniform(table[kNodes][b]), L = uniform(table[kCtx][b]);
@@ -198,250 +218,247 @@ __global__ __launch_bounds__(64 * SH::NW, SH::WPE) void q4_attn_kernel(Q4AttnPar
     const Q4Tiles tiles = q4_tiles(L, p.window, p.sink);
     const int total = tiles.count + (n + 31) / 32;
     const size_t row0 = (size_t)p.kv_off[b] + (size_t)kh * p.kv_cap;
-    const unsigned char* kc = p.k_codes + row0 * (size_t)(p.blocks * kQ4BlockBytes);
-    const unsigned char* ks = p.k_scales + row0 * (size_t)p.blocks;
-    const unsigned char* vc = p.v_codes + row0 * (size_t)(p.blocks * kQ4BlockBytes);
-    const unsigned char* vs = p.v_scales + row0 * (size_t)p.blocks;
-    const size_t tree0 = ((size_t)b * p.H_kv + kh) * p.max_nodes * (size_t)(p.dh * 2);
-
-    // ---- this lane's query rows: step i of a product has elements 32 (KB h2 + i / 4) + 8 (i % 4) .. + 7 -----------------------------
-    const int c = seg_lane & 31, h2 = seg_lane >> 5;
-    u32x4 qf[QT][QU];
-    Q4Mask mw[QT];
-    int low[QT];  // the first position of the window
-#pragma unroll
-    for (int qt = 0; qt < QT; ++qt) {
-      const int r = blk * R + qt * 32 + c;
-      // (rows that are none do as row 0 does: nobody reads what comes of it)
-      const int live = r < n * p.group ? r : 0, node = live / p.group, hg = live - node * p.group;
-      const unsigned char* row = p.q + (((size_t)b * p.H + kh * p.group + hg) * p.max_nodes + node) * (size_t)(p.dh * 2);
-#pragma unroll
-      for (int i = 0; i < QU; ++i) {
-        const int at = 32 * (KB * h2 + i / 4) + 8 * (i % 4);
-        qf[qt][i] = at < p.dh ? *(const u32x4*)(row + at * 2) : u32x4{0u, 0u, 0u, 0u};
-      }
-      const int depth = p.window > 0 ? q4_depth(p, b, node) : 0;
-      low[qt] = L + depth - p.window + 1;
-      mw[qt] = q4_tree_mask(p, b, node, n, L, depth);
-    }
-    f32x16 o[QT][DT];
-    float m_run[QT], l_run[QT];
-    bool odd = false;
-#pragma unroll
-    for (int qt = 0; qt < QT; ++qt) {
-      m_run[qt] = -INFINITY;
-      l_run[qt] = 0.f;
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[qt][dt][i] = 0.f;
-    }
-
-    // codes and scales of a cached tile: of key c the blocks KB h2 .., of the values blocks lane, lane + 64 (rows behind the last one: the last)
+    // codes and scales of cached tile x of the segment: of key c blocks KB h2 .., of the values blocks lane, lane + 64.  (Rows behind the last
+    // one, and blocks behind a row's last, lie outside what the descriptors hold: zeros.)
     u32x4 kraw[KB], vraw[VB];
-    unsigned int kscale[KB], vscale[VB];
+    unsigned int kscale[KB], vscale[VB];  // (two bytes in the first, where a lane's blocks are neighbours)
     auto fetch = [&](int x) __attribute__((always_inline)) {
-      const int tile = x < tiles.lead ? x : x + tiles.gap, last = L - 1 - 32 * tile;
+      const int tile = x < tiles.lead ? x : x + tiles.gap, left = L - 32 * tile < 32 ? L - 32 * tile : 32;
+      const size_t at = (row0 + 32 * (size_t)tile) * DT;
+      const auto kc = buffer(p.k_codes + at * kQ4BlockBytes, left * DT * kQ4BlockBytes), ks = buffer(p.k_scales + at, left * DT);
+      const auto vc = buffer(p.v_codes + at * kQ4BlockBytes, left * DT * kQ4BlockBytes), vs = buffer(p.v_scales + at, left * DT);
+      constexpr int kOutside = 0x1000000;
+      int fl = lane;  // (as something new: places in a tile are formed here, not kept in registers all the way)
+      asm volatile("" : "+v"(fl));
+      const int kfrom = (fl & 31) * DT + KB * (fl >> 5), vfrom = SH::v_row(fl, 0) * DT + SH::v_block(fl, 0);
 #pragma unroll
       for (int k = 0; k < KB; ++k) {
-        const int row = 32 * tile + (c < last ? c : last), blk = KB * h2 + k < p.blocks ? KB * h2 + k : p.blocks - 1;
-        const size_t at = (size_t)row * p.blocks + blk;
-        kraw[k] = *(const u32x4*)(kc + at * kQ4BlockBytes);
-        kscale[k] = ks[at];
+        const int from = DT % 2 == 0 || KB * (fl >> 5) + k < DT ? kfrom : kOutside;
+        kraw[k] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(kc, from * kQ4BlockBytes, k * kQ4BlockBytes, 0));
+        if constexpr (!SH::PAIRS) kscale[k] = __builtin_amdgcn_raw_buffer_load_b8(ks, from, k, 0);
       }
 #pragma unroll
       for (int k = 0; k < VB; ++k) {
-        const int y = lane + 64 * k < 32 * DT ? lane + 64 * k : 0, key = SH::v_row(y);
-        const int row = 32 * tile + (key < last ? key : last), blk = SH::v_block(y) < p.blocks ? SH::v_block(y) : p.blocks - 1;
-        const size_t at = (size_t)row * p.blocks + blk;
-        vraw[k] = *(const u32x4*)(vc + at * kQ4BlockBytes);
-        vscale[k] = vs[at];
+        const int from = SH::PAIRS ? vfrom : (SH::v_there(fl, k) ? SH::v_row(fl, k) * DT + SH::v_block(fl, k) : kOutside);
+        vraw[k] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(vc, from * kQ4BlockBytes, SH::PAIRS ? k * kQ4BlockBytes : 0, 0));
+        if constexpr (!SH::PAIRS) vscale[k] = __builtin_amdgcn_raw_buffer_load_b8(vs, from, 0, 0);
+      }
+      if constexpr (SH::PAIRS) {
+        kscale[0] = (unsigned short)__builtin_amdgcn_raw_buffer_load_b16(ks, kfrom, 0, 0);
+        vscale[0] = (unsigned short)__builtin_amdgcn_raw_buffer_load_b16(vs, vfrom, 0, 0);
       }
     };
-
+    auto scale_of = [&](const auto& scales, int k) __attribute__((always_inline)) -> float {
+      return q4_scale_value((int)(SH::PAIRS ? (scales[0] >> (8 * k)) & 255u : scales[k]));
+    };
     const int first = it0 * kQ4Tiles + wave, end = (it0 + niter) * kQ4Tiles < total ? (it0 + niter) * kQ4Tiles : total;
-    if (first < tiles.count && first < end) fetch(first);
-    for (int x = first; x < end; x += kQ4Tiles) {
-      const bool tree = x >= tiles.count;
-      const int tile = tree ? x - tiles.count : (x < tiles.lead ? x : x + tiles.gap);
-      u32x4 a[QU];
-      if (!tree) {
-#pragma unroll
-        for (int k = 0; k < KB; ++k)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) a[4 * k + e] = q4_decode(kraw[k][e], q4_scale_value((int)kscale[k]));
-        // values: block by block into this wavefront's tile
-#pragma unroll
-        for (int k = 0; k < VB; ++k) {
-          const int y = lane + 64 * k, row = SH::v_row(y < 32 * DT ? y : 0), blk = SH::v_block(y < 32 * DT ? y : 0);
-          if (y < 32 * DT) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              *(u32x4*)(vtile + row * ROWB + (((4 * blk + e) ^ SH::place(row)) << 4)) = q4_decode(vraw[k][e], q4_scale_value((int)vscale[k]));
-          }
-        }
-        if (x + kQ4Tiles < tiles.count && x + kQ4Tiles < end) fetch(x + kQ4Tiles);
-      } else {
-        // tree nodes: keys as they are, values into the tile as they are (nodes that are none: the last one).  (The lane's number, as
-        // something new: what only these tiles need is then formed here, not kept in registers all the way.)
-        int fresh = lane;
-        asm volatile("" : "+v"(fresh));
-        const int c = fresh & 31, h2 = fresh >> 5, key = 32 * tile + c < n ? 32 * tile + c : n - 1;
-        const unsigned char* kt = p.k_tree + tree0 + (size_t)key * (p.dh * 2);
-        const unsigned char* vt = p.v_tree + tree0;
-#pragma unroll
-        for (int i = 0; i < QU; ++i) {
-          const int at = 32 * (KB * h2 + i / 4) + 8 * (i % 4);
-          a[i] = at < p.dh ? *(const u32x4*)(kt + at * 2) : u32x4{0u, 0u, 0u, 0u};
-        }
-#pragma unroll
-        for (int i = 0; i < 2 * DT; ++i) {  // 128 DT chunks of 8 components
-          const int y = fresh + 64 * i, row = y / (4 * DT), ch = y % (4 * DT), from = 32 * tile + row < n ? 32 * tile + row : n - 1;
-          *(u32x4*)(vtile + row * ROWB + ((ch ^ SH::place(row)) << 4)) =
-              8 * ch < p.dh ? *(const u32x4*)(vt + (size_t)from * (p.dh * 2) + ch * 16) : u32x4{0u, 0u, 0u, 0u};
-        }
-      }
-      asm volatile("" ::: "memory");
+    const int cached_end = end < tiles.count ? end : tiles.count;
+    if (first < cached_end) fetch(first);
 
-      // S^T = K Q^T: a lane then holds 16 scores of one query row, its neighbour 32 lanes away the other 16 - register i: key
-      // 8 (i / 4) + 4 h2 + i % 4 -, and P in the same registers is the right operand of O^T += V^T P
-      f32x16 s[QT];
+    // ---- this lane's query row: step i of a product has elements 32 (KB h2 + i / 4) + 8 (i % 4) .. + 7 ------------------------------
+    u32x4 qf[QU];
+    int low;  // the first position of the window
+    {
+      // (rows that are none do as row 0 does: nobody reads what comes of it)
+      const int r = blk * kQ4Rows + (seg_lane & 31), row_at = r < n * group ? r : 0;
+      const int h2 = seg_lane >> 5, node = row_at / group, hg = row_at - node * group;
+      const unsigned char* row = p.q + (((size_t)b * p.H + kh * group + hg) * p.max_nodes + node) * (size_t)(p.dh * 2);
 #pragma unroll
-      for (int qt = 0; qt < QT; ++qt) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[qt][i] = 0.f;
-#pragma unroll
-        for (int i = 0; i < QU; ++i)
-          s[qt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a[i]), __builtin_bit_cast(bf16x8, qf[qt][i]), s[qt], 0, 0, 0);
+      for (int i = 0; i < QU; ++i) {
+        const int at = 32 * (KB * h2 + i / 4) + 8 * (i % 4);
+        qf[i] = at < p.dh ? *(const u32x4*)(row + at * 2) : u32x4{0u, 0u, 0u, 0u};
       }
-      // ---- keys that are not there or not seen ----------------------------------------------------------------------------
-      const bool mixed = tree || 32 * tile + 32 > L || (p.window > 0 && 32 * tile <= L + p.max_nodes - 1 - p.window);
-      unsigned int vis[QT];
+      low = p.window > 0 ? L + q4_depth(p, b, node) - p.window + 1 : 0;
+    }
+    f32x16 o[DT];
+    float m_run = -INFINITY, l_run = 0.f;
+    bool odd = false;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        float zero = 0.f;
+        asm volatile("" : "+v"(zero));  // (one zero for all would stay in registers of its own)
+        o[dt][i] = zero;
+      }
+
+    // S^T = K Q^T: a lane then holds 16 scores of one query row, its neighbour 32 lanes away the other 16 - register i: key
+    // 8 (i / 4) + 4 h2 + i % 4 -, and P in the same registers is the right operand of O^T += V^T P.
+    // What follows the scores s of a tile whose values lie in the LDS.  mixed: not every row sees every key; vis: this lane's keys that its
+    // row sees, register i at bit 8 (i / 4) + i % 4.
+    auto weigh = [&](f32x16& s, bool tree, bool mixed, unsigned int vis) __attribute__((always_inline)) {
       if (mixed) {
 #pragma unroll
-        for (int qt = 0; qt < QT; ++qt) {
-          if (tree) {
-            vis[qt] = mw[qt].tile(tile);
-          } else {
-            const int left = L - 32 * tile;
-            vis[qt] = left >= 32 ? 0xffffffffu : (1u << left) - 1u;
-            if (p.window > 0) {
-              const int from = low[qt] - 32 * tile, sunk = p.sink - 32 * tile;
-              vis[qt] &= (from <= 0 ? 0xffffffffu : (from >= 32 ? 0u : 0xffffffffu << from)) |
-                         (sunk >= 32 ? 0xffffffffu : (sunk <= 0 ? 0u : (1u << sunk) - 1u));
-            }
-          }
-          vis[qt] >>= 4 * h2;  // register i: bit 8 (i / 4) + i % 4
+        for (int i = 0; i < 16; ++i) s[i] = (vis >> (8 * (i / 4) + i % 4)) & 1u ? s[i] : -INFINITY;
+      }
+      // the reference, in the log2 domain, only has to be near the maximum: it is moved when a score exceeds it by more than 2^8
+      float mx = s[0];
 #pragma unroll
-          for (int i = 0; i < 16; ++i) s[qt][i] = (vis[qt] >> (8 * (i / 4) + i % 4)) & 1u ? s[qt][i] : -INFINITY;
+      for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
+      if (__builtin_amdgcn_ballot_w64(fmaf(mx, p.sl2, -m_run) > 8.0f) != 0ull) {
+        const float m = half_max(mx);
+        if (fmaf(m, p.sl2, -m_run) > 8.0f) {
+          const float top = m * p.sl2, alpha = __builtin_amdgcn_exp2f(m_run - top);  // 0 on first use
+          l_run *= alpha;
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt) o[dt] *= alpha;
+          m_run = top;
         }
       }
-
-      // ---- the reference, in the log2 domain, only has to be near the maximum: it is moved when a score exceeds it by more than 2^8 -----
-      bool far = false;
-      float mx[QT];
+      const float ms = m_run > -INFINITY ? m_run : 0.f;
 #pragma unroll
-      for (int qt = 0; qt < QT; ++qt) {
-        mx[qt] = s[qt][0];
+      for (int kb = 0; kb < 2; ++kb) {  // 16 keys each
+        u32x4 hi, lo, rest;
 #pragma unroll
-        for (int i = 1; i < 16; ++i) mx[qt] = fmaxf(mx[qt], s[qt][i]);
-        far |= fmaf(mx[qt], p.sl2, -m_run[qt]) > 8.0f;
-      }
-      if (__builtin_amdgcn_ballot_w64(far) != 0ull) {
-#pragma unroll
-        for (int qt = 0; qt < QT; ++qt) {
-          const float m = fmaxf(mx[qt], __shfl_xor(mx[qt], 32, 64));
-          if (fmaf(m, p.sl2, -m_run[qt]) > 8.0f) {
-            const float top = m * p.sl2, alpha = __builtin_amdgcn_exp2f(m_run[qt] - top);  // 0 on first use
-            l_run[qt] *= alpha;
-#pragma unroll
-            for (int dt = 0; dt < DT; ++dt) o[qt][dt] *= alpha;
-            m_run[qt] = top;
-          }
-        }
-      }
-      // ---- weights, and the products with the values ---------------------------------------------------------------------------
-      u32x4 hi[QT][2], lo[QT][2], rest[QT][2];
-#pragma unroll
-      for (int qt = 0; qt < QT; ++qt) {
-        const float ms = m_run[qt] > -INFINITY ? m_run[qt] : 0.f;
-        float sum = 0.f;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float p0 = __builtin_amdgcn_exp2f(fmaf(s[qt][2 * j], p.sl2, -ms)), p1 = __builtin_amdgcn_exp2f(fmaf(s[qt][2 * j + 1], p.sl2, -ms));
-          const unsigned int h = __builtin_bit_cast(unsigned int, bf16x2{(__bf16)p0, (__bf16)p1});
-          hi[qt][j / 4][j % 4] = h;
+        for (int j = 0; j < 4; ++j) {
+          const float p0 = __builtin_amdgcn_exp2f(fmaf(s[8 * kb + 2 * j], p.sl2, -ms)), p1 = __builtin_amdgcn_exp2f(fmaf(s[8 * kb + 2 * j + 1], p.sl2, -ms));
+          hi[j] = __builtin_bit_cast(unsigned int, bf16x2{(__bf16)p0, (__bf16)p1});
           if constexpr (SH::FINE) {
-            const float h0 = __uint_as_float(h << 16), h1 = __uint_as_float(h & 0xffff0000u);
-            const unsigned int r = __builtin_bit_cast(unsigned int, bf16x2{(__bf16)(p0 - h0), (__bf16)(p1 - h1)});
-            lo[qt][j / 4][j % 4] = r;
-            const float r0 = (p0 - h0) - __uint_as_float(r << 16), r1 = (p1 - h1) - __uint_as_float(r & 0xffff0000u);
-            rest[qt][j / 4][j % 4] = __builtin_bit_cast(unsigned int, bf16x2{(__bf16)r0, (__bf16)r1});
+            const float h0 = __uint_as_float(hi[j] << 16), h1 = __uint_as_float(hi[j] & 0xffff0000u);
+            lo[j] = __builtin_bit_cast(unsigned int, bf16x2{(__bf16)(p0 - h0), (__bf16)(p1 - h1)});
+            const float r0 = (p0 - h0) - __uint_as_float(lo[j] << 16), r1 = (p1 - h1) - __uint_as_float(lo[j] & 0xffff0000u);
+            rest[j] = __builtin_bit_cast(unsigned int, bf16x2{(__bf16)r0, (__bf16)r1});
           }
-          sum += p0 + p1;
+          l_run += p0 + p1;
         }
-        l_run[qt] += sum;
-      }
+        // (two blocks of components at a time: what all of them need at once does not fit the registers)
+        constexpr int PAIR = DT == 4 ? 1 : 2;
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
-        u32x4 vr[DT];
+        for (int d0 = 0; d0 < DT; d0 += PAIR) {
+          u32x4 vr[PAIR];
+          unsigned int vread = vread0;
+          asm volatile("" : "+v"(vread));
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) {
-          const s16x4 v0 = lds_read_tr((vread ^ (dt << 6)) + 16 * kb * ROWB), v1 = lds_read_tr((vread ^ (dt << 6) ^ 32) + (16 * kb + 8) * ROWB);
-          vr[dt] = __builtin_bit_cast(u32x4, s16x8{v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]});
-        }
-        if (mixed) {
-          // A value that is no number must not reach the rows that do not see its key, and 0 times it is no number: such values take part
-          // as 0.  A cached one is NaN and makes the rows that see it NaN: those that a product of marks finds.  What tree nodes have, which
-          // may be infinite, is added by the join.
-          unsigned int all = 0u;  // exponents of nothing but ones carry into the sign's place
+          for (int dt = d0; dt < d0 + PAIR && dt < DT; ++dt) {
+            const s16x4 v0 = lds_read_tr((vread ^ (dt << 6)) + 16 * kb * ROWB), v1 = lds_read_tr((vread ^ (dt << 6) ^ 32) + (16 * kb + 8) * ROWB);
+            vr[dt - d0] = __builtin_bit_cast(u32x4, s16x8{v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]});
+          }
+          if (mixed) {
+            // A value that is no number must not reach the rows that do not see its key, and 0 times it is no number: such values take part
+            // as 0.  A cached one is NaN and makes the rows that see it NaN, by an infinity from either side: products too large for a
+            // float for the rows that see it, of 0 for the others.  What tree nodes have, which may be infinite, is added by the join.
+            unsigned int all = 0u;  // exponents of nothing but ones carry into the sign's place
 #pragma unroll
-          for (int dt = 0; dt < DT; ++dt)
+            for (int dt = d0; dt < d0 + PAIR && dt < DT; ++dt)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) all |= (vr[dt][e] & 0x7f807f80u) + 0x00800080u;
-          if (__builtin_amdgcn_ballot_w64((all & 0x80008000u) != 0u) != 0ull) {
-            odd |= tree;
+              for (int e = 0; e < 4; ++e) all |= (vr[dt - d0][e] & 0x7f807f80u) + 0x00800080u;
+            if (__builtin_amdgcn_ballot_w64((all & 0x80008000u) != 0u) != 0ull) {
+              odd |= tree;
+              u32x4 sees;
 #pragma unroll
-            for (int dt = 0; dt < DT; ++dt) {
-              u32x4 mark;
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const unsigned int t = ((vr[dt][e] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
-                mark[e] = (t >> 15) * 0x3f80u;  // 1 in bf16
-                vr[dt][e] &= ~((t >> 15) * 0xffffu);
+              for (int e = 0; e < 4; ++e) {  // registers 8 kb + 2 e, + 1: 2^127 or 0
+                const int bit = 16 * kb + 8 * (e / 2) + 2 * (e % 2);
+                sees[e] = ((vis >> bit) & 1u) * 0x7f00u + ((vis >> (bit + 1)) & 1u) * 0x7f000000u;
               }
 #pragma unroll
-              for (int qt = 0; qt < QT; ++qt) {
-                if (tree) continue;
-                u32x4 sees;
+              for (int dt = d0; dt < d0 + PAIR && dt < DT; ++dt) {
+                u32x4 mark;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {  // registers 8 kb + 2 e, + 1
-                  const int i = 8 * kb + 2 * e, bit = 8 * (i / 4) + i % 4;
-                  sees[e] = ((vis[qt] >> bit) & 1u) * 0x3f80u + ((vis[qt] >> (bit + 1)) & 1u) * 0x3f800000u;
+                for (int e = 0; e < 4; ++e) {
+                  const unsigned int bad = (((vr[dt - d0][e] & 0x7f807f80u) + 0x00800080u) & 0x80008000u) >> 15;
+                  mark[e] = bad * 0x7f00u;
+                  vr[dt - d0][e] &= ~(bad * 0xffffu);
                 }
-                f32x16 count;
+                if (!tree) {
+                  o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, mark), __builtin_bit_cast(bf16x8, sees), o[dt], 0, 0, 0);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) count[i] = 0.f;
-                count = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, mark), __builtin_bit_cast(bf16x8, sees), count, 0, 0, 0);
-#pragma unroll
-                for (int i = 0; i < 16; ++i) o[qt][dt][i] = count[i] > 0.f ? __uint_as_float(0x7fc00000u) : o[qt][dt][i];
+                  for (int e = 0; e < 4; ++e) mark[e] |= 0x80008000u;
+                  o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, mark), __builtin_bit_cast(bf16x8, sees), o[dt], 0, 0, 0);
+                }
               }
             }
           }
-        }
 #pragma unroll
-        for (int qt = 0; qt < QT; ++qt)
-#pragma unroll
-          for (int dt = 0; dt < DT; ++dt) {
-            const bf16x8 v = __builtin_bit_cast(bf16x8, vr[dt]);
-            o[qt][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(bf16x8, hi[qt][kb]), o[qt][dt], 0, 0, 0);
+          for (int dt = d0; dt < d0 + PAIR && dt < DT; ++dt) {
+            const bf16x8 v = __builtin_bit_cast(bf16x8, vr[dt - d0]);
+            o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(bf16x8, hi), o[dt], 0, 0, 0);
             if constexpr (SH::FINE) {
-              o[qt][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(bf16x8, lo[qt][kb]), o[qt][dt], 0, 0, 0);
-              o[qt][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(bf16x8, rest[qt][kb]), o[qt][dt], 0, 0, 0);
+              o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(bf16x8, lo), o[dt], 0, 0, 0);
+              o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(bf16x8, rest), o[dt], 0, 0, 0);
             }
+            asm volatile("" : "+v"(o[dt]) : : "memory");
           }
+        }
       }
       asm volatile("" ::: "memory");  // (the next tile's values go where these were read)
+    };
+
+    // ---- cached tiles --------------------------------------------------------------------------------------------------------
+    for (int x = first; x < cached_end; x += kQ4Tiles) {
+      const int tile = x < tiles.lead ? x : x + tiles.gap;
+      f32x16 s;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+      for (int k = 0; k < KB; ++k) {
+        const float scale = scale_of(kscale, k);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, q4_decode(kraw[k][e], scale)), __builtin_bit_cast(bf16x8, qf[4 * k + e]), s, 0, 0, 0);
+          asm volatile("" : "+v"(s), "+v"(kraw[k]));  // (this product before the next conversions: all of them do not fit the registers)
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < VB; ++k) {
+        if (!SH::v_there(lane, k)) continue;
+        const float scale = scale_of(vscale, k);
+        unsigned int to = vwrite0;
+        asm volatile("" : "+v"(to));
+        if (k > 0) to = SH::PAIRS ? to ^ 64 : vwrite(k);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) *(__attribute__((address_space(3))) u32x4*)(to ^ (e << 4)) = q4_decode(vraw[k][e], scale);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      asm volatile("" ::: "memory");
+      if (x + kQ4Tiles < cached_end) fetch(x + kQ4Tiles);
+      const bool mixed = 32 * tile + 32 > L || (p.window > 0 && 32 * tile <= L + p.max_nodes - 1 - p.window);
+      unsigned int vis = 0xffffffffu;
+      if (mixed) {
+        const int left = L - 32 * tile;
+        vis = left >= 32 ? 0xffffffffu : (1u << left) - 1u;
+        if (p.window > 0) {
+          const int from = low - 32 * tile, sunk = p.sink - 32 * tile;
+          vis &= (from <= 0 ? 0xffffffffu : (from >= 32 ? 0u : 0xffffffffu << from)) | (sunk >= 32 ? 0xffffffffu : (sunk <= 0 ? 0u : (1u << sunk) - 1u));
+        }
+        vis >>= 4 * (lane >> 5);
+      }
+      weigh(s, false, mixed, vis);
+    }
+    // ---- tree nodes: keys as they are, values into the tile as they are (nodes that are none: the last one) -------------------------------
+    Q4Mask seen = {0ull, 0ull};
+    if (end > tiles.count) {
+      int fresh = lane, heads = p.group;
+      asm volatile("" : "+v"(fresh), "+s"(heads));
+      int row = blk * kQ4Rows + (fresh & 31);
+      row = row < n * heads ? row / heads : 0;
+      seen = q4_tree_mask(p, b, row, n, L, p.window > 0 ? q4_depth(p, b, row) : 0);
+    }
+    for (int x = first < tiles.count ? first + (tiles.count - first + kQ4Tiles - 1) / kQ4Tiles * kQ4Tiles : first; x < end; x += kQ4Tiles) {
+      int fresh = lane;  // (as something new: what only these tiles need is formed here, not kept in registers all the way)
+      asm volatile("" : "+v"(fresh));
+      const int tile = x - tiles.count, c = fresh & 31, h2 = fresh >> 5, key = 32 * tile + c < n ? 32 * tile + c : n - 1;
+      const size_t tree0 = ((size_t)b * p.H_kv + kh) * p.max_nodes * (size_t)(p.dh * 2);
+      const unsigned char* kt = p.k_tree + tree0 + (size_t)key * (p.dh * 2);
+      const unsigned char* vt = p.v_tree + tree0;
+      f32x16 s;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+      for (int i = 0; i < QU; ++i) {
+        const int at = 32 * (KB * h2 + i / 4) + 8 * (i % 4);
+        const u32x4 a = at < p.dh ? *(const u32x4*)(kt + at * 2) : u32x4{0u, 0u, 0u, 0u};
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, qf[i]), s, 0, 0, 0);
+        if (i % 4 == 3) asm volatile("" : "+v"(s) : : "memory");
+      }
+#pragma unroll
+      for (int i = 0; i < 2 * DT; ++i) {  // 128 DT chunks of 8 components
+        const int y = fresh + 64 * i, row = y / (4 * DT), ch = y % (4 * DT), from = 32 * tile + row < n ? 32 * tile + row : n - 1;
+        const u32x4 v = 8 * ch < p.dh ? *(const u32x4*)(vt + (size_t)from * (p.dh * 2) + ch * 16) : u32x4{0u, 0u, 0u, 0u};
+        *(__attribute__((address_space(3))) u32x4*)(vbase + row * ROWB + ((ch ^ SH::place(row)) << 4)) = v;
+        if (i % 4 == 3) asm volatile("" : : : "memory");
+      }
+      asm volatile("" ::: "memory");
+      weigh(s, true, true, seen.tile(tile) >> (4 * h2));
     }
 
     // ---- the four wavefronts' parts joined: 2 to 0 and 3 to 1, then 1 to 0 -------------------------------------------------------
@@ -454,60 +471,51 @@ __global__ __launch_bounds__(64 * SH::NW, SH::WPE) void q4_attn_kernel(Q4AttnPar
 #pragma unroll
     for (int half = 2; half >= 1; half /= 2) {
       if (wave >= half && wave < 2 * half) {
+        float* its = part + (wave - half) * (SH::PART / 4);
 #pragma unroll
-        for (int qt = 0; qt < QT; ++qt) {
-          float* its = part + ((wave - half) * QT + qt) * (SH::PART / 4);
+        for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-          for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              *(f32x4*)(its + el * 4 + (dt * 4 + i) * 256) = f32x4{o[qt][dt][4 * i], o[qt][dt][4 * i + 1], o[qt][dt][4 * i + 2], o[qt][dt][4 * i + 3]};
-          its[DT * 1024 + el] = m_run[qt];
-          its[DT * 1024 + 64 + el] = l_run[qt];
-        }
+          for (int i = 0; i < 4; ++i)
+            *(f32x4*)(its + el * 4 + (dt * 4 + i) * 256) = f32x4{o[dt][4 * i], o[dt][4 * i + 1], o[dt][4 * i + 2], o[dt][4 * i + 3]};
+        its[DT * 1024 + el] = m_run;
+        its[DT * 1024 + 64 + el] = l_run;
       }
       __syncthreads();
       if (wave < half) {
+        const float* its = part + wave * (SH::PART / 4);
+        const float mo = its[DT * 1024 + el], lother = its[DT * 1024 + 64 + el];
+        const float m = fmaxf(m_run, mo), base = m > -INFINITY ? m : 0.f;
+        const float a0 = __builtin_amdgcn_exp2f(m_run - base), a1 = __builtin_amdgcn_exp2f(mo - base);
+        l_run = l_run * a0 + lother * a1;
 #pragma unroll
-        for (int qt = 0; qt < QT; ++qt) {
-          const float* its = part + (wave * QT + qt) * (SH::PART / 4);
-          const float mo = its[DT * 1024 + el], lother = its[DT * 1024 + 64 + el];
-          const float m = fmaxf(m_run[qt], mo), base = m > -INFINITY ? m : 0.f;
-          const float a0 = __builtin_amdgcn_exp2f(m_run[qt] - base), a1 = __builtin_amdgcn_exp2f(mo - base);
-          l_run[qt] = l_run[qt] * a0 + lother * a1;
+        for (int dt = 0; dt < DT; ++dt) {
+          __builtin_amdgcn_sched_barrier(0);  // (32 components at a time: all reads ahead do not fit the registers)
 #pragma unroll
-          for (int dt = 0; dt < DT; ++dt) {
-            __builtin_amdgcn_sched_barrier(0);  // (32 components at a time: all reads ahead do not fit the registers)
+          for (int i = 0; i < 4; ++i) {
+            const f32x4 x = *(const f32x4*)(its + el * 4 + (dt * 4 + i) * 256);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const f32x4 x = *(const f32x4*)(its + el * 4 + (dt * 4 + i) * 256);
-#pragma unroll
-              for (int e = 0; e < 4; ++e) o[qt][dt][4 * i + e] = o[qt][dt][4 * i + e] * a0 + x[e] * a1;
-            }
+            for (int e = 0; e < 4; ++e) o[dt][4 * i + e] = o[dt][4 * i + e] * a0 + x[e] * a1;
           }
-          m_run[qt] = m;
         }
+        m_run = m;
       }
       __syncthreads();
     }
     if (threadIdx.x == 0) p.odd[slot] = table[kOdd][0];
     // ---- what the segment leaves, in the order of the registers -------------------------------------------------------------
     if (wave == 0) {
+      l_run = half_sum(l_run);
+      if (blk * kQ4Rows + (el & 31) < n * p.group) {
+        float* po = p.po + (size_t)slot * (DT * 1024) + el * 4;
 #pragma unroll
-      for (int qt = 0; qt < QT; ++qt) {
-        l_run[qt] += __shfl_xor(l_run[qt], 32, 64);
-        if (blk * R + qt * 32 + (el & 31) < n * p.group) {
-          float* po = p.po + ((size_t)slot * QT + qt) * (DT * 1024) + el * 4;
+        for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-          for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              *(f32x4*)(po + (dt * 4 + i) * 256) = f32x4{o[qt][dt][4 * i], o[qt][dt][4 * i + 1], o[qt][dt][4 * i + 2], o[qt][dt][4 * i + 3]};
-          if (el < 32) {
-            float* ml = p.pml + (size_t)slot * 2 * R + qt * 32 + el;
-            ml[0] = m_run[qt];
-            ml[R] = l_run[qt];
-          }
+          for (int i = 0; i < 4; ++i)
+            *(f32x4*)(po + (dt * 4 + i) * 256) = f32x4{o[dt][4 * i], o[dt][4 * i + 1], o[dt][4 * i + 2], o[dt][4 * i + 3]};
+        if (el < 32) {
+          float* ml = p.pml + (size_t)slot * (2 * kQ4Rows) + el;
+          ml[0] = m_run;
+          ml[kQ4Rows] = l_run;
         }
       }
     }
@@ -520,14 +528,14 @@ __global__ __launch_bounds__(64 * SH::NW, SH::WPE) void q4_attn_kernel(Q4AttnPar
 // components of them, in the order of their keys, four at a time under way.
 template <typename SH>
 __global__ __launch_bounds__(64 * SH::DT) void q4_join_kernel(Q4AttnParams p) {
-  constexpr int DT = SH::DT, R = SH::R;
+  constexpr int DT = SH::DT;
   const int lane = threadIdx.x & 63, dt = threadIdx.x >> 6, c = lane & 31, h2 = lane >> 5;
   const int kh = blockIdx.y, b = blockIdx.z, r = blockIdx.x * 32 + c;
   const Q4Work t = q4_read_work<SH>(p);
   const int n = __builtin_amdgcn_readlane(t.n, b), L = __builtin_amdgcn_readlane(t.ctx, b);
   if ((int)blockIdx.x * 32 >= n * p.group) return;
-  const Deal d = prefix_deal(t.units, SH::GROUPS);
-  const int iters = __builtin_amdgcn_readlane(t.iters, b), blk = uniform(blockIdx.x * 32 / R);
+  const Deal d = prefix_deal(t.units, kQ4Groups);
+  const int iters = __builtin_amdgcn_readlane(t.iters, b), blk = blockIdx.x;
   const int first = kh * t.head_units + __builtin_amdgcn_readlane(t.unit0, b) + blk * q4_units(iters) + prefix_block_units(false);
   const int item = kh * t.head_blocks + __builtin_amdgcn_readlane(t.block0, b) + blk;
   const int w0 = d.owner(first), w1 = d.owner(first + (iters - 1) * kPrefixOwnWeight);
@@ -536,8 +544,8 @@ __global__ __launch_bounds__(64 * SH::DT) void q4_join_kernel(Q4AttnParams p) {
   f32x4 o[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const float* ml = p.pml + (size_t)item * 2 * R + r % R;
-  const float* po = p.po + ((size_t)item * (R / 32) + r % R / 32) * (DT * 1024) + dt * 1024 + lane * 4;
+  const float* ml = p.pml + (size_t)item * (2 * kQ4Rows) + c;
+  const float* po = p.po + (size_t)item * (DT * 1024) + dt * 1024 + lane * 4;
   constexpr int kBatch = 4;
   int odd = 0;
   for (int w = w0; w <= w1; w += kBatch) {
@@ -546,10 +554,10 @@ __global__ __launch_bounds__(64 * SH::DT) void q4_join_kernel(Q4AttnParams p) {
 #pragma unroll
     for (int q = 0; q < kBatch; ++q) {  // (behind the last one: the last one again, with no weight)
       const size_t s = w + q < w1 ? w + q : w1;
-      pm[q] = ml[s * 2 * R];
-      pl[q] = ml[s * 2 * R + R];
+      pm[q] = ml[s * (2 * kQ4Rows)];
+      pl[q] = ml[s * (2 * kQ4Rows) + kQ4Rows];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) x[q][i] = *(const f32x4*)(po + s * (R / 32) * (DT * 1024) + i * 256);
+      for (int i = 0; i < 4; ++i) x[q][i] = *(const f32x4*)(po + s * (DT * 1024) + i * 256);
       odd |= p.odd[s + item];
     }
     float top = m;
@@ -605,29 +613,29 @@ __global__ __launch_bounds__(64 * SH::DT) void q4_join_kernel(Q4AttnParams p) {
 }
 
 // ---- host side -----------------------------------------------------------------------------------------------------------
-template <int QT, int DT, typename F>
+template <int DT, typename F>
 static hipError_t q4_with_precision(bool fine, F&& f) {
-  return fine ? f(Q4Shape<QT, DT, true>{}) : f(Q4Shape<QT, DT, false>{});
-}
-template <int QT, typename F>
-static hipError_t q4_with_dim(int blocks, bool fine, F&& f) {
-  return blocks <= 2 ? q4_with_precision<QT, 2>(fine, f) : (blocks == 3 ? q4_with_precision<QT, 3>(fine, f) : q4_with_precision<QT, 4>(fine, f));
+  return fine ? f(Q4Shape<DT, true>{}) : f(Q4Shape<DT, false>{});
 }
 template <typename F>
-static hipError_t q4_with_shape(int rows, int blocks, bool fine, F&& f) {
-  return rows == 32 ? q4_with_dim<1>(blocks, fine, f) : q4_with_dim<2>(blocks, fine, f);
+static hipError_t q4_with_shape(int blocks, bool fine, F&& f) {
+  switch (blocks) {
+    case 1: return q4_with_precision<1>(fine, f);
+    case 2: return q4_with_precision<2>(fine, f);
+    case 3: return q4_with_precision<3>(fine, f);
+    default: return q4_with_precision<4>(fine, f);
+  }
 }
 
 hipError_t prepare_q4_attn() {
   hipError_t e = hipSuccess;
-  for (int rows = 32; rows <= 64; rows *= 2)
-    for (int blocks = 2; blocks <= 4; ++blocks)
-      for (int fine = 0; fine < 2; ++fine)
-        if (e == hipSuccess)
-          e = q4_with_shape(rows, blocks, fine, [](auto shape) {
-            using SH = decltype(shape);
-            return hipFuncSetAttribute((const void*)q4_attn_kernel<SH>, hipFuncAttributeMaxDynamicSharedMemorySize, SH::LDS);
-          });
+  for (int blocks = 1; blocks <= 4; ++blocks)
+    for (int fine = 0; fine < 2; ++fine)
+      if (e == hipSuccess)
+        e = q4_with_shape(blocks, fine, [](auto shape) {
+          using SH = decltype(shape);
+          return hipFuncSetAttribute((const void*)q4_attn_kernel<SH>, hipFuncAttributeMaxDynamicSharedMemorySize, SH::LDS);
+        });
   return e;
 }
 
@@ -667,6 +675,7 @@ extern "C" int q4_verify_attn(ctcspec_ctx* ctx, ctcspec_dtype dt, const void* q,
                   "q4_verify_attn: capacities or rows beyond 2^30, or work of more than 2^31 units");
   for (const void* a : {q, (const void*)cache->k_codes, (const void*)cache->v_codes, k_tree, v_tree, (const void*)workspace, (const void*)out})
     CTCSPEC_REQUIRE(ctx, aligned16(a), CTCSPEC_EINVAL, "q4_verify_attn: pointers must be 16-byte aligned");
+  CTCSPEC_REQUIRE(ctx, q4_scales_aligned(cache), CTCSPEC_EINVAL, "q4_verify_attn: scales must be 4-byte aligned");
   const Q4Workspace ws = q4_workspace(B, H, H_kv, dh, max_nodes);
   CTCSPEC_REQUIRE(ctx, workspace_bytes >= ws.total, CTCSPEC_EINVAL, "q4_verify_attn: workspace of %zu bytes needed, %zu given", ws.total,
                   workspace_bytes);
@@ -678,7 +687,7 @@ extern "C" int q4_verify_attn(ctcspec_ctx* ctx, ctcspec_dtype dt, const void* q,
   p.kv_off = kv_off; p.ctx_len = ctx_len;
   p.k_tree = (const unsigned char*)k_tree; p.v_tree = (const unsigned char*)v_tree; p.n_nodes = n_nodes; p.depth = window ? node_depth : nullptr;
   p.anc_mask = (const unsigned long long*)anc_mask;
-  p.kv_cap = kv_cap; p.B = B; p.H = H; p.H_kv = H_kv; p.group = H / H_kv; p.dh = dh; p.blocks = q4_blocks(dh); p.max_nodes = max_nodes;
+  p.kv_cap = kv_cap; p.B = B; p.H = H; p.H_kv = H_kv; p.group = H / H_kv; p.dh = dh; p.max_nodes = max_nodes;
   // (positions stay below 2^30 + 128: a longer window or sink is one that holds them all)
   p.window = window < (1 << 30) + 256 ? window : (1 << 30) + 256;
   p.sink = sink < (1 << 30) + 256 ? sink : (1 << 30) + 256;
@@ -686,9 +695,9 @@ extern "C" int q4_verify_attn(ctcspec_ctx* ctx, ctcspec_dtype dt, const void* q,
   p.po = (float*)(base + ws.o); p.pml = (float*)(base + ws.ml); p.odd = (int*)(base + ws.odd);
   p.out_bf16 = out_dt == CTCSPEC_BF16; p.out = out; p.lse = lse;
   hipStream_t st = ctx->stream;
-  const hipError_t e = q4_with_shape(ws.rows, p.blocks, out_dt == CTCSPEC_F32, [&](auto shape) {
+  const hipError_t e = q4_with_shape(q4_blocks(dh), out_dt == CTCSPEC_F32, [&](auto shape) {
     using SH = decltype(shape);
-    hipLaunchKernelGGL(q4_attn_kernel<SH>, dim3(SH::GROUPS), dim3(64 * SH::NW), SH::LDS, st, p);
+    hipLaunchKernelGGL(q4_attn_kernel<SH>, dim3(kQ4Groups), dim3(64 * SH::NW), SH::LDS, st, p);
     if (const hipError_t e1 = hipGetLastError(); e1 != hipSuccess) return e1;
     hipLaunchKernelGGL(q4_join_kernel<SH>, dim3((unsigned)((seq_rows + 31) / 32), (unsigned)H_kv, (unsigned)B), dim3(64 * SH::DT), 0, st, p);
     return hipGetLastError();

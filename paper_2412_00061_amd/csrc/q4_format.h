@@ -14,6 +14,9 @@ constexpr int kQ4NoNumber = 255;
 constexpr int kQ4MinScale = 2, kQ4MaxScale = 252;
 
 __host__ __device__ inline int q4_blocks(int dh) { return (dh + kQ4Block - 1) / kQ4Block; }
+inline bool q4_scales_aligned(const ctcspec_q4_cache* cache) {
+  return ((reinterpret_cast<uintptr_t>(cache->k_scales) | reinterpret_cast<uintptr_t>(cache->v_scales)) & 3u) == 0;
+}
 
 #if defined(__HIP_DEVICE_COMPILE__)
 

@@ -8,8 +8,9 @@ namespace ctcspec {
 
 constexpr int kQ4Tiles = 4;  // tiles of 32 keys in an iteration: one for each wavefront of a workgroup
 
-// Query rows of a workgroup: a sequence's rows (nodes x heads that share a key head) for as long as they fit.
-inline int q4_block_rows(long long rows) { return rows <= 32 ? 32 : 64; }
+constexpr int kQ4Rows = 32;    // query rows of a workgroup: nodes of a sequence x heads that share a key head
+constexpr int kQ4Waves = 3;    // workgroups that a compute unit holds at once, and wavefronts of each of its four SIMDs
+constexpr int kQ4Groups = 256 * kQ4Waves;
 
 // The cached tiles that a window leaves: the first `lead`, then those from lead + gap on; `count` of them.  A row at position p >= len sees
 // keys above p - window and below sink, so the tiles between the sink and position len - window stay out.
@@ -37,14 +38,12 @@ CTCSPEC_BOTH constexpr int q4_units(int iters) { return prefix_block_units(false
 // Rows, keys and units are counted in 32 bits: whether that is enough for the largest lengths.
 inline bool q4_units_fit(long long B, int H_kv, long long seq_rows, int kv_cap, int max_nodes) {
   if (seq_rows > 1LL << 30 || kv_cap > 1 << 30) return false;
-  const int rows = q4_block_rows(seq_rows);
   const long long tiles = (kv_cap + 31LL) / 32 + (max_nodes + 31) / 32;
   const double block = prefix_block_units(false) + (double)kPrefixOwnWeight * (double)((tiles + kQ4Tiles - 1) / kQ4Tiles);
-  return (double)B * (double)((seq_rows + rows - 1) / rows) * block * H_kv < 2147483647.0;
+  return (double)B * (double)((seq_rows + kQ4Rows - 1) / kQ4Rows) * block * H_kv < 2147483647.0;
 }
 
 struct Q4Workspace {
-  int rows;  // of a workgroup
   size_t o, ml, odd, total;
 };
 // Numbers of partial results: below workgroups + blocks.
@@ -53,11 +52,10 @@ inline Q4Workspace q4_workspace(int B, int H, int H_kv, int dh, int max_nodes) {
   size_t off = 0;
   auto carve = [&](size_t bytes) { size_t at = off; off = (off + bytes + 255) / 256 * 256; return at; };
   const long long seq_rows = (long long)max_nodes * (H / H_kv);
-  w.rows = q4_block_rows(seq_rows);
-  const size_t slots = kPrefixMaxGroups + (size_t)H_kv * B * (size_t)((seq_rows + w.rows - 1) / w.rows);
-  const int tiles = dh <= 64 ? 2 : (dh + 31) / 32;  // of 32 components
-  w.o = carve(slots * w.rows * tiles * 32 * sizeof(float));
-  w.ml = carve(slots * w.rows * 2 * sizeof(float));
+  const size_t slots = kQ4Groups + (size_t)H_kv * B * (size_t)((seq_rows + kQ4Rows - 1) / kQ4Rows);
+  const int tiles = (dh + 31) / 32;  // of 32 components
+  w.o = carve(slots * kQ4Rows * tiles * 32 * sizeof(float));
+  w.ml = carve(slots * kQ4Rows * 2 * sizeof(float));
   w.odd = carve(slots * sizeof(int));
   w.total = off;
   return w;

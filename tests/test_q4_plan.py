@@ -21,7 +21,7 @@ int main() {
       printf("%d 0 0\n", (int)q4_units_fit(a, b, c, d, e));
     } else {
       const Q4Workspace w = q4_workspace(a, b, c, d, e);
-      printf("%d %zu %zu\n", w.rows, w.o, w.total);
+      printf("%d %zu %zu\n", kQ4Groups, w.o, w.total);
     }
   }
 }
@@ -60,8 +60,6 @@ def test_units_are_counted_for_the_largest_lengths():
 
 def test_workspace_has_room_for_every_partial_result():
     for B, H, Hkv, dh, N in ((1, 1, 1, 8, 1), (8, 32, 32, 128, 64), (64, 40, 8, 96, 128), (3, 32, 1, 64, 1)):
-        (rows, o, total), = ask([("w", B, H, Hkv, dh, N)])
-        seq = N * H // Hkv
-        slots = 512 + Hkv * B * -(-seq // rows)
-        assert rows == (32 if seq <= 32 else 64) and o == 0
-        assert total >= slots * (rows * (max(64, -(-dh // 32) * 32) + 2) + 1) * 4
+        (groups, o, total), = ask([("w", B, H, Hkv, dh, N)])
+        slots = groups + Hkv * B * -(-(N * H // Hkv) // 32)  # a part for each workgroup, and one more where a block of rows ends in its share
+        assert o == 0 and total >= slots * (32 * (-(-dh // 32) * 32 + 2) + 1) * 4

@@ -34,6 +34,7 @@ BAD += [(name, key, value, UNSUPPORTED, "limits") for name, args in CALLS.items(
         for key, value in (("B", 9), ("H", 9), ("dh", 128), ("cap", (1 << 30) + 1), ("max_rows", (1 << 30) + 1), ("N", 65)) if key in args]
 BAD += [(name, key, P + 8, INVALID, "aligned") for name in CALLS for key in ("k", "v")]
 BAD += [(name, "cache", cache(**{part: P + 4}), INVALID, "aligned") for name in CALLS for part in ("k_codes", "v_codes")]
+BAD += [(name, "cache", cache(**{part: P + 2}), INVALID, "4-byte") for name in [*CALLS, "q4_verify_attn"] for part in ("k_scales", "v_scales")]
 BAD += [("kv_commit_q4", "T", 9, UNSUPPORTED, "T <= 8"), ("kv_append_q4", "out", P, INVALID, "ctx_len_out"), ("kv_commit_q4", "out", P, INVALID, "ctx_len_out")]
 
 
