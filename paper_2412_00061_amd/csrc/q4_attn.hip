@@ -52,24 +52,23 @@ struct Q4Shape {
   static constexpr bool FINE = FINE_;
   static constexpr int KB = (DT + 1) / 2, QU = 4 * KB;        // blocks of a key in a lane; steps of 16 elements of a product
   static constexpr int VB = (DT + 1) / 2;                     // blocks of values in a lane: 32 DT of them in 64 lanes
-  static constexpr int ROWB = DT <= 2 ? 128 : 256, TILE = 32 * ROWB;  // values in the LDS
+  // Values in the LDS: a row has 64 bytes a block and as many more as make an odd number of them, four rows have 16 bytes more.  A transposing
+  // read of 32 lanes takes 64 bytes of each of four consecutive rows, which then lie in different banks; a write of 16 lanes (0 to 7 with 16
+  // to 23) the same 16 bytes of their blocks, which do if the lanes' rows are of four such groups, two of each (v_row).
+  static constexpr int ROWB = 64 * (DT | 1), FOURB = 4 * ROWB + 16, TILE = 8 * FOURB;
+  static __device__ __forceinline__ int place(int row) { return (row >> 2) * FOURB + (row & 3) * ROWB; }
   static constexpr int PART = (DT * 16 + 2) * 64 * 4;         // O, m, l of 32 rows
   static constexpr int STAGE = NW * TILE > 2 * PART ? NW * TILE : 2 * PART;
-  static constexpr int LDS = STAGE + 6 * 64 * 4;              // and the sequences' table: behind the tiles, whose places are formed by xor
+  static constexpr int LDS = STAGE + 6 * 64 * 4;              // and the sequences' table
   static_assert(kQ4Waves * LDS <= 160 * 1024 && kQ4Groups % 8 == 0);
-  // 16-byte chunk c of row r lies at chunk c ^ place(r).  A transposing read of 32 lanes takes four chunks of each of four consecutive
-  // rows: these differ in the chunk's upper bits (rows of 128 bytes: in every second row).  A write of eight lanes takes the same chunk of
-  // a block from rows that are four apart: these differ in its lower bits.
-  static __device__ __forceinline__ int place(int r) { return (ROWB == 256 ? (r & 3) << 2 : ((r >> 1) & 1) << 2) ^ ((r >> 2) & 3); }
   // The blocks of values that a lane converts: row and block of the row of its k-th.  (Four blocks a row: two neighbours of a row; else
   // those 64 further.)
   static constexpr bool PAIRS = DT == 4;
   static __device__ __forceinline__ int v_row(int lane, int k) {
-    const int a = PAIRS ? lane / 2 : (lane + 64 * k) / DT;
-    if constexpr (ROWB == 128) return (a & 1) | ((a >> 1) & 7) << 2 | ((a >> 4) & 1) << 1;
-    else return (a & 7) << 2 | a >> 3;
+    const int a = PAIRS ? lane >> 1 : (int)((unsigned)(lane + 64 * k) / DT);
+    return PAIRS ? (a & 25) | (a & 2) << 1 | (a & 4) >> 1 : (DT == 2 ? (a & 24) | (a & 1) << 1 | (a & 2) << 1 | (a & 4) >> 2 : a);
   }
-  static __device__ __forceinline__ int v_block(int lane, int k) { return PAIRS ? 2 * (lane % 2) + k : (lane + 64 * k) % DT; }
+  static __device__ __forceinline__ int v_block(int lane, int k) { return PAIRS ? 2 * (lane & 1) + k : (int)((unsigned)(lane + 64 * k) % DT); }
   static __device__ __forceinline__ bool v_there(int lane, int k) { return DT % 2 == 0 || lane + 64 * k < 32 * DT; }
 };
 
@@ -159,7 +158,7 @@ template <typename SH>
 __global__ __launch_bounds__(64 * SH::NW, kQ4Waves) void q4_attn_kernel(Q4AttnParams p) {
 #if defined(__HIP_DEVICE_COMPILE__)
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-  constexpr int DT = SH::DT, KB = SH::KB, VB = SH::VB, QU = SH::QU, ROWB = SH::ROWB;
+  constexpr int DT = SH::DT, KB = SH::KB, VB = SH::VB, QU = SH::QU;
   const int lane = threadIdx.x & 63;
   const int wave = uniform(threadIdx.x >> 6);
   const Q4Work t = q4_read_work<SH>(p);
@@ -185,15 +184,15 @@ __global__ __launch_bounds__(64 * SH::NW, kQ4Waves) void q4_attn_kernel(Q4AttnPa
   unsigned char* vtile = smem + wave * SH::TILE;
   const unsigned int vbase = (unsigned int)(size_t)(lds_byte*)vtile;
   // the transposing read: 16 lanes fetch 4 rows x 16 components, 8 bytes each, and lane s of them receives component s of the four rows
-  unsigned int vread0;
+  unsigned int vread;
   {
     const int s = lane & 15, row = 4 * (lane >> 5) + (s >> 2), ch = (((lane & 31) >> 4) << 1) + ((s & 3) >> 1);
-    vread0 = vbase + row * ROWB + ((ch ^ SH::place(row)) << 4) + (s & 1) * 8;
+    vread = vbase + SH::place(row) + ch * 16 + (s & 1) * 8;
   }
   // where this lane's k-th block of values goes in the tile
   auto vwrite = [&](int k) __attribute__((always_inline)) -> unsigned int {
     const int row = SH::v_there(lane, k) ? SH::v_row(lane, k) : 0, blk = SH::v_there(lane, k) ? SH::v_block(lane, k) : 0;
-    return vbase + row * ROWB + (((4 * blk) ^ SH::place(row)) << 4);
+    return vbase + SH::place(row) + blk * 64;
   };
   const unsigned int vwrite0 = vwrite(0);
 
@@ -217,7 +216,8 @@ __global__ __launch_bounds__(64 * SH::NW, kQ4Waves) void q4_attn_kernel(Q4AttnPa
     if (niter <= 0) continue;
     const Q4Tiles tiles = q4_tiles(L, p.window, p.sink);
     const int total = tiles.count + (n + 31) / 32;
-    const size_t row0 = (size_t)p.kv_off[b] + (size_t)kh * p.kv_cap;
+    const unsigned long long off = (unsigned long long)p.kv_off[b];
+    const size_t row0 = ((size_t)(unsigned)uniform((int)(off >> 32)) << 32 | (unsigned)uniform((int)off)) + (size_t)kh * p.kv_cap;
     // codes and scales of cached tile x of the segment: of key c blocks KB h2 .., of the values blocks lane, lane + 64.  (Rows behind the last
     // one, and blocks behind a row's last, lie outside what the descriptors hold: zeros.)
     u32x4 kraw[KB], vraw[VB];
@@ -248,25 +248,31 @@ __global__ __launch_bounds__(64 * SH::NW, kQ4Waves) void q4_attn_kernel(Q4AttnPa
         vscale[0] = (unsigned short)__builtin_amdgcn_raw_buffer_load_b16(vs, vfrom, 0, 0);
       }
     };
-    auto scale_of = [&](const auto& scales, int k) __attribute__((always_inline)) -> float {
-      return q4_scale_value((int)(SH::PAIRS ? (scales[0] >> (8 * k)) & 255u : scales[k]));
+    auto scale_byte = [&](const auto& scales, int k) __attribute__((always_inline)) -> int {
+      return (int)(SH::PAIRS ? (scales[0] >> (8 * k)) & 255u : scales[k]);
     };
+    auto scale_of = [&](const auto& scales, int k) __attribute__((always_inline)) -> float { return q4_scale_value(scale_byte(scales, k)); };
     const int first = it0 * kQ4Tiles + wave, end = (it0 + niter) * kQ4Tiles < total ? (it0 + niter) * kQ4Tiles : total;
-    const int cached_end = end < tiles.count ? end : tiles.count;
+    // Of the cached tiles those from x_all on, up to x_part, are seen by every row in full.
+    int x_all = p.window > 0 ? L + p.max_nodes - 1 - p.window : -1;
+    x_all = x_all < 0 ? 0 : x_all / 32 + 1 - tiles.gap;
+    const int x_part = L / 32 - tiles.gap, cached_end = end < tiles.count ? end : tiles.count;
     if (first < cached_end) fetch(first);
 
     // ---- this lane's query row: step i of a product has elements 32 (KB h2 + i / 4) + 8 (i % 4) .. + 7 ------------------------------
     u32x4 qf[QU];
     int low;  // the first position of the window
     {
+      int fresh = lane, heads = p.group;
+      asm volatile("" : "+v"(fresh), "+s"(heads));
       // (rows that are none do as row 0 does: nobody reads what comes of it)
-      const int r = blk * kQ4Rows + (seg_lane & 31), row_at = r < n * group ? r : 0;
-      const int h2 = seg_lane >> 5, node = row_at / group, hg = row_at - node * group;
-      const unsigned char* row = p.q + (((size_t)b * p.H + kh * group + hg) * p.max_nodes + node) * (size_t)(p.dh * 2);
+      const int r = blk * kQ4Rows + (fresh & 31), at_row = r < n * heads ? r : 0, node = at_row / heads, hg = at_row - node * heads;
+      const unsigned char* row = p.q + (((size_t)b * p.H + kh * heads + hg) * p.max_nodes + node) * (size_t)(p.dh * 2);
 #pragma unroll
       for (int i = 0; i < QU; ++i) {
-        const int at = 32 * (KB * h2 + i / 4) + 8 * (i % 4);
-        qf[i] = at < p.dh ? *(const u32x4*)(row + at * 2) : u32x4{0u, 0u, 0u, 0u};
+        const int at = 32 * (KB * (fresh >> 5) + i / 4) + 8 * (i % 4);
+        qf[i] = *(const u32x4*)(row + (at < p.dh ? at * 2 : 0));
+        if (p.dh < 64 * KB) qf[i] = at < p.dh ? qf[i] : u32x4{0u, 0u, 0u, 0u};
       }
       low = p.window > 0 ? L + q4_depth(p, b, node) - p.window + 1 : 0;
     }
@@ -284,13 +290,8 @@ __global__ __launch_bounds__(64 * SH::NW, kQ4Waves) void q4_attn_kernel(Q4AttnPa
 
     // S^T = K Q^T: a lane then holds 16 scores of one query row, its neighbour 32 lanes away the other 16 - register i: key
     // 8 (i / 4) + 4 h2 + i % 4 -, and P in the same registers is the right operand of O^T += V^T P.
-    // What follows the scores s of a tile whose values lie in the LDS.  mixed: not every row sees every key; vis: this lane's keys that its
-    // row sees, register i at bit 8 (i / 4) + i % 4.
-    auto weigh = [&](f32x16& s, bool tree, bool mixed, unsigned int vis) __attribute__((always_inline)) {
-      if (mixed) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] = (vis >> (8 * (i / 4) + i % 4)) & 1u ? s[i] : -INFINITY;
-      }
+    // What follows the scores s of a tile whose values lie in the LDS.
+    auto weigh = [&](f32x16& s) __attribute__((always_inline)) {
       // the reference, in the log2 domain, only has to be near the maximum: it is moved when a score exceeds it by more than 2^8
       float mx = s[0];
 #pragma unroll
@@ -306,9 +307,8 @@ __global__ __launch_bounds__(64 * SH::NW, kQ4Waves) void q4_attn_kernel(Q4AttnPa
         }
       }
       const float ms = m_run > -INFINITY ? m_run : 0.f;
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {  // 16 keys each
-        u32x4 hi, lo, rest;
+      u32x4 hi, lo, rest;
+      auto weights = [&](int kb) __attribute__((always_inline)) {  // of 16 keys
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const float p0 = __builtin_amdgcn_exp2f(fmaf(s[8 * kb + 2 * j], p.sl2, -ms)), p1 = __builtin_amdgcn_exp2f(fmaf(s[8 * kb + 2 * j + 1], p.sl2, -ms));
@@ -321,72 +321,33 @@ __global__ __launch_bounds__(64 * SH::NW, kQ4Waves) void q4_attn_kernel(Q4AttnPa
           }
           l_run += p0 + p1;
         }
-        // (two blocks of components at a time: what all of them need at once does not fit the registers)
-        constexpr int PAIR = DT == 4 ? 1 : 2;
+      };
+      // the values of step i: 16 keys i / DT, 32 components i % DT; each is read a step ahead
+      auto values = [&](int i) __attribute__((always_inline)) -> u32x4 {
+        const int kb = i / DT, dt = i % DT;
+        const s16x4 v0 = lds_read_tr(vread + dt * 64 + 4 * kb * SH::FOURB), v1 = lds_read_tr(vread + dt * 64 + (4 * kb + 2) * SH::FOURB);
+        return __builtin_bit_cast(u32x4, s16x8{v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]});
+      };
+      u32x4 next = values(0);
 #pragma unroll
-        for (int d0 = 0; d0 < DT; d0 += PAIR) {
-          u32x4 vr[PAIR];
-          unsigned int vread = vread0;
-          asm volatile("" : "+v"(vread));
-#pragma unroll
-          for (int dt = d0; dt < d0 + PAIR && dt < DT; ++dt) {
-            const s16x4 v0 = lds_read_tr((vread ^ (dt << 6)) + 16 * kb * ROWB), v1 = lds_read_tr((vread ^ (dt << 6) ^ 32) + (16 * kb + 8) * ROWB);
-            vr[dt - d0] = __builtin_bit_cast(u32x4, s16x8{v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]});
-          }
-          if (mixed) {
-            // A value that is no number must not reach the rows that do not see its key, and 0 times it is no number: such values take part
-            // as 0.  A cached one is NaN and makes the rows that see it NaN, by an infinity from either side: products too large for a
-            // float for the rows that see it, of 0 for the others.  What tree nodes have, which may be infinite, is added by the join.
-            unsigned int all = 0u;  // exponents of nothing but ones carry into the sign's place
-#pragma unroll
-            for (int dt = d0; dt < d0 + PAIR && dt < DT; ++dt)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) all |= (vr[dt - d0][e] & 0x7f807f80u) + 0x00800080u;
-            if (__builtin_amdgcn_ballot_w64((all & 0x80008000u) != 0u) != 0ull) {
-              odd |= tree;
-              u32x4 sees;
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {  // registers 8 kb + 2 e, + 1: 2^127 or 0
-                const int bit = 16 * kb + 8 * (e / 2) + 2 * (e % 2);
-                sees[e] = ((vis >> bit) & 1u) * 0x7f00u + ((vis >> (bit + 1)) & 1u) * 0x7f000000u;
-              }
-#pragma unroll
-              for (int dt = d0; dt < d0 + PAIR && dt < DT; ++dt) {
-                u32x4 mark;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                  const unsigned int bad = (((vr[dt - d0][e] & 0x7f807f80u) + 0x00800080u) & 0x80008000u) >> 15;
-                  mark[e] = bad * 0x7f00u;
-                  vr[dt - d0][e] &= ~(bad * 0xffffu);
-                }
-                if (!tree) {
-                  o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, mark), __builtin_bit_cast(bf16x8, sees), o[dt], 0, 0, 0);
-#pragma unroll
-                  for (int e = 0; e < 4; ++e) mark[e] |= 0x80008000u;
-                  o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, mark), __builtin_bit_cast(bf16x8, sees), o[dt], 0, 0, 0);
-                }
-              }
-            }
-          }
-#pragma unroll
-          for (int dt = d0; dt < d0 + PAIR && dt < DT; ++dt) {
-            const bf16x8 v = __builtin_bit_cast(bf16x8, vr[dt - d0]);
-            o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(bf16x8, hi), o[dt], 0, 0, 0);
-            if constexpr (SH::FINE) {
-              o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(bf16x8, lo), o[dt], 0, 0, 0);
-              o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(bf16x8, rest), o[dt], 0, 0, 0);
-            }
-            asm volatile("" : "+v"(o[dt]) : : "memory");
-          }
+      for (int i = 0; i < 2 * DT; ++i) {
+        const int kb = i / DT, dt = i % DT;
+        const u32x4 vr = next;
+        if (i + 1 < 2 * DT) next = values(i + 1);
+        if (dt == 0) weights(kb);
+        const bf16x8 v = __builtin_bit_cast(bf16x8, vr);
+        o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(bf16x8, hi), o[dt], 0, 0, 0);
+        if constexpr (SH::FINE) {
+          o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(bf16x8, lo), o[dt], 0, 0, 0);
+          o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(bf16x8, rest), o[dt], 0, 0, 0);
         }
+        // (step by step: what all of them need at once does not fit the registers)
+        asm volatile("" : "+v"(o[dt]) : : "memory");
       }
       asm volatile("" ::: "memory");  // (the next tile's values go where these were read)
     };
 
-    // ---- cached tiles --------------------------------------------------------------------------------------------------------
-    for (int x = first; x < cached_end; x += kQ4Tiles) {
-      const int tile = x < tiles.lead ? x : x + tiles.gap;
-      f32x16 s;
+    auto cached_scores = [&](f32x16& s) __attribute__((always_inline)) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[i] = 0.f;
 #pragma unroll
@@ -398,73 +359,105 @@ __global__ __launch_bounds__(64 * SH::NW, kQ4Waves) void q4_attn_kernel(Q4AttnPa
           asm volatile("" : "+v"(s), "+v"(kraw[k]));  // (this product before the next conversions: all of them do not fit the registers)
         }
       }
+    };
+    auto cached_values = [&]() __attribute__((always_inline)) {
 #pragma unroll
       for (int k = 0; k < VB; ++k) {
         if (!SH::v_there(lane, k)) continue;
         const float scale = scale_of(vscale, k);
-        unsigned int to = vwrite0;
-        asm volatile("" : "+v"(to));
-        if (k > 0) to = SH::PAIRS ? to ^ 64 : vwrite(k);
+        const unsigned int to = SH::PAIRS || k == 0 ? vwrite0 + 64 * k : vwrite(k);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) *(__attribute__((address_space(3))) u32x4*)(to ^ (e << 4)) = q4_decode(vraw[k][e], scale);
+        for (int e = 0; e < 4; ++e) *(__attribute__((address_space(3))) u32x4*)(to + 16 * e) = q4_decode(vraw[k][e], scale);
         __builtin_amdgcn_sched_barrier(0);
       }
       asm volatile("" ::: "memory");
-      if (x + kQ4Tiles < cached_end) fetch(x + kQ4Tiles);
-      const bool mixed = 32 * tile + 32 > L || (p.window > 0 && 32 * tile <= L + p.max_nodes - 1 - p.window);
-      unsigned int vis = 0xffffffffu;
-      if (mixed) {
-        const int left = L - 32 * tile;
-        vis = left >= 32 ? 0xffffffffu : (1u << left) - 1u;
+    };
+    // A row that does not see a key has no part of it: a score of -infinity, and a value that is a number (0 times another is none).
+    auto hide = [&](f32x16& s, unsigned int vis) __attribute__((always_inline)) {  // vis: the keys of the tile that this lane's row sees
+      vis >>= 4 * (lane >> 5);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = (vis >> (8 * (i / 4) + i % 4)) & 1u ? s[i] : -INFINITY;
+    };
+    // ---- cached tiles -------------------------------------------------------------------------------------------------------------------
+    for (int x = first; x < cached_end; x += kQ4Tiles) {
+      f32x16 s;
+      cached_scores(s);
+      if (x < x_all || x >= x_part) {  // not every row sees every key
+        const int at = 32 * (x < tiles.lead ? x : x + tiles.gap), left = L - at;
+        unsigned int vis = left >= 32 ? 0xffffffffu : (1u << left) - 1u;
         if (p.window > 0) {
-          const int from = low - 32 * tile, sunk = p.sink - 32 * tile;
+          const int from = low - at, sunk = p.sink - at;
           vis &= (from <= 0 ? 0xffffffffu : (from >= 32 ? 0u : 0xffffffffu << from)) | (sunk >= 32 ? 0xffffffffu : (sunk <= 0 ? 0u : (1u << sunk) - 1u));
         }
-        vis >>= 4 * (lane >> 5);
+        hide(s, vis);
+        // blocks of values that are NaN: of the rows that see them here, and zeros for the product
+#pragma unroll
+        for (int k = 0; k < VB; ++k) {
+          const bool nan = SH::v_there(lane, k) && scale_byte(vscale, k) == kQ4NoNumber;
+          unsigned long long lanes = __builtin_amdgcn_ballot_w64(nan);
+          while (lanes != 0ull) {
+            const int from = __builtin_ctzll(lanes), row = SH::v_row(from, k), block = SH::v_block(from, k);
+            lanes &= lanes - 1;
+            const float add = (vis >> row) & 1u ? __builtin_nanf("") : 0.f;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt)
+              if (block == dt) o[dt] += add;
+          }
+          vraw[k] = nan ? u32x4{0u, 0u, 0u, 0u} : vraw[k];
+          if (nan) vscale[SH::PAIRS ? 0 : k] &= ~(SH::PAIRS ? 255u << (8 * k) : 255u);
+        }
       }
-      weigh(s, false, mixed, vis);
+      cached_values();
+      if (x + kQ4Tiles < cached_end) fetch(x + kQ4Tiles);
+      weigh(s);
     }
-    // ---- tree nodes: keys as they are, values into the tile as they are (nodes that are none: the last one) -------------------------------
-    Q4Mask seen = {0ull, 0ull};
-    if (end > tiles.count) {
-      int fresh = lane, heads = p.group;
-      asm volatile("" : "+v"(fresh), "+s"(heads));
-      int row = blk * kQ4Rows + (fresh & 31);
-      row = row < n * heads ? row / heads : 0;
-      seen = q4_tree_mask(p, b, row, n, L, p.window > 0 ? q4_depth(p, b, row) : 0);
-    }
-    for (int x = first < tiles.count ? first + (tiles.count - first + kQ4Tiles - 1) / kQ4Tiles * kQ4Tiles : first; x < end; x += kQ4Tiles) {
-      int fresh = lane;  // (as something new: what only these tiles need is formed here, not kept in registers all the way)
+    // ---- a tile of the tree, of which a wavefront has one at the most: keys as they are, values into the LDS (nodes that are none: zeros) -----
+    static_assert(kQ4Tiles * 32 >= 128);
+    const int x_tree = first + (tiles.count <= first ? 0 : (tiles.count - first + kQ4Tiles - 1) / kQ4Tiles * kQ4Tiles);
+    if (x_tree < end) {
+      int fresh = lane;  // (as something new: what only this tile needs is formed here, not kept in registers all the way)
       asm volatile("" : "+v"(fresh));
-      const int tile = x - tiles.count, c = fresh & 31, h2 = fresh >> 5, key = 32 * tile + c < n ? 32 * tile + c : n - 1;
+      const int c = fresh & 31, h2 = fresh >> 5, tile = x_tree - tiles.count;
       const size_t tree0 = ((size_t)b * p.H_kv + kh) * p.max_nodes * (size_t)(p.dh * 2);
-      const unsigned char* kt = p.k_tree + tree0 + (size_t)key * (p.dh * 2);
-      const unsigned char* vt = p.v_tree + tree0;
+      const auto kt = buffer(p.k_tree + tree0, n * p.dh * 2), vt = buffer(p.v_tree + tree0, n * p.dh * 2);
+      constexpr int kOutside = 0x1000000;
       f32x16 s;
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[i] = 0.f;
 #pragma unroll
       for (int i = 0; i < QU; ++i) {
         const int at = 32 * (KB * h2 + i / 4) + 8 * (i % 4);
-        const u32x4 a = at < p.dh ? *(const u32x4*)(kt + at * 2) : u32x4{0u, 0u, 0u, 0u};
+        const u32x4 a = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(kt, at < p.dh ? ((32 * tile + c) * p.dh + at) * 2 : kOutside, 0, 0));
         s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, qf[i]), s, 0, 0, 0);
         if (i % 4 == 3) asm volatile("" : "+v"(s) : : "memory");
       }
+      // values that are infinite or no numbers: left out, and added by the join to the rows that see them
+      unsigned int strange = 0u;
 #pragma unroll
       for (int i = 0; i < 2 * DT; ++i) {  // 128 DT chunks of 8 components
-        const int y = fresh + 64 * i, row = y / (4 * DT), ch = y % (4 * DT), from = 32 * tile + row < n ? 32 * tile + row : n - 1;
-        const u32x4 v = 8 * ch < p.dh ? *(const u32x4*)(vt + (size_t)from * (p.dh * 2) + ch * 16) : u32x4{0u, 0u, 0u, 0u};
-        *(__attribute__((address_space(3))) u32x4*)(vbase + row * ROWB + ((ch ^ SH::place(row)) << 4)) = v;
+        const int y = fresh + 64 * i, row = y / (4 * DT), ch = y % (4 * DT);
+        u32x4 v = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(vt, 8 * ch < p.dh ? ((32 * tile + row) * p.dh + 8 * ch) * 2 : kOutside, 0, 0));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {  // (exponents of nothing but ones carry into the sign's place)
+          const unsigned int bad = (((v[e] & 0x7f807f80u) + 0x00800080u) & 0x80008000u) >> 15;
+          strange |= bad;
+          v[e] &= ~(bad * 0xffffu);
+        }
+        *(__attribute__((address_space(3))) u32x4*)(vbase + SH::place(row) + ch * 16) = v;
         if (i % 4 == 3) asm volatile("" : : : "memory");
       }
-      asm volatile("" ::: "memory");
-      weigh(s, true, true, seen.tile(tile) >> (4 * h2));
+      odd = __builtin_amdgcn_ballot_w64(strange != 0u) != 0ull;
+      int heads = p.group, row = blk * kQ4Rows + c;
+      asm volatile("" : "+s"(heads));
+      row = row < n * heads ? row / heads : 0;
+      hide(s, q4_tree_mask(p, b, row, n, L, p.window > 0 ? q4_depth(p, b, row) : 0).tile(tile));
+      weigh(s);
     }
 
     // ---- the four wavefronts' parts joined: 2 to 0 and 3 to 1, then 1 to 0 -------------------------------------------------------
     if (threadIdx.x == 0) table[kOdd][0] = 0;
     __syncthreads();  // every tile is consumed: the LDS is free
-    if (__builtin_amdgcn_ballot_w64(odd) != 0ull) table[kOdd][0] = 1;
+    if (odd) table[kOdd][0] = 1;
     float* part = (float*)smem;
     asm volatile("" : "+v"(seg_lane));
     const int el = seg_lane;
