@@ -649,8 +649,8 @@ int kv_read_q4(ctcspec_ctx* ctx, const ctcspec_q4_cache* cache, const int64_t* k
  * lse           [B,H,max_nodes] float out or NULL
  * Pointers 16-byte aligned (scales, ctx_len, n_nodes, node_depth, kv_off, anc_mask and lse as their types are).
  * Limits: dh % 8 == 0, dh <= CTCSPEC_MAX_HEAD_DIM, max_nodes <= CTCSPEC_MAX_NODES, B <= 64; B, H, dh, max_nodes within the context's
- * limits; H % H_kv == 0; kv_cap and max_nodes * H / H_kv <= 2^30; iterations over the keys (of 128, for a block of 32 or 64 rows) are
- * counted in 32 bits: 64 sequences x 128 nodes x 32 heads may have 3e7 cached rows, and a call that could need more is refused
+ * limits; H % H_kv == 0; kv_cap and max_nodes * H / H_kv <= 2^30; iterations over the keys (of 128, for a block of 32 rows) are
+ * counted in 32 bits: 64 sequences x 128 nodes x 32 heads may have 1.6e7 cached rows, and a call that could need more is refused
  * (CTCSPEC_EUNSUPPORTED).  The same bits on every run.
  */
 size_t q4_verify_attn_workspace_bytes(int B, int H, int H_kv, int dh, int max_nodes);

@@ -39,6 +39,8 @@ struct Q4AttnParams {
   float* po;                      // partial O: [slot][DT][4][64 lanes][4]
   float* pml;                     // [slot][2][32]: maximum in the log2 domain, sum
   int* odd;                       // [slot]: a value of a tree node is infinite or not a number
+  int* span;                      // [key head][B][blocks of rows][4]: the workgroups from the first to the last one with keys of a block, and
+  int blocks;                     // the block's number; blocks of max_nodes nodes
   int out_bf16;
   void* out;                      // [B][H][max_nodes][dh]
   float* lse;                     // [B][H][max_nodes] or null
@@ -59,7 +61,7 @@ struct Q4Shape {
   static __device__ __forceinline__ int place(int row) { return (row >> 2) * FOURB + (row & 3) * ROWB; }
   static constexpr int PART = (DT * 16 + 2) * 64 * 4;         // O, m, l of 32 rows
   static constexpr int STAGE = NW * TILE > 2 * PART ? NW * TILE : 2 * PART;
-  static constexpr int LDS = STAGE + 6 * 64 * 4;              // and the sequences' table
+  static constexpr int LDS = STAGE + 8 * 64 * 4;              // and the sequences' table
   static_assert(kQ4Waves * LDS <= 160 * 1024 && kQ4Groups % 8 == 0);
   // The blocks of values that a lane converts: row and block of the row of its k-th.  (Four blocks a row: two neighbours of a row; else
   // those 64 further.)
@@ -161,6 +163,7 @@ __global__ __launch_bounds__(64 * SH::NW, kQ4Waves) void q4_attn_kernel(Q4AttnPa
   constexpr int DT = SH::DT, KB = SH::KB, VB = SH::VB, QU = SH::QU;
   const int lane = threadIdx.x & 63;
   const int wave = uniform(threadIdx.x >> 6);
+  const long long my_off = lane < p.B ? p.kv_off[lane] : 0;
   const Q4Work t = q4_read_work<SH>(p);
   const Deal d = prefix_deal(t.units, kQ4Groups);
   // (consecutive shares - neighbouring keys - to the same of the 8 XCDs)
@@ -171,13 +174,15 @@ __global__ __launch_bounds__(64 * SH::NW, kQ4Waves) void q4_attn_kernel(Q4AttnPa
 
   // What the lanes know about the sequences, out of the registers while the keys go by; and a flag.
   int(*table)[64] = (int(*)[64])(smem + SH::STAGE);
-  enum { kNodes, kCtx, kIters, kUnit0, kBlock0, kOdd };
+  enum { kNodes, kCtx, kIters, kUnit0, kBlock0, kOffLow, kOffHigh, kOdd };
   if (wave == 0) {
     table[kNodes][lane] = t.n;
     table[kCtx][lane] = t.ctx;
     table[kIters][lane] = t.iters;
     table[kUnit0][lane] = t.unit0;
     table[kBlock0][lane] = t.block0;
+    table[kOffLow][lane] = (int)my_off;
+    table[kOffHigh][lane] = (int)(my_off >> 32);
   }
   __syncthreads();
   const int head_units = t.head_units, head_blocks = t.head_blocks;
@@ -214,10 +219,14 @@ __global__ __launch_bounds__(64 * SH::NW, kQ4Waves) void q4_attn_kernel(Q4AttnPa
     const int it0 = uniform(prefix_iterations(at_unit, kPrefixOwnWeight, false));
     const int niter = uniform(prefix_iterations(at_unit + share, kPrefixOwnWeight, false)) - it0;
     if (niter <= 0) continue;
+    if (threadIdx.x == 0) {  // (the join need not deal the work once more)
+      int* span = p.span + (((size_t)kh * p.B + b) * p.blocks + blk) * 4;
+      if (it0 == 0) *(u32x2*)span = u32x2{(unsigned)(slot - w), (unsigned)w};
+      if (q4_units(it0 + niter) == units) span[2] = w;
+    }
     const Q4Tiles tiles = q4_tiles(L, p.window, p.sink);
     const int total = tiles.count + (n + 31) / 32;
-    const unsigned long long off = (unsigned long long)p.kv_off[b];
-    const size_t row0 = ((size_t)(unsigned)uniform((int)(off >> 32)) << 32 | (unsigned)uniform((int)off)) + (size_t)kh * p.kv_cap;
+    const size_t row0 = ((size_t)(unsigned)uniform(table[kOffHigh][b]) << 32 | (unsigned)uniform(table[kOffLow][b])) + (size_t)kh * p.kv_cap;
     // codes and scales of cached tile x of the segment: of key c blocks KB h2 .., of the values blocks lane, lane + 64.  (Rows behind the last
     // one, and blocks behind a row's last, lie outside what the descriptors hold: zeros.)
     u32x4 kraw[KB], vraw[VB];
@@ -517,91 +526,83 @@ __global__ __launch_bounds__(64 * SH::NW, kQ4Waves) void q4_attn_kernel(Q4AttnPa
 }
 
 // ---- the join ------------------------------------------------------------------------------------------------------------
-// One workgroup of DT wavefronts per (32 rows of a sequence, key head): every wavefront weighs the rows' partial results and adds up 32
-// components of them, in the order of their keys, four at a time under way.
+// One workgroup of DT wavefronts per (32 rows of a sequence, 8 of every 32 components, key head): every wavefront weighs the rows' partial
+// results and adds up its components of them, four in a lane.  Where there are 16 rows or fewer, lanes share a row: `shares` of them take
+// every shares-th partial result, and what they have is added up in an order that the number of shares gives.
 template <typename SH>
 __global__ __launch_bounds__(64 * SH::DT) void q4_join_kernel(Q4AttnParams p) {
   constexpr int DT = SH::DT;
-  const int lane = threadIdx.x & 63, dt = threadIdx.x >> 6, c = lane & 31, h2 = lane >> 5;
-  const int kh = blockIdx.y, b = blockIdx.z, r = blockIdx.x * 32 + c;
-  const Q4Work t = q4_read_work<SH>(p);
-  const int n = __builtin_amdgcn_readlane(t.n, b), L = __builtin_amdgcn_readlane(t.ctx, b);
-  if ((int)blockIdx.x * 32 >= n * p.group) return;
-  const Deal d = prefix_deal(t.units, kQ4Groups);
-  const int iters = __builtin_amdgcn_readlane(t.iters, b), blk = blockIdx.x;
-  const int first = kh * t.head_units + __builtin_amdgcn_readlane(t.unit0, b) + blk * q4_units(iters) + prefix_block_units(false);
-  const int item = kh * t.head_blocks + __builtin_amdgcn_readlane(t.block0, b) + blk;
-  const int w0 = d.owner(first), w1 = d.owner(first + (iters - 1) * kPrefixOwnWeight);
-  if (r >= n * p.group) return;
+  const int lane = threadIdx.x & 63, dt = threadIdx.x >> 6, h2 = lane >> 5;
+  const int kh = blockIdx.y, b = blockIdx.z, blk = blockIdx.x >> 2, part = blockIdx.x & 3;
+  const int* span = p.span + (((size_t)kh * p.B + b) * p.blocks + blk) * 4;
+  const int item = span[0], w0 = span[1], w1 = span[2];  // (of a block without rows whatever was there)
+  const int n = p.n_nodes[b] < p.max_nodes ? p.n_nodes[b] : p.max_nodes, rows = n * p.group - blk * 32;
+  if (rows <= 0) return;
+  int shares = 1;
+  while (shares < 32 && shares <= w1 - w0 && 32 / (2 * shares) >= rows) shares *= 2;
+  const int of = 32 / shares, c = lane & (of - 1), share = (lane & 31) / of, r = blk * 32 + c;
   float m = -INFINITY, l = 0.f;
-  f32x4 o[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
   const float* ml = p.pml + (size_t)item * (2 * kQ4Rows) + c;
-  const float* po = p.po + (size_t)item * (DT * 1024) + dt * 1024 + lane * 4;
+  const float* po = p.po + (size_t)item * (DT * 1024) + (dt * 4 + part) * 256 + (h2 * 32 + c) * 4;
+  auto add = [&](float pm, float pl, f32x4 x) __attribute__((always_inline)) {
+    const float top = fmaxf(m, pm), base = top > -INFINITY ? top : 0.f;
+    const float old = __builtin_amdgcn_exp2f(m - base), a = __builtin_amdgcn_exp2f(pm - base);
+    l = l * old + a * pl;
+    o = o * old + a * x;
+    m = top;
+  };
   constexpr int kBatch = 4;
   int odd = 0;
-  for (int w = w0; w <= w1; w += kBatch) {
+  for (int w = w0 + share; w <= w1; w += kBatch * shares) {
     float pm[kBatch], pl[kBatch];
-    f32x4 x[kBatch][4];
+    f32x4 x[kBatch];
 #pragma unroll
     for (int q = 0; q < kBatch; ++q) {  // (behind the last one: the last one again, with no weight)
-      const size_t s = w + q < w1 ? w + q : w1;
+      const int at = w + q * shares;
+      const size_t s = at <= w1 ? at : w1;
       pm[q] = ml[s * (2 * kQ4Rows)];
       pl[q] = ml[s * (2 * kQ4Rows) + kQ4Rows];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) x[q][i] = *(const f32x4*)(po + s * (DT * 1024) + i * 256);
+      x[q] = *(const f32x4*)(po + s * (DT * 1024));
       odd |= p.odd[s + item];
     }
-    float top = m;
 #pragma unroll
-    for (int q = 0; q < kBatch; ++q) top = fmaxf(top, pm[q]);
-    const float base = top > -INFINITY ? top : 0.f, old = __builtin_amdgcn_exp2f(m - base);
-    l *= old;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) o[i] *= old;
-#pragma unroll
-    for (int q = 0; q < kBatch; ++q) {
-      if (w + q > w1) continue;
-      const float a = __builtin_amdgcn_exp2f(pm[q] - base);
-      l += a * pl[q];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) o[i] += a * x[q][i];
-    }
-    m = top;
+    for (int q = 0; q < kBatch; ++q)
+      if (w + q * shares <= w1) add(pm[q], pl[q], x[q]);
   }
-  const int node = r / p.group, hg = r - node * p.group;
+  for (int d = of; d < 32; d *= 2) {
+    const float pm = __shfl_xor(m, d, 64), pl = __shfl_xor(l, d, 64);
+    const f32x4 x = {__shfl_xor(o[0], d, 64), __shfl_xor(o[1], d, 64), __shfl_xor(o[2], d, 64), __shfl_xor(o[3], d, 64)};
+    add(pm, pl, x);
+    odd |= __shfl_xor(odd, d, 64);
+  }
+  if (c >= rows || share) return;
+  const int node = r / p.group, hg = r - node * p.group, at = 32 * dt + 8 * part + 4 * h2;
   if (odd) {  // values of tree nodes that are infinite or not a number, left out so far: into the rows that see them
+    const int len = p.ctx_len[b], L = len < 0 ? 0 : (len > p.kv_cap ? p.kv_cap : len);
     const Q4Mask mask = q4_tree_mask(p, b, node, n, L, p.window > 0 ? q4_depth(p, b, node) : 0);
     const unsigned short* vt = (const unsigned short*)p.v_tree + ((size_t)b * p.H_kv + kh) * p.max_nodes * p.dh;
     for (int j = 0; j < n; ++j) {
       if (!mask.node(j)) continue;
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int at = 32 * dt + 8 * i + 4 * h2 + e;
-          if (at >= p.dh) continue;
-          const float v = bf16_bits_to_float(vt[(size_t)j * p.dh + at]);
-          if ((__float_as_uint(v) & 0x7f800000u) == 0x7f800000u) o[i][e] += v;
-        }
+      for (int e = 0; e < 4; ++e) {
+        if (at + e >= p.dh) continue;
+        const float v = bf16_bits_to_float(vt[(size_t)j * p.dh + at + e]);
+        if ((__float_as_uint(v) & 0x7f800000u) == 0x7f800000u) o[e] += v;
+      }
     }
   }
   const size_t row = ((size_t)b * p.H + kh * p.group + hg) * p.max_nodes + node;
   const bool none = m == -INFINITY && l == 0.f;  // no key at all
   const float inv = none ? 0.f : 1.0f / l;
-  if (p.lse && dt == 0 && h2 == 0) p.lse[row] = none ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int at = 32 * dt + 8 * i + 4 * h2;
-    if (at >= p.dh) continue;
-    const f32x4 v = none ? f32x4{0.f, 0.f, 0.f, 0.f} : o[i] * inv;
-    if (p.out_bf16) {
-      *(u32x2*)((unsigned short*)p.out + row * p.dh + at) = u32x2{__builtin_bit_cast(unsigned int, bf16x2{(__bf16)v[0], (__bf16)v[1]}),
-                                                                  __builtin_bit_cast(unsigned int, bf16x2{(__bf16)v[2], (__bf16)v[3]})};
-    } else {
-      *(f32x4*)((float*)p.out + row * p.dh + at) = v;
-    }
+  if (p.lse && dt == 0 && part == 0 && h2 == 0) p.lse[row] = none ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+  if (at >= p.dh) return;
+  const f32x4 v = none ? f32x4{0.f, 0.f, 0.f, 0.f} : o * inv;
+  if (p.out_bf16) {
+    *(u32x2*)((unsigned short*)p.out + row * p.dh + at) = u32x2{__builtin_bit_cast(unsigned int, bf16x2{(__bf16)v[0], (__bf16)v[1]}),
+                                                                __builtin_bit_cast(unsigned int, bf16x2{(__bf16)v[2], (__bf16)v[3]})};
+  } else {
+    *(f32x4*)((float*)p.out + row * p.dh + at) = v;
   }
 }
 
@@ -685,14 +686,15 @@ extern "C" int q4_verify_attn(ctcspec_ctx* ctx, ctcspec_dtype dt, const void* q,
   p.window = window < (1 << 30) + 256 ? window : (1 << 30) + 256;
   p.sink = sink < (1 << 30) + 256 ? sink : (1 << 30) + 256;
   p.sl2 = scale * 1.4426950408889634f;
-  p.po = (float*)(base + ws.o); p.pml = (float*)(base + ws.ml); p.odd = (int*)(base + ws.odd);
+  p.po = (float*)(base + ws.o); p.pml = (float*)(base + ws.ml); p.odd = (int*)(base + ws.odd); p.span = (int*)(base + ws.span);
+  p.blocks = (int)((seq_rows + kQ4Rows - 1) / kQ4Rows);
   p.out_bf16 = out_dt == CTCSPEC_BF16; p.out = out; p.lse = lse;
   hipStream_t st = ctx->stream;
   const hipError_t e = q4_with_shape(q4_blocks(dh), out_dt == CTCSPEC_F32, [&](auto shape) {
     using SH = decltype(shape);
     hipLaunchKernelGGL(q4_attn_kernel<SH>, dim3(kQ4Groups), dim3(64 * SH::NW), SH::LDS, st, p);
     if (const hipError_t e1 = hipGetLastError(); e1 != hipSuccess) return e1;
-    hipLaunchKernelGGL(q4_join_kernel<SH>, dim3((unsigned)((seq_rows + 31) / 32), (unsigned)H_kv, (unsigned)B), dim3(64 * SH::DT), 0, st, p);
+    hipLaunchKernelGGL(q4_join_kernel<SH>, dim3((unsigned)(p.blocks * 4), (unsigned)H_kv, (unsigned)B), dim3(64 * SH::DT), 0, st, p);
     return hipGetLastError();
   });
   CTCSPEC_HIP(ctx, e);

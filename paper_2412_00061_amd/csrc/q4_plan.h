@@ -44,7 +44,7 @@ inline bool q4_units_fit(long long B, int H_kv, long long seq_rows, int kv_cap, 
 }
 
 struct Q4Workspace {
-  size_t o, ml, odd, total;
+  size_t o, ml, odd, span, total;
 };
 // Numbers of partial results: below workgroups + blocks.
 inline Q4Workspace q4_workspace(int B, int H, int H_kv, int dh, int max_nodes) {
@@ -57,6 +57,7 @@ inline Q4Workspace q4_workspace(int B, int H, int H_kv, int dh, int max_nodes) {
   w.o = carve(slots * kQ4Rows * tiles * 32 * sizeof(float));
   w.ml = carve(slots * kQ4Rows * 2 * sizeof(float));
   w.odd = carve(slots * sizeof(int));
+  w.span = carve((slots - kQ4Groups) * 4 * sizeof(int));
   w.total = off;
   return w;
 }

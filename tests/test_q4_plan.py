@@ -53,13 +53,17 @@ def test_a_window_keeps_every_tile_that_a_row_sees():
 
 
 def test_units_are_counted_for_the_largest_lengths():
+    # 64 x 32 x 4 blocks of 32 rows, 8 units each and 2 for every iteration of 4 tiles: 2^31 > 8192 (8 + 2 x) allows x = 131067, 524268 tiles, of
+    # which the tree has 4
+    last = (524268 - 4) * 32
     fits = ask([("f", 64, 32, 128, 30_000_000, 128), ("f", 64, 32, 128, 40_000_000, 128), ("f", 1, 1, 1, 1 << 30, 1), ("f", 1, 1, 1, (1 << 30) + 1, 1),
-                ("f", 1, 1, (1 << 30) + 1, 8, 128)])
-    assert [f[0] for f in fits] == [1, 0, 1, 0, 0]
+                ("f", 1, 1, (1 << 30) + 1, 8, 128), ("f", 64, 32, 128, last, 128), ("f", 64, 32, 128, last + 1, 128)])
+    assert [f[0] for f in fits] == [0, 0, 1, 0, 0, 1, 0]
 
 
 def test_workspace_has_room_for_every_partial_result():
     for B, H, Hkv, dh, N in ((1, 1, 1, 8, 1), (8, 32, 32, 128, 64), (64, 40, 8, 96, 128), (3, 32, 1, 64, 1)):
         (groups, o, total), = ask([("w", B, H, Hkv, dh, N)])
-        slots = groups + Hkv * B * -(-(N * H // Hkv) // 32)  # a part for each workgroup, and one more where a block of rows ends in its share
-        assert o == 0 and total >= slots * (32 * (-(-dh // 32) * 32 + 2) + 1) * 4
+        blocks = Hkv * B * -(-(N * H // Hkv) // 32)
+        slots = groups + blocks  # a part for each workgroup, and one more where a block of rows ends in its share
+        assert o == 0 and total >= slots * (32 * (-(-dh // 32) * 32 + 2) + 1) * 4 + blocks * 16
