@@ -430,36 +430,60 @@ __global__ __launch_bounds__(64 * SH::NW, kQ4Waves) void q4_attn_kernel(Q4AttnPa
       const size_t tree0 = ((size_t)b * p.H_kv + kh) * p.max_nodes * (size_t)(p.dh * 2);
       const auto kt = buffer(p.k_tree + tree0, n * p.dh * 2), vt = buffer(p.v_tree + tree0, n * p.dh * 2);
       constexpr int kOutside = 0x1000000;
+      // (everything fetched ahead of its use, as far as the registers hold it: keys and mask, and half of the values for half of the keys)
+      u32x4 kf[QU], vf[DT];
+      unsigned int strange = 0u;
+      auto fetch_values = [&](int half) __attribute__((always_inline)) {  // of 128 DT chunks of 8 components
+        int own = lane;
+        asm volatile("" : "+v"(own));
+#pragma unroll
+        for (int i = 0; i < DT; ++i) {
+          const int y = own + 64 * (half * DT + i), row = y / (4 * DT), ch = y % (4 * DT);
+          vf[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(vt, 8 * ch < p.dh ? ((32 * tile + row) * p.dh + 8 * ch) * 2 : kOutside, 0, 0));
+        }
+      };
+      // values that are infinite or no numbers: left out, and added by the join to the rows that see them
+      auto take_values = [&](int half) __attribute__((always_inline)) {
+        int own = lane;
+        asm volatile("" : "+v"(own));
+#pragma unroll
+        for (int i = 0; i < DT; ++i) {
+          const int y = own + 64 * (half * DT + i), row = y / (4 * DT), ch = y % (4 * DT);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {  // (exponents of nothing but ones carry into the sign's place)
+            const unsigned int bad = (((vf[i][e] & 0x7f807f80u) + 0x00800080u) & 0x80008000u) >> 15;
+            strange |= bad;
+            vf[i][e] &= ~(bad * 0xffffu);
+          }
+          *(__attribute__((address_space(3))) u32x4*)(vbase + SH::place(row) + ch * 16) = vf[i];
+        }
+        asm volatile("" : : : "memory");
+      };
+#pragma unroll
+      for (int i = 0; i < QU; ++i) {
+        const int at = 32 * (KB * h2 + i / 4) + 8 * (i % 4);
+        kf[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(kt, at < p.dh ? ((32 * tile + c) * p.dh + at) * 2 : kOutside, 0, 0));
+      }
       f32x16 s;
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[i] = 0.f;
 #pragma unroll
       for (int i = 0; i < QU; ++i) {
-        const int at = 32 * (KB * h2 + i / 4) + 8 * (i % 4);
-        const u32x4 a = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(kt, at < p.dh ? ((32 * tile + c) * p.dh + at) * 2 : kOutside, 0, 0));
-        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, qf[i]), s, 0, 0, 0);
-        if (i % 4 == 3) asm volatile("" : "+v"(s) : : "memory");
-      }
-      // values that are infinite or no numbers: left out, and added by the join to the rows that see them
-      unsigned int strange = 0u;
-#pragma unroll
-      for (int i = 0; i < 2 * DT; ++i) {  // 128 DT chunks of 8 components
-        const int y = fresh + 64 * i, row = y / (4 * DT), ch = y % (4 * DT);
-        u32x4 v = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(vt, 8 * ch < p.dh ? ((32 * tile + row) * p.dh + 8 * ch) * 2 : kOutside, 0, 0));
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {  // (exponents of nothing but ones carry into the sign's place)
-          const unsigned int bad = (((v[e] & 0x7f807f80u) + 0x00800080u) & 0x80008000u) >> 15;
-          strange |= bad;
-          v[e] &= ~(bad * 0xffffu);
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[i]), __builtin_bit_cast(bf16x8, qf[i]), s, 0, 0, 0);
+        if (i % 4 == 3) {
+          asm volatile("" : "+v"(s) : : "memory");
+          if (i == 3) fetch_values(0);
         }
-        *(__attribute__((address_space(3))) u32x4*)(vbase + SH::place(row) + ch * 16) = v;
-        if (i % 4 == 3) asm volatile("" : : : "memory");
       }
-      odd = __builtin_amdgcn_ballot_w64(strange != 0u) != 0ull;
-      int heads = p.group, row = blk * kQ4Rows + c;
+      int heads = p.group, node = blk * kQ4Rows + c;
       asm volatile("" : "+s"(heads));
-      row = row < n * heads ? row / heads : 0;
-      hide(s, q4_tree_mask(p, b, row, n, L, p.window > 0 ? q4_depth(p, b, row) : 0).tile(tile));
+      node = node < n * heads ? node / heads : 0;
+      const unsigned int vis = q4_tree_mask(p, b, node, n, L, p.window > 0 ? q4_depth(p, b, node) : 0).tile(tile);
+      take_values(0);
+      fetch_values(1);
+      take_values(1);
+      odd = __builtin_amdgcn_ballot_w64(strange != 0u) != 0ull;
+      hide(s, vis);
       weigh(s);
     }
 
@@ -526,14 +550,18 @@ __global__ __launch_bounds__(64 * SH::NW, kQ4Waves) void q4_attn_kernel(Q4AttnPa
 }
 
 // ---- the join ------------------------------------------------------------------------------------------------------------
-// One workgroup of DT wavefronts per (32 rows of a sequence, 8 of every 32 components, key head): every wavefront weighs the rows' partial
-// results and adds up its components of them, four in a lane.  Where there are 16 rows or fewer, lanes share a row: `shares` of them take
-// every shares-th partial result, and what they have is added up in an order that the number of shares gives.
-template <typename SH>
+// Workgroups of DT wavefronts, PARTS of them per (32 rows of a sequence, key head): every wavefront weighs the rows' partial results and adds
+// up its components of them, 32 / PARTS.  Where there are 16 rows or fewer, lanes share a row: `shares` of them take every shares-th partial
+// result, and what they have is added up in an order that the number of shares gives.  (4 single tokens with 8 key heads, 32 blocks of up
+// to 39 partial results, us: 10.4 with neither, 6.8 with lanes that share, 5.2 with 4 parts as well.)
+//
+// Up to kQ4JoinFew blocks have 4 parts.  (us with 4 / 1: 32 blocks 5.2 / 6.8, 256 5.2 / 5.2 and 8.5 / 5.9, 416 5.9 / 5.1, 512 9.7 / 7.0.)
+constexpr int kQ4JoinFew = 128;
+template <typename SH, int PARTS>
 __global__ __launch_bounds__(64 * SH::DT) void q4_join_kernel(Q4AttnParams p) {
-  constexpr int DT = SH::DT;
+  constexpr int DT = SH::DT, OWN = 4 / PARTS;
   const int lane = threadIdx.x & 63, dt = threadIdx.x >> 6, h2 = lane >> 5;
-  const int kh = blockIdx.y, b = blockIdx.z, blk = blockIdx.x >> 2, part = blockIdx.x & 3;
+  const int kh = blockIdx.y, b = blockIdx.z, blk = blockIdx.x / PARTS, part = blockIdx.x % PARTS * OWN;
   const int* span = p.span + (((size_t)kh * p.B + b) * p.blocks + blk) * 4;
   const int item = span[0], w0 = span[1], w1 = span[2];  // (of a block without rows whatever was there)
   const int n = p.n_nodes[b] < p.max_nodes ? p.n_nodes[b] : p.max_nodes, rows = n * p.group - blk * 32;
@@ -542,28 +570,32 @@ __global__ __launch_bounds__(64 * SH::DT) void q4_join_kernel(Q4AttnParams p) {
   while (shares < 32 && shares <= w1 - w0 && 32 / (2 * shares) >= rows) shares *= 2;
   const int of = 32 / shares, c = lane & (of - 1), share = (lane & 31) / of, r = blk * 32 + c;
   float m = -INFINITY, l = 0.f;
-  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  f32x4 o[OWN];
+#pragma unroll
+  for (int i = 0; i < OWN; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
   const float* ml = p.pml + (size_t)item * (2 * kQ4Rows) + c;
   const float* po = p.po + (size_t)item * (DT * 1024) + (dt * 4 + part) * 256 + (h2 * 32 + c) * 4;
-  auto add = [&](float pm, float pl, f32x4 x) __attribute__((always_inline)) {
+  auto add = [&](float pm, float pl, const f32x4 (&x)[OWN]) __attribute__((always_inline)) {
     const float top = fmaxf(m, pm), base = top > -INFINITY ? top : 0.f;
     const float old = __builtin_amdgcn_exp2f(m - base), a = __builtin_amdgcn_exp2f(pm - base);
     l = l * old + a * pl;
-    o = o * old + a * x;
+#pragma unroll
+    for (int i = 0; i < OWN; ++i) o[i] = o[i] * old + a * x[i];
     m = top;
   };
   constexpr int kBatch = 4;
   int odd = 0;
   for (int w = w0 + share; w <= w1; w += kBatch * shares) {
     float pm[kBatch], pl[kBatch];
-    f32x4 x[kBatch];
+    f32x4 x[kBatch][OWN];
 #pragma unroll
     for (int q = 0; q < kBatch; ++q) {  // (behind the last one: the last one again, with no weight)
       const int at = w + q * shares;
       const size_t s = at <= w1 ? at : w1;
       pm[q] = ml[s * (2 * kQ4Rows)];
       pl[q] = ml[s * (2 * kQ4Rows) + kQ4Rows];
-      x[q] = *(const f32x4*)(po + s * (DT * 1024));
+#pragma unroll
+      for (int i = 0; i < OWN; ++i) x[q][i] = *(const f32x4*)(po + s * (DT * 1024) + i * 256);
       odd |= p.odd[s + item];
     }
 #pragma unroll
@@ -572,12 +604,14 @@ __global__ __launch_bounds__(64 * SH::DT) void q4_join_kernel(Q4AttnParams p) {
   }
   for (int d = of; d < 32; d *= 2) {
     const float pm = __shfl_xor(m, d, 64), pl = __shfl_xor(l, d, 64);
-    const f32x4 x = {__shfl_xor(o[0], d, 64), __shfl_xor(o[1], d, 64), __shfl_xor(o[2], d, 64), __shfl_xor(o[3], d, 64)};
+    f32x4 x[OWN];
+#pragma unroll
+    for (int i = 0; i < OWN; ++i) x[i] = f32x4{__shfl_xor(o[i][0], d, 64), __shfl_xor(o[i][1], d, 64), __shfl_xor(o[i][2], d, 64), __shfl_xor(o[i][3], d, 64)};
     add(pm, pl, x);
     odd |= __shfl_xor(odd, d, 64);
   }
   if (c >= rows || share) return;
-  const int node = r / p.group, hg = r - node * p.group, at = 32 * dt + 8 * part + 4 * h2;
+  const int node = r / p.group, hg = r - node * p.group;
   if (odd) {  // values of tree nodes that are infinite or not a number, left out so far: into the rows that see them
     const int len = p.ctx_len[b], L = len < 0 ? 0 : (len > p.kv_cap ? p.kv_cap : len);
     const Q4Mask mask = q4_tree_mask(p, b, node, n, L, p.window > 0 ? q4_depth(p, b, node) : 0);
@@ -585,24 +619,31 @@ __global__ __launch_bounds__(64 * SH::DT) void q4_join_kernel(Q4AttnParams p) {
     for (int j = 0; j < n; ++j) {
       if (!mask.node(j)) continue;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        if (at + e >= p.dh) continue;
-        const float v = bf16_bits_to_float(vt[(size_t)j * p.dh + at + e]);
-        if ((__float_as_uint(v) & 0x7f800000u) == 0x7f800000u) o[e] += v;
-      }
+      for (int i = 0; i < OWN; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int at = 32 * dt + 8 * (part + i) + 4 * h2 + e;
+          if (at >= p.dh) continue;
+          const float v = bf16_bits_to_float(vt[(size_t)j * p.dh + at]);
+          if ((__float_as_uint(v) & 0x7f800000u) == 0x7f800000u) o[i][e] += v;
+        }
     }
   }
   const size_t row = ((size_t)b * p.H + kh * p.group + hg) * p.max_nodes + node;
   const bool none = m == -INFINITY && l == 0.f;  // no key at all
   const float inv = none ? 0.f : 1.0f / l;
   if (p.lse && dt == 0 && part == 0 && h2 == 0) p.lse[row] = none ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
-  if (at >= p.dh) return;
-  const f32x4 v = none ? f32x4{0.f, 0.f, 0.f, 0.f} : o * inv;
-  if (p.out_bf16) {
-    *(u32x2*)((unsigned short*)p.out + row * p.dh + at) = u32x2{__builtin_bit_cast(unsigned int, bf16x2{(__bf16)v[0], (__bf16)v[1]}),
-                                                                __builtin_bit_cast(unsigned int, bf16x2{(__bf16)v[2], (__bf16)v[3]})};
-  } else {
-    *(f32x4*)((float*)p.out + row * p.dh + at) = v;
+#pragma unroll
+  for (int i = 0; i < OWN; ++i) {
+    const int at = 32 * dt + 8 * (part + i) + 4 * h2;
+    if (at >= p.dh) continue;
+    const f32x4 v = none ? f32x4{0.f, 0.f, 0.f, 0.f} : o[i] * inv;
+    if (p.out_bf16) {
+      *(u32x2*)((unsigned short*)p.out + row * p.dh + at) = u32x2{__builtin_bit_cast(unsigned int, bf16x2{(__bf16)v[0], (__bf16)v[1]}),
+                                                                  __builtin_bit_cast(unsigned int, bf16x2{(__bf16)v[2], (__bf16)v[3]})};
+    } else {
+      *(f32x4*)((float*)p.out + row * p.dh + at) = v;
+    }
   }
 }
 
@@ -694,7 +735,10 @@ extern "C" int q4_verify_attn(ctcspec_ctx* ctx, ctcspec_dtype dt, const void* q,
     using SH = decltype(shape);
     hipLaunchKernelGGL(q4_attn_kernel<SH>, dim3(kQ4Groups), dim3(64 * SH::NW), SH::LDS, st, p);
     if (const hipError_t e1 = hipGetLastError(); e1 != hipSuccess) return e1;
-    hipLaunchKernelGGL(q4_join_kernel<SH>, dim3((unsigned)(p.blocks * 4), (unsigned)H_kv, (unsigned)B), dim3(64 * SH::DT), 0, st, p);
+    if ((long long)p.blocks * H_kv * B <= kQ4JoinFew)
+      hipLaunchKernelGGL((q4_join_kernel<SH, 4>), dim3((unsigned)(p.blocks * 4), (unsigned)H_kv, (unsigned)B), dim3(64 * SH::DT), 0, st, p);
+    else
+      hipLaunchKernelGGL((q4_join_kernel<SH, 1>), dim3((unsigned)p.blocks, (unsigned)H_kv, (unsigned)B), dim3(64 * SH::DT), 0, st, p);
     return hipGetLastError();
   });
   CTCSPEC_HIP(ctx, e);
