@@ -2,6 +2,9 @@
 step q4_verify_attn per layer, verify_head_argmax, verify_sample_filtered, accept_longest and kv_commit_q4 per layer - one after the other,
 in a captured graph, and on two streams at once."""
 import contextlib
+import os
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -237,6 +240,13 @@ def test_the_steps_on_two_streams_at_once(eager):
     assert same(alone.state(), runs[1][0].state())
     for run in (alone, *(r for r, _ in runs)):
         run.ctx.close()
+
+
+@pytest.mark.gpu
+def test_the_first_calls_of_a_process_captured():
+    program = os.path.join(os.path.dirname(os.path.abspath(__file__)), "capture_first_q4.py")
+    r = subprocess.run([sys.executable, program], capture_output=True, text=True, timeout=100)
+    assert r.returncode == 0 and "capture-first ok" in r.stdout, r.stdout + r.stderr
 
 
 def test_scratch_comes_from_the_stream_of_the_context(monkeypatch):
