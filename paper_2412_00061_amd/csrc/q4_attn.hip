@@ -113,7 +113,6 @@ __device__ __forceinline__ int q4_depth(const Q4AttnParams& p, int b, int node) 
 }
 struct Q4Mask {
   unsigned long long low, high;  // nodes 0 to 63, 64 to 127
-  __device__ __forceinline__ unsigned int tile(int i) const { return (unsigned int)((i < 2 ? low : high) >> (32 * (i & 1))); }
   __device__ __forceinline__ bool node(int j) const { return ((j < 64 ? low : high) >> (j & 63)) & 1ull; }
 };
 __device__ __forceinline__ Q4Mask q4_tree_mask(const Q4AttnParams& p, int b, int node, int n, int L, int depth) {
@@ -478,7 +477,17 @@ __global__ __launch_bounds__(64 * SH::NW, kQ4Waves) void q4_attn_kernel(Q4AttnPa
       int heads = p.group, node = blk * kQ4Rows + c;
       asm volatile("" : "+s"(heads));
       node = node < n * heads ? node / heads : 0;
-      const unsigned int vis = q4_tree_mask(p, b, node, n, L, p.window > 0 ? q4_depth(p, b, node) : 0).tile(tile);
+      // which nodes of the tile the row sees, as q4_tree_mask has it
+      const int nodes = n - 32 * tile;  // (at least one)
+      unsigned int vis = (unsigned int)(p.anc_mask[((size_t)b * p.max_nodes + node) * ((p.max_nodes + 63) >> 6) + (tile >> 1)] >> (32 * (tile & 1)));
+      vis &= nodes >= 32 ? 0xffffffffu : (1u << nodes) - 1u;
+      if (p.window > 0 && p.window < p.max_nodes) {  // (lane j has node j's depth: fetched one after the other they would take 0.2 us each)
+        const int depth = q4_depth(p, b, node), theirs = q4_depth(p, b, 32 * tile + (c < nodes ? c : 0));
+        for (int j = 0; j < 32; ++j) {
+          const int dj = __builtin_amdgcn_readlane(theirs, j);
+          vis &= depth - dj >= p.window && L + dj >= p.sink ? ~(1u << j) : 0xffffffffu;
+        }
+      }
       take_values(0);
       fetch_values(1);
       take_values(1);

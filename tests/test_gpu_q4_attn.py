@@ -168,6 +168,25 @@ def test_windows(shape, window, sink):
     ctx.close()
 
 
+@pytest.mark.parametrize("window,sink", [(1, 0), (2, 0), (3, 66), (5, 70), (9, 0)])
+def test_windows_shorter_than_a_path(window, sink):
+    """Trees of 128 nodes, paths up to dozens deep: nodes outside the window in every tile of the tree, sinks that end among them."""
+    import torch
+    c = make(window + sink, 3, 4, 2, 128, 64, [0, 65, 61], [128, 97, 66], window=window, sink=sink)
+    for b in range(3):  # one long path, and what hangs on it
+        for i in range(1, c["n"][b]):
+            parent = i - 1 if i % 3 else max(0, i - 4)
+            c["seen"][b, i], c["depth"][b, i] = c["seen"][b, parent], c["depth"][b, parent] + 1
+            c["seen"][b, i, i] = True
+    assert c["depth"].max() > 40
+    ctx = context(c)
+    for dtype in (torch.float32, torch.bfloat16):
+        check(c, call(ctx, c, upload(c), dtype))
+    c["vt"][0, 0, 3, 7], c["vt"][1, 1, 60, 9], c["vt"][2, 0, 65, 40] = np.inf, np.nan, -np.inf
+    check(c, call(ctx, c, upload(c), torch.float32))
+    ctx.close()
+
+
 def test_a_window_that_holds_everything_is_none():
     import torch
     c = make(3, *SHAPES[8])
