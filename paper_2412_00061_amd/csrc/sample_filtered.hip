@@ -105,6 +105,9 @@ __device__ __forceinline__ u64 whole(double w) {
   return (u64)__double_as_longlong(__builtin_fma(w, 35184372088832.0, 4503599627370496.0)) - 0x4330000000000000ull;
 }
 
+// a sum of weights
+__device__ __forceinline__ u64 whole_sum(double w) { return (u64)(w * 35184372088832.0); }
+
 // What the temperature and the filters of a sequence ask for.
 struct Filters {
   int top_k;
@@ -436,7 +439,7 @@ struct ListShared {
   float largest[kFilterWaves], lowest[kFilterWaves];
   unsigned int part_sum[kFilterWaves], count_sum[kFilterWaves], kept[kFilterWaves];
   u64 ahead_weight, threshold, mass;
-  unsigned int candidates, ahead, found, members;
+  unsigned int candidates, ahead, found, members, certain;
 };
 
 __device__ __forceinline__ double dpp_f64(double v, int which) {
@@ -481,6 +484,11 @@ __device__ __forceinline__ void sums_before(u64 own, u64& before, u64& all, u64*
   all = readlane_u64(of_waves, 15);
   before = incl - own + (wave > 0 ? readlane_u64(of_waves, wave > 0 ? wave - 1 : 0) : 0ull);
 }
+
+// Top-p's share of all tokens is first taken of a sum in float: exponents whole in 64 bits, their fractions off by 2^-25, the exponential by
+// 2^-23, sums of four by 2^-23, then 64 bits again; together below 2.7e-7 of the sum, 2^-21 = 4.8e-7.  Where the tokens that top-p keeps are
+// not the same for both ends of that, the sum is formed in 64 bits.
+constexpr double kFilterRough = 4.76837158203125e-07;
 
 // The tokens that may be kept are few, mostly, and a bound below them all is easily had: among the first top_k tokens' logits is none below
 // the top_k-th of any top_k and more logits - such as the largest logits of the threads' parts of the row -, min-p is a distance from the
@@ -748,13 +756,16 @@ __device__ __forceinline__ bool sample_listed(const FilterParams& p, ListShared&
   }
   bound = fmaxf(bound, distance);
   u64 mass = 0ull;
+  double rough = 0.0;
   list(bound, INFINITY, [&](const f32x4& v) __attribute__((always_inline)) {
     if (of_all) {
+      float w[4];
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
-        const u64 y = whole(weight(v[c]));
-        mass += v[c] > -INFINITY ? y : 0ull;
+        const double x = fmax(((double)v[c] - weight.mx) * weight.per, -1000.0), n = __builtin_rint(x);  // (what is no number: a weight of 0)
+        w[c] = __builtin_amdgcn_ldexpf(__builtin_amdgcn_exp2f((float)(x - n)), (int)n);
       }
+      rough += (double)((w[0] + w[1]) + (w[2] + w[3]));
     }
   }, std::false_type{});
   unsigned int listed = sh.candidates;
@@ -767,8 +778,8 @@ __device__ __forceinline__ bool sample_listed(const FilterParams& p, ListShared&
   };
   if (of_all) {
     // as many candidates as it takes to weigh enough: a quarter of the parts, three quarters, nearly all
-    mass = block_sum(mass);
-    const double enough = (double)want.top_p * (double)mass;
+    mass = block_sum(whole_sum(rough));
+    const double enough = (double)want.top_p * (double)mass * (1.0 + kFilterRough);
     u64 weighs = 0ull;
     unsigned int weighed = 0u;
     for (int round = 1;; ++round) {
@@ -855,24 +866,45 @@ __device__ __forceinline__ bool sample_listed(const FilterParams& p, ListShared&
     }
     if (want.by_p) {
       if (want.by_k) mass = all_weight;
-      const double need = fmax((double)want.top_p * (double)mass, 0.5);  // the weight before a token that is kept is below this
-      if ((double)all_weight >= need) {
-        // (in the bin where top-k ends its last tokens bring the weights there, if none before did)
-        const bool here = (double)before_weight < need && (tid < (int)last_bin ? (double)(before_weight + own_weight) >= need : tid == (int)last_bin);
-        if (here) {
-          sh.found = tid;
-          sh.ahead_weight = before_weight;
-          sh.members = 0u;
+      for (double slack = of_all ? kFilterRough : 0.0;;) {
+        // the weight before a token that is kept is below the share, which lies between these two
+        const double share = (double)want.top_p * (double)mass, need = fmax(share * (1.0 + slack), 0.5), least_need = fmax(share * (1.0 - slack), 0.5);
+        bool certain = (double)all_weight < least_need;
+        if ((double)all_weight >= need) {
+          // (in the bin where top-k ends its last tokens bring the weights there, if none before did)
+          const bool here = (double)before_weight < need && (tid < (int)last_bin ? (double)(before_weight + own_weight) >= need : tid == (int)last_bin);
+          if (here) {
+            sh.found = tid;
+            sh.ahead_weight = before_weight;
+            sh.members = 0u;
+          }
+          __syncthreads();
+          const unsigned int bin = sh.found;
+          const u64 base_weight = sh.ahead_weight;
+          if (sh.count[bin] > kFilterMembers) return true;
+          rank(bin, [&](u64 key, u64 w, unsigned int, u64 aw) __attribute__((always_inline)) {
+            if ((double)(base_weight + aw) < need && (double)(base_weight + aw + w) >= need) {
+              sh.threshold = key;
+              sh.certain = (double)(base_weight + aw) < least_need ? 1u : 0u;
+            }
+          });
+          threshold = sh.threshold;
+          certain = sh.certain != 0u;
+        }  // (else all candidates: the tokens that min-p keeps, or all)
+        if (certain || slack == 0.0) break;
+        mass = 0ull;
+        for (int j = 0; j < nv; ++j) {  // (fetched again: kept until here, the row would not fit the registers)
+          const f32x4 v = load(j);
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            const u64 y = whole(weight(v[c]));
+            mass += v[c] > -INFINITY ? y : 0ull;
+            __builtin_amdgcn_sched_barrier(0);
+          }
         }
-        __syncthreads();
-        const unsigned int bin = sh.found;
-        const u64 base_weight = sh.ahead_weight;
-        if (sh.count[bin] > kFilterMembers) return true;
-        rank(bin, [&](u64 key, u64 w, unsigned int, u64 aw) __attribute__((always_inline)) {
-          if ((double)(base_weight + aw) < need && (double)(base_weight + aw + w) >= need) sh.threshold = key;
-        });
-        threshold = sh.threshold;
-      }  // (else all candidates: the tokens that min-p keeps, or all)
+        mass = block_sum(mass);
+        slack = 0.0;
+      }
     }
     __syncthreads();
   }

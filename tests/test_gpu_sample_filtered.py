@@ -85,6 +85,18 @@ def test_equal_logits(more):
 
 
 @pytest.mark.gpu
+def test_shares_that_end_near_a_token():
+    """Flat rows of 14000 tokens: a share known to 2^-18 covers a tenth of a token's weight, so of 120 rows about twelve need it exactly;
+    temperatures for which it is not taken in float."""
+    z, u = rows(17, 3, 40, 14000, 0.2)
+    ctx = pkg.Context(max_batch=4, max_slots=1, max_topk=1, max_vocab_rows=8, max_nodes=40, max_heads=1, max_head_dim=8)
+    check(z, u, p=[0.9, 0.97, 0.6], ctx=ctx)
+    check(z[:, :4], u[:, :4], p=[0.9, 0.97, 0.6], m=[0.0, 0.5, 0.9], ctx=ctx)
+    check(z[:, :3], u[:, :3], p=[0.9, 0.5, 0.9], t=[1e-33, 1e33, 2.0], ctx=ctx)
+    ctx.close()
+
+
+@pytest.mark.gpu
 def test_no_numbers_and_infinities():
     rng = np.random.default_rng(2)
     z = rng.standard_normal((1, 8, 3001)).astype(np.float32)
