@@ -9,6 +9,13 @@
 //
 // The work - iterations of four tiles, one for each wavefront, of a block of rows - is dealt to the workgroups in equal shares
 // (prefix_plan.h); the four wavefronts' results are joined in the LDS, the shares' by a second kernel.
+//
+// What bounds it.  Four single tokens behind 16384 to 65536 rows (8 key heads of 128): the cache's bytes, 178 MB in 37 us (4.8 TB/s), and the join,
+// 5 us.  64 rows a sequence and key head behind 32768 rows (four sequences, 32 heads, 577 MB, 121 GFLOP): 186 us, the matrix units busy for 0.41
+// of them, the vector units for about half, and the two overlap only in part: a tile takes a wavefront 172 vector instructions beside its 16
+// matrix ones, 64 of them conversions (every block of 32 rows converts every key and value), 16 exponentials.  Short calls (8 single tokens
+// behind 256 to 2048 rows 19 us, 64-node trees 31 us with weights in three parts): the way in - lengths, shares, first tile -, segments of
+// a few iterations, and their joins.
 #include <type_traits>
 
 #include "q4_format.h"
@@ -47,7 +54,9 @@ struct Q4AttnParams {
 };
 
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
-// DT: blocks of 32 components, of a row of the cache too.  FINE: weights in three bf16 parts.
+// DT: blocks of 32 components, of a row of the cache too.  FINE: weights in three bf16 parts, 24 bits together, for a float result; for a bf16 one
+// they are one bf16 each, off by 2^-9 at most as the result itself (against 64 bits the result is off by 1.8e-3 of its norm, 1.7e-3 with float
+// weights), and a tile has 16 products instead of 32.
 template <int DT_, bool FINE_>
 struct Q4Shape {
   static constexpr int DT = DT_, NW = kQ4Tiles;
@@ -56,7 +65,8 @@ struct Q4Shape {
   static constexpr int VB = (DT + 1) / 2;                     // blocks of values in a lane: 32 DT of them in 64 lanes
   // Values in the LDS: a row has 64 bytes a block and as many more as make an odd number of them, four rows have 16 bytes more.  A transposing
   // read of 32 lanes takes 64 bytes of each of four consecutive rows, which then lie in different banks; a write of 16 lanes (0 to 7 with 16
-  // to 23) the same 16 bytes of their blocks, which do if the lanes' rows are of four such groups, two of each (v_row).
+  // to 23) the same 16 bytes of their blocks, which do if the lanes' rows are of four such groups, two of each (v_row).  (The document above
+  // took 201 us so and 217 with a lane pair's rows in their order, 192 cycles of conflicts a tile instead of 64.)
   static constexpr int ROWB = 64 * (DT | 1), FOURB = 4 * ROWB + 16, TILE = 8 * FOURB;
   static __device__ __forceinline__ int place(int row) { return (row >> 2) * FOURB + (row & 3) * ROWB; }
   static constexpr int PART = (DT * 16 + 2) * 64 * 4;         // O, m, l of 32 rows

@@ -8,8 +8,11 @@ namespace ctcspec {
 
 constexpr int kQ4Tiles = 4;  // tiles of 32 keys in an iteration: one for each wavefront of a workgroup
 
-constexpr int kQ4Rows = 32;    // query rows of a workgroup: nodes of a sequence x heads that share a key head
-constexpr int kQ4Waves = 3;    // workgroups that a compute unit holds at once, and wavefronts of each of its four SIMDs
+// Query rows of a workgroup (nodes of a sequence x heads that share a key head), and the workgroups that a compute unit holds at once: with
+// 32 rows the registers of three wavefronts a SIMD hold a row's result and the next tile, with 64 those of two.  (8 sequences x 64 nodes x 32
+// heads behind 256 to 2048 rows, four behind 32768, us: 64 rows and two 57 and 253, 32 and three 42 and 210 - of the kernel as it was then.)
+constexpr int kQ4Rows = 32;
+constexpr int kQ4Waves = 3;
 constexpr int kQ4Groups = 256 * kQ4Waves;
 
 // The cached tiles that a window leaves: the first `lead`, then those from lead + gap on; `count` of them.  A row at position p >= len sees
@@ -33,6 +36,7 @@ CTCSPEC_BOTH Q4Tiles q4_tiles(int len, int window, int sink) {
   return t;
 }
 
+// A block of rows counts as four iterations over the keys beside its own.  (As two: the same times within 2 %.)
 CTCSPEC_BOTH constexpr int q4_units(int iters) { return prefix_block_units(false) + iters * kPrefixOwnWeight; }
 
 // Rows, keys and units are counted in 32 bits: whether that is enough for the largest lengths.
