@@ -603,7 +603,7 @@ typedef struct {
  * out_dt          element type of k_rows, v_rows [B,H_kv,max_rows,dh], 16-byte aligned (either type holds the values exactly)
  *
  * Limits of the three: dh % 8 == 0, dh <= CTCSPEC_MAX_HEAD_DIM; B, H_kv (max_heads), dh, and max_nodes of kv_commit_q4 within the
- * context's limits; kv_cap, max_rows <= 2^30; T <= CTCSPEC_MAX_SLOTS.
+ * context's limits; kv_cap <= 2^30, max_rows <= 2^27; T <= CTCSPEC_MAX_SLOTS.
  */
 int kv_append_q4(ctcspec_ctx* ctx, ctcspec_dtype dt, const void* k_rows, const void* v_rows, const int32_t* n_rows, int max_rows,
                  const ctcspec_q4_cache* cache, const int64_t* kv_off, const int32_t* ctx_len, int kv_cap, int B, int H_kv,
@@ -688,7 +688,7 @@ int q4_verify_attn(ctcspec_ctx* ctx, ctcspec_dtype dt, const void* q, const ctcs
  * target_sampled [B,max_nodes] int32 device out
  * n_kept         [B,max_nodes] int32 device out or NULL
  * logp           [B,max_nodes] float device out or NULL
- * Limits: V <= 262144, B <= 65535.  The same bits on every run.
+ * Limits: V <= 262144, B <= 65535, max_nodes < 2^22.  The same bits on every run.
  */
 int verify_sample_filtered(ctcspec_ctx* ctx, const float* logits, const int32_t* n_nodes, const float* uniforms,
                            const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p, int B,

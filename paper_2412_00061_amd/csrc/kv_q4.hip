@@ -150,8 +150,8 @@ static int q4_check(ctcspec_ctx* ctx, const char* call, ctcspec_dtype dt, const 
   CTCSPEC_REQUIRE(ctx, dh % 8 == 0 && dh <= CTCSPEC_MAX_HEAD_DIM, CTCSPEC_EUNSUPPORTED, "%s: dh must be a multiple of 8 and <= %d", call,
                   CTCSPEC_MAX_HEAD_DIM);
   CTCSPEC_REQUIRE(ctx, B <= ctx->lim.max_batch && B <= 65535 && dh <= ctx->lim.max_head_dim && H_kv <= ctx->lim.max_heads && H_kv <= 65535 && kv_cap <= 1 << 30 &&
-                           rows <= 1 << 30,
-                  CTCSPEC_EUNSUPPORTED, "%s: shape exceeds the context's limits, or rows beyond 2^30", call);
+                           rows <= 1 << 27,  // (16 to 64 rows a workgroup: below 2^32 threads)
+                  CTCSPEC_EUNSUPPORTED, "%s: shape exceeds the context's limits, kv_cap beyond 2^30 or max_rows beyond 2^27", call);
   CTCSPEC_REQUIRE(ctx, aligned16(cache->k_codes) && aligned16(cache->v_codes) && aligned16(k_rows) && aligned16(v_rows) &&
                            q4_scales_aligned(cache),
                   CTCSPEC_EINVAL, "%s: codes and rows must be 16-byte aligned, scales 4-byte aligned", call);

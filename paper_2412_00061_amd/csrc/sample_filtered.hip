@@ -1006,7 +1006,8 @@ extern "C" int verify_sample_filtered(ctcspec_ctx* ctx, const float* logits, con
   CTCSPEC_REQUIRE(ctx, logits && n_nodes && uniforms && temperature && target_sampled, CTCSPEC_EINVAL, "verify_sample_filtered: null pointer");
   CTCSPEC_REQUIRE(ctx, B > 0 && max_nodes > 0 && V > 0, CTCSPEC_EINVAL, "verify_sample_filtered: sizes must be positive");
   CTCSPEC_REQUIRE(ctx, aligned16(logits), CTCSPEC_EINVAL, "verify_sample_filtered: logits must be 16-byte aligned");
-  CTCSPEC_REQUIRE(ctx, V <= kFilterMaxV && B <= 65535, CTCSPEC_EUNSUPPORTED, "verify_sample_filtered: V <= %d, B <= 65535", kFilterMaxV);
+  CTCSPEC_REQUIRE(ctx, V <= kFilterMaxV && B <= 65535 && max_nodes < 1 << 22, CTCSPEC_EUNSUPPORTED,
+                  "verify_sample_filtered: V <= %d, B <= 65535, max_nodes < 2^22", kFilterMaxV);
   FilterParams p;
   p.logits = logits; p.n_nodes = n_nodes; p.uniforms = uniforms; p.temperature = temperature; p.top_k = top_k; p.top_p = top_p; p.min_p = min_p;
   p.N = max_nodes; p.V = V; p.target = target_sampled; p.n_kept = n_kept; p.logp = logp;

@@ -176,7 +176,7 @@ ARGS = dict(logits=P, n=P, u=P, t=P, k=None, p=None, m=None, B=2, N=5, V=100, ou
 
 @pytest.mark.parametrize("key,value,code,text", [(k, None, INVALID, "null pointer") for k in ("logits", "n", "u", "t", "out")] +
                          [(k, v, INVALID, "positive") for k in ("B", "N", "V") for v in (0, -1)] +
-                         [("logits", P + 4, INVALID, "aligned"), ("V", 262145, UNSUPPORTED, "V <="), ("B", 65536, UNSUPPORTED, "B <=")])
+                         [("logits", P + 4, INVALID, "aligned"), ("V", 262145, UNSUPPORTED, "V <="), ("B", 65536, UNSUPPORTED, "B <="), ("N", 1 << 22, UNSUPPORTED, "max_nodes <")])
 def test_refusals(key, value, code, text):
     HostContext().refuses("verify_sample_filtered", list(dict(ARGS, **{key: value}).values()), code, text)
 

@@ -35,6 +35,7 @@ BAD += [(name, key, value, UNSUPPORTED, "limits") for name, args in CALLS.items(
 BAD += [(name, key, P + 8, INVALID, "aligned") for name in CALLS for key in ("k", "v")]
 BAD += [(name, "cache", cache(**{part: P + 4}), INVALID, "aligned") for name in CALLS for part in ("k_codes", "v_codes")]
 BAD += [(name, "cache", cache(**{part: P + 2}), INVALID, "4-byte") for name in [*CALLS, "q4_verify_attn"] for part in ("k_scales", "v_scales")]
+BAD += [(name, "max_rows", (1 << 27) + 1, UNSUPPORTED, "2^27") for name in ("kv_append_q4", "kv_read_q4")]
 BAD += [("kv_commit_q4", "T", 9, UNSUPPORTED, "T <= 8"), ("kv_append_q4", "out", P, INVALID, "ctx_len_out"), ("kv_commit_q4", "out", P, INVALID, "ctx_len_out")]
 
 
@@ -56,6 +57,17 @@ BAD += [("q4_verify_attn", "cache", cache(**{part: P + 4}), INVALID, "aligned") 
 def test_refusals(name, key, value, code, text):
     args = dict(CALLS[name], **{key: value})
     HostContext(max_head_dim=64 if key == "dh" else 128).refuses(name, list(args.values()), code, text)
+
+
+def test_prepared_calls_take_the_cache(monkeypatch):
+    """(What is refused shows that the struct arrived: its code pointers were looked at.)"""
+    ctx = HostContext()
+    ctx._check = lambda rc, what: (_ for _ in ()).throw(pkg.CtcspecError(ctx.lib.ctcspec_last_error(ctx.handle).decode()))
+    args = {k: v for k, v in READ.items() if k != "cache"}
+    with pytest.raises(pkg.CtcspecError, match="null pointer"):
+        pkg.prepared(ctx, "kv_read_q4", binding._Q4Cache(P, P, None, P), *args.values())()
+    with pytest.raises(pkg.CtcspecError, match="limits"):
+        pkg.prepared(ctx, "kv_read_q4", binding._Q4Cache(P, P, P, P), *dict(args, B=9).values())()
 
 
 def test_no_context():
