@@ -7,8 +7,8 @@
 // free, as long as the query's lanes hold the same.  Values are needed by columns: they are converted, written to the LDS a row at a time
 // and fetched by transposing reads, each wavefront its own tile, so the loop has no barriers.
 //
-// The work - iterations of four tiles, one for each wavefront, of a block of rows - is dealt to the workgroups in equal shares
-// (prefix_plan.h); the four wavefronts' results are joined in the LDS, the shares' by a second kernel.
+// The work - iterations of four tiles, one for each wavefront, of a block of rows - is dealt to the workgroups in pieces of blocks, or in equal
+// shares that go across them (q4_plan.h, prefix_plan.h); the four wavefronts' results are joined in the LDS, the shares' by a second kernel.
 //
 // What bounds it.  Four single tokens behind 16384 to 65536 rows (8 key heads of 128): the cache's bytes, 178 MB in 37 us (4.8 TB/s), and the join,
 // 5 us.  64 rows a sequence and key head behind 32768 rows (four sequences, 32 heads, 577 MB, 121 GFLOP): 186 us, the matrix units busy for 0.41
@@ -90,6 +90,7 @@ struct Q4Work {
   int unit0, block0;             // lane: units and blocks of the sequences before it, for one key head
   int head_units, head_blocks;   // of a key head
   int units;                     // of all key heads
+  int most;                      // iterations of a piece: then units are pieces, a share each; or 0
 };
 template <typename SH>
 __device__ __forceinline__ Q4Work q4_read_work(const Q4AttnParams& p) {
@@ -113,6 +114,37 @@ __device__ __forceinline__ Q4Work q4_read_work(const Q4AttnParams& p) {
   t.head_blocks = __builtin_amdgcn_readlane(b, p.B - 1);
   t.head_units = __builtin_amdgcn_readlane(u, p.B - 1);
   t.units = p.H_kv * t.head_units;
+  // Where little balance is lost, every share is a piece of one block, and no workgroup has parts of two: lane by lane the pieces' size, from the
+  // ideal one on, and the first that makes no more pieces than there are workgroups.
+  if (p.H_kv * t.head_blocks <= kQ4Groups && t.head_blocks > 0) {
+    const int all = p.H_kv * ((t.head_units - t.head_blocks * q4_units(0)) / kPrefixOwnWeight);
+    int ideal = (all - 1) / kQ4Groups + 1;
+    ideal = ideal < kQ4LeastPiece ? kQ4LeastPiece : ideal;
+    const int most = ideal + lane * (ideal < 64 ? 1 : ideal / 32);
+    const float inv = __builtin_amdgcn_rcpf((float)most);
+    int pieces = 0;
+    for (int x = 0; x < p.B; ++x) {  // q4_pieces, the division by a product and what it may be off by
+      const int n = __builtin_amdgcn_readlane(t.iters, x) - 1, blocks = __builtin_amdgcn_readlane(t.blocks, x);
+      int q = (int)((float)n * inv);
+      const int r = n - q * most;
+      q += r >= most ? 1 : (r < 0 ? -1 : 0);
+      pieces += n < 0 ? 0 : blocks * (q + 1);
+    }
+    const unsigned long long fits = __builtin_amdgcn_ballot_w64(p.H_kv * pieces <= kQ4Groups);
+    const int first = fits ? __builtin_ctzll(fits) : 0, size = __builtin_amdgcn_readlane(most, first);
+    if (fits && size <= ideal + kQ4PieceSlack) {
+      t.most = size;
+      const int own = t.blocks * q4_pieces(t.iters, size);
+      int s = own;
+      for (int d = 1; d < p.B; d *= 2) {
+        const int sb = __shfl_up(s, d, 64);
+        if (lane >= d) s += sb;
+      }
+      t.unit0 = s - own;
+      t.head_units = __builtin_amdgcn_readlane(s, p.B - 1);
+      t.units = p.H_kv * t.head_units;
+    }
+  }
   return t;
 }
 
@@ -174,7 +206,9 @@ __global__ __launch_bounds__(64 * SH::NW, kQ4Waves) void q4_attn_kernel(Q4AttnPa
   const int wave = uniform(threadIdx.x >> 6);
   const long long my_off = lane < p.B ? p.kv_off[lane] : 0;
   const Q4Work t = q4_read_work<SH>(p);
-  const Deal d = prefix_deal(t.units, kQ4Groups);
+  Deal d = prefix_deal(t.units, kQ4Groups);
+  const int most = t.most;
+  if (most) d = Deal{t.units, t.units, 1, 0};
   // (consecutive shares - neighbouring keys - to the same of the 8 XCDs)
   const int per = (d.groups + 7) / 8, w = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
   if ((int)(blockIdx.x >> 3) >= per || w >= d.groups) return;
@@ -220,18 +254,18 @@ __global__ __launch_bounds__(64 * SH::NW, kQ4Waves) void q4_attn_kernel(Q4AttnPa
     // (sequences without nodes have no units: the last sequence that starts at or before the unit and has some)
     const int b = 63 - __builtin_clzll(__builtin_amdgcn_ballot_w64(table[kIters][seg_lane] > 0 && table[kUnit0][seg_lane] <= in_head));
     const int n = uniform(table[kNodes][b]), L = uniform(table[kCtx][b]);
-    const int units = q4_units(uniform(table[kIters][b]));
+    const int iters = uniform(table[kIters][b]), units = uniform(most ? q4_pieces(iters, most) : q4_units(iters));
     const int in_seq = in_head - uniform(table[kUnit0][b]), blk = uniform(in_seq / units), at_unit = in_seq - blk * units;
     const int slot = w + kh * head_blocks + uniform(table[kBlock0][b]) + blk;
     const int share = uniform(units - at_unit < u1 - u ? units - at_unit : u1 - u);
     u += share;
-    const int it0 = uniform(prefix_iterations(at_unit, kPrefixOwnWeight, false));
-    const int niter = uniform(prefix_iterations(at_unit + share, kPrefixOwnWeight, false)) - it0;
+    const int it0 = uniform(most ? q4_piece_begin(iters, units, at_unit) : prefix_iterations(at_unit, kPrefixOwnWeight, false));
+    const int niter = uniform(most ? q4_piece_begin(iters, units, at_unit + 1) : prefix_iterations(at_unit + share, kPrefixOwnWeight, false)) - it0;
     if (niter <= 0) continue;
     if (threadIdx.x == 0) {  // (the join need not deal the work once more)
       int* span = p.span + (((size_t)kh * p.B + b) * p.blocks + blk) * 4;
       if (it0 == 0) *(u32x2*)span = u32x2{(unsigned)(slot - w), (unsigned)w};
-      if (q4_units(it0 + niter) == units) span[2] = w;
+      if (it0 + niter == iters) span[2] = w;
     }
     const Q4Tiles tiles = q4_tiles(L, p.window, p.sink);
     const int total = tiles.count + (n + 31) / 32;

@@ -1,5 +1,5 @@
 // q4_verify_attn: rows of a workgroup, which tiles of keys a window leaves, and the workspace.  The work is dealt to the workgroups as in
-// prefix_plan.h.  Code without HIP, so that a test can ask it.
+// prefix_plan.h, or in pieces of blocks.  Code without HIP, so that a test can ask it.
 #pragma once
 
 #include "prefix_plan.h"
@@ -38,6 +38,19 @@ CTCSPEC_BOTH Q4Tiles q4_tiles(int len, int window, int sink) {
 
 // A block of rows counts as four iterations over the keys beside its own.  (As two: the same times within 2 %.)
 CTCSPEC_BOTH constexpr int q4_units(int iters) { return prefix_block_units(false) + iters * kPrefixOwnWeight; }
+
+// A block's iterations in pieces of `most` at the most, as equal as can be: how many pieces, and where the i-th begins.
+CTCSPEC_BOTH constexpr int q4_pieces(int iters, int most) { return iters > 0 ? (iters - 1) / most + 1 : 0; }
+CTCSPEC_BOTH constexpr int q4_piece_begin(int iters, int pieces, int i) {
+  const int each = iters / pieces, more = iters - each * pieces;
+  return i * each + (i < more ? i : more);
+}
+// Such pieces are the shares where they are no more than the workgroups and at most kQ4PieceSlack iterations longer than equal shares would be -
+// what a second block in a share costs -, and are not made shorter than kQ4LeastPiece.  (Eight sequences of one length, 32 heads; us with
+// equal shares / pieces of 2 / of 4 or more.  Single tokens behind 224, 480, 992, 2048 rows: 14.8 / 13.8 / 13.8, 19.7 / 16.6 / 16.1, 20.6 /
+// 21.8 / 21.4, 29.0 / 29.9 / 29.9; 64 nodes: 25.0 / 23.1 / 23.3, 26.2 / 25.6 / 25.7, 38.0 / 33.7 / 33.3, 52.5 / 53.7 / 53.7; of
+// 256 to 2048 rows, 64 nodes: 39.6 / 36.6 / 37.4.)
+constexpr int kQ4LeastPiece = 4, kQ4PieceSlack = 4;
 
 // Rows, keys and units are counted in 32 bits: whether that is enough for the largest lengths.
 inline bool q4_units_fit(long long B, int H_kv, long long seq_rows, int kv_cap, int max_nodes) {

@@ -17,6 +17,9 @@ int main() {
     if (what == 't') {
       const Q4Tiles t = q4_tiles(a, b, c);
       printf("%d %d %d\n", t.lead, t.gap, t.count);
+    } else if (what == 'p') {
+      const int pieces = q4_pieces(a, b);
+      for (int i = 0; i <= pieces; ++i) printf("%d %d %d\n", pieces, i, pieces ? q4_piece_begin(a, pieces, i) : 0);
     } else if (what == 'f') {
       printf("%d 0 0\n", (int)q4_units_fit(a, b, c, d, e));
     } else {
@@ -50,6 +53,18 @@ def test_a_window_keeps_every_tile_that_a_row_sees():
         seen = {j // 32 for j in range(L) if not W or j > L - W or j < S}  # (a row at a later position sees fewer)
         assert seen <= tiles <= set(range((L + 31) // 32)), (L, W, S)
         assert len(tiles) == count <= len(seen) + 1  # (a window of 1 sees no cached row, its tile is kept)
+
+
+def test_pieces_cover_a_block():
+    for iters in (0, 1, 2, 3, 7, 64, 257, 2000, 8_388_609):
+        for most in (1, 2, 4, 5, 86, 300, 30000):
+            if iters / most > 5000:
+                continue
+            got = ask([("p", iters, most, 0, 0, 0)])
+            begins = [x[2] for x in got]
+            assert got[0][0] == -(-iters // most) and begins[0] == 0 and begins[-1] == iters
+            sizes = [b - a for a, b in zip(begins, begins[1:])]
+            assert all(1 <= x <= most for x in sizes) and (not sizes or max(sizes) - min(sizes) <= 1)
 
 
 def test_units_are_counted_for_the_largest_lengths():
