@@ -175,6 +175,25 @@ __device__ __forceinline__ Q4Mask q4_tree_mask(const Q4AttnParams& p, int b, int
   return m;
 }
 
+// Four components from `at` on, and those 8, 16 .. behind, of a row of the result: its weighted values o, the maximum m and the sum l of its weights.
+template <int N>
+__device__ __forceinline__ void q4_write(const Q4AttnParams& p, size_t row, bool with_lse, int at, const f32x4 (&o)[N], float m, float l) {
+  const bool none = m == -INFINITY && l == 0.f;  // no key at all
+  const float inv = none ? 0.f : 1.0f / l;
+  if (p.lse && with_lse) p.lse[row] = none ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    if (at + 8 * i >= p.dh) continue;
+    const f32x4 v = none ? f32x4{0.f, 0.f, 0.f, 0.f} : o[i] * inv;
+    if (p.out_bf16) {
+      *(u32x2*)((unsigned short*)p.out + row * p.dh + at + 8 * i) = u32x2{__builtin_bit_cast(unsigned int, bf16x2{(__bf16)v[0], (__bf16)v[1]}),
+                                                                          __builtin_bit_cast(unsigned int, bf16x2{(__bf16)v[2], (__bf16)v[3]})};
+    } else {
+      *(f32x4*)((float*)p.out + row * p.dh + at + 8 * i) = v;
+    }
+  }
+}
+
 #if defined(__HIP_DEVICE_COMPILE__)
 typedef __attribute__((address_space(3))) unsigned char lds_byte;
 // of a value of lanes 32 apart, in both
@@ -262,7 +281,8 @@ __global__ __launch_bounds__(64 * SH::NW, kQ4Waves) void q4_attn_kernel(Q4AttnPa
     const int it0 = uniform(most ? q4_piece_begin(iters, units, at_unit) : prefix_iterations(at_unit, kPrefixOwnWeight, false));
     const int niter = uniform(most ? q4_piece_begin(iters, units, at_unit + 1) : prefix_iterations(at_unit + share, kPrefixOwnWeight, false)) - it0;
     if (niter <= 0) continue;
-    if (threadIdx.x == 0) {  // (the join need not deal the work once more)
+    const bool whole = it0 == 0 && niter == iters;  // (then there is nothing to join)
+    if (threadIdx.x == 0 && !whole) {  // (the join need not deal the work once more)
       int* span = p.span + (((size_t)kh * p.B + b) * p.blocks + blk) * 4;
       if (it0 == 0) *(u32x2*)span = u32x2{(unsigned)(slot - w), (unsigned)w};
       if (it0 + niter == iters) span[2] = w;
@@ -584,7 +604,27 @@ __global__ __launch_bounds__(64 * SH::NW, kQ4Waves) void q4_attn_kernel(Q4AttnPa
     // ---- what the segment leaves, in the order of the registers -------------------------------------------------------------
     if (wave == 0) {
       l_run = half_sum(l_run);
-      if (blk * kQ4Rows + (el & 31) < n * p.group) {
+      // A block that one workgroup has whole is written by it, unless the join has infinite values of the tree, or such that are no numbers, to
+      // add.  (8 sequences x 64 nodes x 32 heads behind 0, 224, 480 rows, us: 16.2, 18.9, 23.3; by way of the join 22.1, 23.3, 25.7.)
+      const bool direct = whole && uniform(table[kOdd][0]) == 0;
+      if (threadIdx.x == 0 && whole) {
+        int* span = p.span + (((size_t)kh * p.B + b) * p.blocks + blk) * 4;
+        *(u32x2*)span = u32x2{(unsigned)(slot - w), direct ? 1u : (unsigned)w};
+        span[2] = direct ? 0 : w;
+      }
+      int heads = p.group;
+      asm volatile("" : "+s"(heads));
+      const int r = blk * kQ4Rows + (el & 31), node = r / heads, hg = r - node * heads;
+      if (r < n * heads && direct) {
+        const size_t row = ((size_t)b * p.H + kh * heads + hg) * p.max_nodes + node;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+          f32x4 x[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[i] = f32x4{o[dt][4 * i], o[dt][4 * i + 1], o[dt][4 * i + 2], o[dt][4 * i + 3]};
+          q4_write(p, row, dt == 0 && el < 32, 32 * dt + 4 * (el >> 5), x, m_run, l_run);
+        }
+      } else if (r < n * heads) {
         float* po = p.po + (size_t)slot * (DT * 1024) + el * 4;
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
@@ -618,7 +658,7 @@ __global__ __launch_bounds__(64 * SH::DT) void q4_join_kernel(Q4AttnParams p) {
   const int* span = p.span + (((size_t)kh * p.B + b) * p.blocks + blk) * 4;
   const int item = span[0], w0 = span[1], w1 = span[2];  // (of a block without rows whatever was there)
   const int n = p.n_nodes[b] < p.max_nodes ? p.n_nodes[b] : p.max_nodes, rows = n * p.group - blk * 32;
-  if (rows <= 0) return;
+  if (rows <= 0 || w0 > w1) return;  // (one workgroup had the whole block and has written the rows)
   int shares = 1;
   while (shares < 32 && shares <= w1 - w0 && 32 / (2 * shares) >= rows) shares *= 2;
   const int of = 32 / shares, c = lane & (of - 1), share = (lane & 31) / of, r = blk * 32 + c;
@@ -683,21 +723,7 @@ __global__ __launch_bounds__(64 * SH::DT) void q4_join_kernel(Q4AttnParams p) {
     }
   }
   const size_t row = ((size_t)b * p.H + kh * p.group + hg) * p.max_nodes + node;
-  const bool none = m == -INFINITY && l == 0.f;  // no key at all
-  const float inv = none ? 0.f : 1.0f / l;
-  if (p.lse && dt == 0 && part == 0 && h2 == 0) p.lse[row] = none ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
-#pragma unroll
-  for (int i = 0; i < OWN; ++i) {
-    const int at = 32 * dt + 8 * (part + i) + 4 * h2;
-    if (at >= p.dh) continue;
-    const f32x4 v = none ? f32x4{0.f, 0.f, 0.f, 0.f} : o[i] * inv;
-    if (p.out_bf16) {
-      *(u32x2*)((unsigned short*)p.out + row * p.dh + at) = u32x2{__builtin_bit_cast(unsigned int, bf16x2{(__bf16)v[0], (__bf16)v[1]}),
-                                                                  __builtin_bit_cast(unsigned int, bf16x2{(__bf16)v[2], (__bf16)v[3]})};
-    } else {
-      *(f32x4*)((float*)p.out + row * p.dh + at) = v;
-    }
-  }
+  q4_write(p, row, dt == 0 && part == 0 && h2 == 0, 32 * dt + 8 * part + 4 * h2, o, m, l);
 }
 
 // ---- host side -----------------------------------------------------------------------------------------------------------

@@ -46,7 +46,7 @@ CTCSPEC_BOTH constexpr int q4_piece_begin(int iters, int pieces, int i) {
   return i * each + (i < more ? i : more);
 }
 // Such pieces are the shares where they are no more than the workgroups and at most kQ4PieceSlack iterations longer than equal shares would be -
-// what a second block in a share costs -, and are not made shorter than kQ4LeastPiece.  (Eight sequences of one length, 32 heads; us with
+// what a second block in a share costs -, and are not made shorter than kQ4LeastPiece.  (When every block went by way of the join: eight sequences of one length, 32 heads; us with
 // equal shares / pieces of 2 / of 4 or more.  Single tokens behind 224, 480, 992, 2048 rows: 14.8 / 13.8 / 13.8, 19.7 / 16.6 / 16.1, 20.6 /
 // 21.8 / 21.4, 29.0 / 29.9 / 29.9; 64 nodes: 25.0 / 23.1 / 23.3, 26.2 / 25.6 / 25.7, 38.0 / 33.7 / 33.3, 52.5 / 53.7 / 53.7; of
 // 256 to 2048 rows, 64 nodes: 39.6 / 36.6 / 37.4.)
