@@ -10,11 +10,11 @@
 // The work - iterations of four tiles, one for each wavefront, of a block of rows - is dealt to the workgroups in pieces of blocks, or in equal
 // shares that go across them (q4_plan.h, prefix_plan.h); the four wavefronts' results are joined in the LDS, the shares' by a second kernel.
 //
-// What bounds it.  Four single tokens behind 16384 to 65536 rows (8 key heads of 128): the cache's bytes, 178 MB in 37 us (4.8 TB/s), and the join,
-// 5 us.  64 rows a sequence and key head behind 32768 rows (four sequences, 32 heads, 577 MB, 121 GFLOP): 186 us, the matrix units busy for 0.41
-// of them, the vector units for about half, and the two overlap only in part: a tile takes a wavefront 172 vector instructions beside its 16
+// What bounds it.  Four single tokens behind 16384 to 65536 rows (8 key heads of 128): the cache's bytes, 178 MB in 37 to 39 us (4.7 TB/s), and the join,
+// 5 us.  64 rows a sequence and key head behind 32768 rows (four sequences, 32 heads, 577 MB, 121 GFLOP): 174 us, the matrix units busy for 0.43
+// of them, the vector units for about half, and the two overlap only in part: a tile takes a wavefront 174 vector instructions beside its 16
 // matrix ones, 64 of them conversions (every block of 32 rows converts every key and value), 16 exponentials.  Short calls (8 single tokens
-// behind 256 to 2048 rows 19 us, 64-node trees 31 us with weights in three parts): the way in - lengths, shares, first tile -, segments of
+// behind 256 to 2048 rows 19 to 21 us, 64-node trees 31 us with weights in three parts): the way in - lengths, shares, first tile -, segments of
 // a few iterations, and their joins.
 #include <type_traits>
 
@@ -452,6 +452,15 @@ __global__ __launch_bounds__(64 * SH::NW, kQ4Waves) void q4_attn_kernel(Q4AttnPa
     };
     // ---- cached tiles -------------------------------------------------------------------------------------------------------------------
     for (int x = first; x < cached_end; x += kQ4Tiles) {
+      // A SIMD serves its oldest wavefront first: three that began together ended after 118, 163 and 209 us of a document's attention, and the
+      // last one alone is slow.  So a wavefront's priority falls with every quarter of its way.  (187 us -> 181; shorter ones leave it.)
+      if (cached_end - first >= 16 * kQ4Tiles) {
+        const int left = 4 * (cached_end - x), all = cached_end - first;
+        if (left > 3 * all) __builtin_amdgcn_s_setprio(3);
+        else if (left > 2 * all) __builtin_amdgcn_s_setprio(2);
+        else if (left > all) __builtin_amdgcn_s_setprio(1);
+        else __builtin_amdgcn_s_setprio(0);
+      }
       f32x16 s;
       cached_scores(s);
       if (x < x_all || x >= x_part) {  // not every row sees every key
