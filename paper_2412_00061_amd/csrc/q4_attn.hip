@@ -57,10 +57,11 @@ __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirs
 // DT: blocks of 32 components, of a row of the cache too.  FINE: weights in three bf16 parts, 24 bits together, for a float result; for a bf16 one
 // they are one bf16 each, off by 2^-9 at most as the result itself (against 64 bits the result is off by 1.8e-3 of its norm, 1.7e-3 with float
 // weights), and a tile has 16 products instead of 32.
-template <int DT_, bool FINE_>
+// ALONE: a workgroup has a block of rows whole, there is neither a deal nor a join.
+template <int DT_, bool FINE_, bool ALONE_>
 struct Q4Shape {
   static constexpr int DT = DT_, NW = kQ4Tiles;
-  static constexpr bool FINE = FINE_;
+  static constexpr bool FINE = FINE_, ALONE = ALONE_;
   static constexpr int KB = (DT + 1) / 2, QU = 4 * KB;        // blocks of a key in a lane; steps of 16 elements of a product
   static constexpr int VB = (DT + 1) / 2;                     // blocks of values in a lane: 32 DT of them in 64 lanes
   // Values in the LDS: a row has 64 bytes a block and as many more as make an odd number of them, four rows have 16 bytes more.  A transposing
@@ -102,7 +103,7 @@ __device__ __forceinline__ Q4Work q4_read_work(const Q4AttnParams& p) {
     t.ctx = L < 0 ? 0 : (L > p.kv_cap ? p.kv_cap : L);
   }
   t.blocks = (t.n * p.group + kQ4Rows - 1) / kQ4Rows;
-  t.iters = t.n ? (q4_tiles(t.ctx, p.window, p.sink).count + (t.n + 31) / 32 + kQ4Tiles - 1) / kQ4Tiles : 0;
+  t.iters = t.n ? q4_iterations(t.n, t.ctx, p.window, p.sink) : 0;
   const int mine = t.blocks * q4_units(t.iters);
   int b = t.blocks, u = mine;
   for (int d = 1; d < p.B; d *= 2) {
@@ -132,7 +133,7 @@ __device__ __forceinline__ Q4Work q4_read_work(const Q4AttnParams& p) {
     }
     const unsigned long long fits = __builtin_amdgcn_ballot_w64(p.H_kv * pieces <= kQ4Groups);
     const int first = fits ? __builtin_ctzll(fits) : 0, size = __builtin_amdgcn_readlane(most, first);
-    if (fits && size <= ideal + kQ4PieceSlack) {
+    if (fits && size <= ideal + ideal / 2 + kQ4PieceSlack) {
       t.most = size;
       const int own = t.blocks * q4_pieces(t.iters, size);
       int s = own;
@@ -175,6 +176,24 @@ __device__ __forceinline__ Q4Mask q4_tree_mask(const Q4AttnParams& p, int b, int
   return m;
 }
 
+// Values of tree nodes that are infinite or not a number, left out so far: into the rows that see them.  (o: as in q4_write.)
+template <int N>
+__device__ __forceinline__ void q4_add_odd(const Q4AttnParams& p, int b, int kh, int node, int n, int at, f32x4 (&o)[N]) {
+  const int len = p.ctx_len[b], L = len < 0 ? 0 : (len > p.kv_cap ? p.kv_cap : len);
+  const Q4Mask mask = q4_tree_mask(p, b, node, n, L, p.window > 0 ? q4_depth(p, b, node) : 0);
+  const unsigned short* vt = (const unsigned short*)p.v_tree + ((size_t)b * p.H_kv + kh) * p.max_nodes * p.dh;
+  for (int j = 0; j < n; ++j) {
+    if (!mask.node(j)) continue;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (at + 8 * i + e >= p.dh) continue;
+        const float v = bf16_bits_to_float(vt[(size_t)j * p.dh + at + 8 * i + e]);
+        if ((__float_as_uint(v) & 0x7f800000u) == 0x7f800000u) o[i][e] += v;
+      }
+  }
+}
 // Four components from `at` on, and those 8, 16 .. behind, of a row of the result: its weighted values o, the maximum m and the sum l of its weights.
 template <int N>
 __device__ __forceinline__ void q4_write(const Q4AttnParams& p, size_t row, bool with_lse, int at, const f32x4 (&o)[N], float m, float l) {
@@ -223,31 +242,36 @@ __global__ __launch_bounds__(64 * SH::NW, kQ4Waves) void q4_attn_kernel(Q4AttnPa
   constexpr int DT = SH::DT, KB = SH::KB, VB = SH::VB, QU = SH::QU;
   const int lane = threadIdx.x & 63;
   const int wave = uniform(threadIdx.x >> 6);
-  const long long my_off = lane < p.B ? p.kv_off[lane] : 0;
-  const Q4Work t = q4_read_work<SH>(p);
-  Deal d = prefix_deal(t.units, kQ4Groups);
-  const int most = t.most;
-  if (most) d = Deal{t.units, t.units, 1, 0};
-  // (consecutive shares - neighbouring keys - to the same of the 8 XCDs)
-  const int per = (d.groups + 7) / 8, w = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
-  if ((int)(blockIdx.x >> 3) >= per || w >= d.groups) return;
-  int u = uniform(d.begin(w));
-  const int u1 = uniform(d.begin(w + 1));
-
-  // What the lanes know about the sequences, out of the registers while the keys go by; and a flag.
   int(*table)[64] = (int(*)[64])(smem + SH::STAGE);
   enum { kNodes, kCtx, kIters, kUnit0, kBlock0, kOffLow, kOffHigh, kOdd };
-  if (wave == 0) {
-    table[kNodes][lane] = t.n;
-    table[kCtx][lane] = t.ctx;
-    table[kIters][lane] = t.iters;
-    table[kUnit0][lane] = t.unit0;
-    table[kBlock0][lane] = t.block0;
-    table[kOffLow][lane] = (int)my_off;
-    table[kOffHigh][lane] = (int)(my_off >> 32);
+  int u = 0, u1 = 1, w = 0, most = 0, head_units = 0, head_blocks = 0;
+  Deal d{};
+  if constexpr (!SH::ALONE) {
+    const long long my_off = lane < p.B ? p.kv_off[lane] : 0;
+    const Q4Work t = q4_read_work<SH>(p);
+    d = prefix_deal(t.units, kQ4Groups);
+    most = t.most;
+    if (most) d = Deal{t.units, t.units, 1, 0};
+    // (consecutive shares - neighbouring keys - to the same of the 8 XCDs)
+    const int per = (d.groups + 7) / 8;
+    w = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+    if ((int)(blockIdx.x >> 3) >= per || w >= d.groups) return;
+    u = uniform(d.begin(w));
+    u1 = uniform(d.begin(w + 1));
+    // What the lanes know about the sequences, out of the registers while the keys go by; and a flag.
+    if (wave == 0) {
+      table[kNodes][lane] = t.n;
+      table[kCtx][lane] = t.ctx;
+      table[kIters][lane] = t.iters;
+      table[kUnit0][lane] = t.unit0;
+      table[kBlock0][lane] = t.block0;
+      table[kOffLow][lane] = (int)my_off;
+      table[kOffHigh][lane] = (int)(my_off >> 32);
+    }
+    __syncthreads();
+    head_units = t.head_units;
+    head_blocks = t.head_blocks;
   }
-  __syncthreads();
-  const int head_units = t.head_units, head_blocks = t.head_blocks;
   unsigned char* vtile = smem + wave * SH::TILE;
   const unsigned int vbase = (unsigned int)(size_t)(lds_byte*)vtile;
   // the transposing read: 16 lanes fetch 4 rows x 16 components, 8 bytes each, and lane s of them receives component s of the four rows
@@ -267,21 +291,43 @@ __global__ __launch_bounds__(64 * SH::NW, kQ4Waves) void q4_attn_kernel(Q4AttnPa
     // ---- which block of rows, which keys -------------------------------------------------------------------------------
     int seg_lane = lane;  // (as something new: addresses that only a segment's ends need are formed there)
     asm volatile("" : "+v"(seg_lane));
-    int per_head = head_units, group = p.group;  // (and what divisions by them take)
-    asm volatile("" : "+s"(per_head), "+s"(group));
-    const int kh = uniform(u / per_head), in_head = u - kh * per_head;
-    // (sequences without nodes have no units: the last sequence that starts at or before the unit and has some)
-    const int b = 63 - __builtin_clzll(__builtin_amdgcn_ballot_w64(table[kIters][seg_lane] > 0 && table[kUnit0][seg_lane] <= in_head));
-    const int n = uniform(table[kNodes][b]), L = uniform(table[kCtx][b]);
-    const int iters = uniform(table[kIters][b]), units = uniform(most ? q4_pieces(iters, most) : q4_units(iters));
-    const int in_seq = in_head - uniform(table[kUnit0][b]), blk = uniform(in_seq / units), at_unit = in_seq - blk * units;
-    const int slot = w + kh * head_blocks + uniform(table[kBlock0][b]) + blk;
-    const int share = uniform(units - at_unit < u1 - u ? units - at_unit : u1 - u);
-    u += share;
-    const int it0 = uniform(most ? q4_piece_begin(iters, units, at_unit) : prefix_iterations(at_unit, kPrefixOwnWeight, false));
-    const int niter = uniform(most ? q4_piece_begin(iters, units, at_unit + 1) : prefix_iterations(at_unit + share, kPrefixOwnWeight, false)) - it0;
-    if (niter <= 0) continue;
-    const bool whole = it0 == 0 && niter == iters;  // (then there is nothing to join)
+    int kh, b, n, L, blk, slot = 0, iters, it0 = 0, niter;
+    long long off;
+    if constexpr (SH::ALONE) {
+      blk = blockIdx.x;
+      kh = blockIdx.y;
+      b = blockIdx.z;
+      n = p.n_nodes[b];
+      L = p.ctx_len[b];
+      off = p.kv_off[b];
+      n = n > p.max_nodes ? p.max_nodes : n;
+      if (n * p.group <= blk * kQ4Rows) return;
+      L = L < 0 ? 0 : (L > p.kv_cap ? p.kv_cap : L);
+      iters = niter = q4_iterations(n, L, p.window, p.sink);
+      u = u1;
+    } else {
+      int per_head = head_units;  // (and what divisions by it take)
+      asm volatile("" : "+s"(per_head));
+      kh = uniform(u / per_head);
+      const int in_head = u - kh * per_head;
+      // (sequences without nodes have no units: the last sequence that starts at or before the unit and has some)
+      b = 63 - __builtin_clzll(__builtin_amdgcn_ballot_w64(table[kIters][seg_lane] > 0 && table[kUnit0][seg_lane] <= in_head));
+      n = uniform(table[kNodes][b]);
+      L = uniform(table[kCtx][b]);
+      off = (long long)((unsigned long long)(unsigned)uniform(table[kOffHigh][b]) << 32 | (unsigned)uniform(table[kOffLow][b]));
+      iters = uniform(table[kIters][b]);
+      const int units = uniform(most ? q4_pieces(iters, most) : q4_units(iters));
+      const int in_seq = in_head - uniform(table[kUnit0][b]);
+      blk = uniform(in_seq / units);
+      const int at_unit = in_seq - blk * units;
+      slot = w + kh * head_blocks + uniform(table[kBlock0][b]) + blk;
+      const int share = uniform(units - at_unit < u1 - u ? units - at_unit : u1 - u);
+      u += share;
+      it0 = uniform(most ? q4_piece_begin(iters, units, at_unit) : prefix_iterations(at_unit, kPrefixOwnWeight, false));
+      niter = uniform(most ? q4_piece_begin(iters, units, at_unit + 1) : prefix_iterations(at_unit + share, kPrefixOwnWeight, false)) - it0;
+      if (niter <= 0) continue;
+    }
+    const bool whole = SH::ALONE || (it0 == 0 && niter == iters);  // (then there is nothing to join)
     if (threadIdx.x == 0 && !whole) {  // (the join need not deal the work once more)
       int* span = p.span + (((size_t)kh * p.B + b) * p.blocks + blk) * 4;
       if (it0 == 0) *(u32x2*)span = u32x2{(unsigned)(slot - w), (unsigned)w};
@@ -289,7 +335,7 @@ __global__ __launch_bounds__(64 * SH::NW, kQ4Waves) void q4_attn_kernel(Q4AttnPa
     }
     const Q4Tiles tiles = q4_tiles(L, p.window, p.sink);
     const int total = tiles.count + (n + 31) / 32;
-    const size_t row0 = ((size_t)(unsigned)uniform(table[kOffHigh][b]) << 32 | (unsigned)uniform(table[kOffLow][b])) + (size_t)kh * p.kv_cap;
+    const size_t row0 = (size_t)off + (size_t)kh * p.kv_cap;
     // codes and scales of cached tile x of the segment: of key c blocks KB h2 .., of the values blocks lane, lane + 64.  (Rows behind the last
     // one, and blocks behind a row's last, lie outside what the descriptors hold: zeros.)
     u32x4 kraw[KB], vraw[VB];
@@ -609,14 +655,14 @@ __global__ __launch_bounds__(64 * SH::NW, kQ4Waves) void q4_attn_kernel(Q4AttnPa
       }
       __syncthreads();
     }
-    if (threadIdx.x == 0) p.odd[slot] = table[kOdd][0];
+    if (!SH::ALONE && threadIdx.x == 0) p.odd[slot] = table[kOdd][0];
     // ---- what the segment leaves, in the order of the registers -------------------------------------------------------------
     if (wave == 0) {
       l_run = half_sum(l_run);
       // A block that one workgroup has whole is written by it, unless the join has infinite values of the tree, or such that are no numbers, to
       // add.  (8 sequences x 64 nodes x 32 heads behind 0, 224, 480 rows, us: 16.2, 18.9, 23.3; by way of the join 22.1, 23.3, 25.7.)
-      const bool direct = whole && uniform(table[kOdd][0]) == 0;
-      if (threadIdx.x == 0 && whole) {
+      const bool infinite = uniform(table[kOdd][0]) != 0, direct = whole && (SH::ALONE || !infinite);
+      if (!SH::ALONE && threadIdx.x == 0 && whole) {
         int* span = p.span + (((size_t)kh * p.B + b) * p.blocks + blk) * 4;
         *(u32x2*)span = u32x2{(unsigned)(slot - w), direct ? 1u : (unsigned)w};
         span[2] = direct ? 0 : w;
@@ -631,9 +677,10 @@ __global__ __launch_bounds__(64 * SH::NW, kQ4Waves) void q4_attn_kernel(Q4AttnPa
           f32x4 x[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i) x[i] = f32x4{o[dt][4 * i], o[dt][4 * i + 1], o[dt][4 * i + 2], o[dt][4 * i + 3]};
+          if (SH::ALONE && infinite) q4_add_odd(p, b, kh, node, n, 32 * dt + 4 * (el >> 5), x);
           q4_write(p, row, dt == 0 && el < 32, 32 * dt + 4 * (el >> 5), x, m_run, l_run);
         }
-      } else if (r < n * heads) {
+      } else if (!SH::ALONE && r < n * heads) {
         float* po = p.po + (size_t)slot * (DT * 1024) + el * 4;
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
@@ -714,48 +761,33 @@ __global__ __launch_bounds__(64 * SH::DT) void q4_join_kernel(Q4AttnParams p) {
   }
   if (c >= rows || share) return;
   const int node = r / p.group, hg = r - node * p.group;
-  if (odd) {  // values of tree nodes that are infinite or not a number, left out so far: into the rows that see them
-    const int len = p.ctx_len[b], L = len < 0 ? 0 : (len > p.kv_cap ? p.kv_cap : len);
-    const Q4Mask mask = q4_tree_mask(p, b, node, n, L, p.window > 0 ? q4_depth(p, b, node) : 0);
-    const unsigned short* vt = (const unsigned short*)p.v_tree + ((size_t)b * p.H_kv + kh) * p.max_nodes * p.dh;
-    for (int j = 0; j < n; ++j) {
-      if (!mask.node(j)) continue;
-#pragma unroll
-      for (int i = 0; i < OWN; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int at = 32 * dt + 8 * (part + i) + 4 * h2 + e;
-          if (at >= p.dh) continue;
-          const float v = bf16_bits_to_float(vt[(size_t)j * p.dh + at]);
-          if ((__float_as_uint(v) & 0x7f800000u) == 0x7f800000u) o[i][e] += v;
-        }
-    }
-  }
+  if (odd) q4_add_odd(p, b, kh, node, n, 32 * dt + 8 * part + 4 * h2, o);
   const size_t row = ((size_t)b * p.H + kh * p.group + hg) * p.max_nodes + node;
   q4_write(p, row, dt == 0 && part == 0 && h2 == 0, 32 * dt + 8 * part + 4 * h2, o, m, l);
 }
 
 // ---- host side -----------------------------------------------------------------------------------------------------------
 template <int DT, typename F>
-static hipError_t q4_with_precision(bool fine, F&& f) {
-  return fine ? f(Q4Shape<DT, true>{}) : f(Q4Shape<DT, false>{});
+static hipError_t q4_with_kind(bool fine, bool alone, F&& f) {
+  if (alone) return fine ? f(Q4Shape<DT, true, true>{}) : f(Q4Shape<DT, false, true>{});
+  return fine ? f(Q4Shape<DT, true, false>{}) : f(Q4Shape<DT, false, false>{});
 }
 template <typename F>
-static hipError_t q4_with_shape(int blocks, bool fine, F&& f) {
+static hipError_t q4_with_shape(int blocks, bool fine, bool alone, F&& f) {
   switch (blocks) {
-    case 1: return q4_with_precision<1>(fine, f);
-    case 2: return q4_with_precision<2>(fine, f);
-    case 3: return q4_with_precision<3>(fine, f);
-    default: return q4_with_precision<4>(fine, f);
+    case 1: return q4_with_kind<1>(fine, alone, f);
+    case 2: return q4_with_kind<2>(fine, alone, f);
+    case 3: return q4_with_kind<3>(fine, alone, f);
+    default: return q4_with_kind<4>(fine, alone, f);
   }
 }
 
 hipError_t prepare_q4_attn() {
   hipError_t e = hipSuccess;
   for (int blocks = 1; blocks <= 4; ++blocks)
-    for (int fine = 0; fine < 2; ++fine)
+    for (int kind = 0; kind < 4; ++kind)
       if (e == hipSuccess)
-        e = q4_with_shape(blocks, fine, [](auto shape) {
+        e = q4_with_shape(blocks, kind & 1, kind & 2, [](auto shape) {
           using SH = decltype(shape);
           return hipFuncSetAttribute((const void*)q4_attn_kernel<SH>, hipFuncAttributeMaxDynamicSharedMemorySize, SH::LDS);
         });
@@ -819,14 +851,18 @@ extern "C" int q4_verify_attn(ctcspec_ctx* ctx, ctcspec_dtype dt, const void* q,
   p.blocks = (int)((seq_rows + kQ4Rows - 1) / kQ4Rows);
   p.out_bf16 = out_dt == CTCSPEC_BF16; p.out = out; p.lse = lse;
   hipStream_t st = ctx->stream;
-  const hipError_t e = q4_with_shape(q4_blocks(dh), out_dt == CTCSPEC_F32, [&](auto shape) {
+  const hipError_t e = q4_with_shape(q4_blocks(dh), out_dt == CTCSPEC_F32, q4_alone(B, H_kv, seq_rows, kv_cap, max_nodes, window, sink), [&](auto shape) {
     using SH = decltype(shape);
-    hipLaunchKernelGGL(q4_attn_kernel<SH>, dim3(kQ4Groups), dim3(64 * SH::NW), SH::LDS, st, p);
-    if (const hipError_t e1 = hipGetLastError(); e1 != hipSuccess) return e1;
-    if ((long long)p.blocks * H_kv * B <= kQ4JoinFew)
-      hipLaunchKernelGGL((q4_join_kernel<SH, 4>), dim3((unsigned)(p.blocks * 4), (unsigned)H_kv, (unsigned)B), dim3(64 * SH::DT), 0, st, p);
-    else
-      hipLaunchKernelGGL((q4_join_kernel<SH, 1>), dim3((unsigned)p.blocks, (unsigned)H_kv, (unsigned)B), dim3(64 * SH::DT), 0, st, p);
+    if constexpr (SH::ALONE) {
+      hipLaunchKernelGGL(q4_attn_kernel<SH>, dim3((unsigned)p.blocks, (unsigned)H_kv, (unsigned)B), dim3(64 * SH::NW), SH::LDS, st, p);
+    } else {
+      hipLaunchKernelGGL(q4_attn_kernel<SH>, dim3(kQ4Groups), dim3(64 * SH::NW), SH::LDS, st, p);
+      if (const hipError_t e1 = hipGetLastError(); e1 != hipSuccess) return e1;
+      const bool few = (long long)p.blocks * H_kv * B <= kQ4JoinFew;
+      const dim3 grid((unsigned)(p.blocks * (few ? 4 : 1)), (unsigned)H_kv, (unsigned)B), block(64 * SH::DT);
+      if (few) hipLaunchKernelGGL((q4_join_kernel<SH, 4>), grid, block, 0, st, p);
+      else hipLaunchKernelGGL((q4_join_kernel<SH, 1>), grid, block, 0, st, p);
+    }
     return hipGetLastError();
   });
   CTCSPEC_HIP(ctx, e);

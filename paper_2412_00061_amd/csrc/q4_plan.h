@@ -45,12 +45,28 @@ CTCSPEC_BOTH constexpr int q4_piece_begin(int iters, int pieces, int i) {
   const int each = iters / pieces, more = iters - each * pieces;
   return i * each + (i < more ? i : more);
 }
-// Such pieces are the shares where they are no more than the workgroups and at most kQ4PieceSlack iterations longer than equal shares would be -
-// what a second block in a share costs -, and are not made shorter than kQ4LeastPiece.  (When every block went by way of the join: eight sequences of one length, 32 heads; us with
-// equal shares / pieces of 2 / of 4 or more.  Single tokens behind 224, 480, 992, 2048 rows: 14.8 / 13.8 / 13.8, 19.7 / 16.6 / 16.1, 20.6 /
-// 21.8 / 21.4, 29.0 / 29.9 / 29.9; 64 nodes: 25.0 / 23.1 / 23.3, 26.2 / 25.6 / 25.7, 38.0 / 33.7 / 33.3, 52.5 / 53.7 / 53.7; of
-// 256 to 2048 rows, 64 nodes: 39.6 / 36.6 / 37.4.)
+// Such pieces are the shares where they are no more than the workgroups and not much longer than equal shares would be - half as long again, and
+// kQ4PieceSlack iterations: equal shares go across blocks, and a second block in a share costs its way in and out -, and are not made shorter than
+// kQ4LeastPiece.  (us with equal shares / pieces.  Eight sequences of one length, 32 heads, single tokens behind 480, 992, 2048 rows: 19.7 / 15.8,
+// 20.6 / 21.7, 29.0 / 29.8; 64 nodes: 26.2 / 23.0, 38.0 / 31.0, 54.7 / 46.8, 256 to 2048 rows 39 / 39, windows of 4096 73 / 59.)
 constexpr int kQ4LeastPiece = 4, kQ4PieceSlack = 4;
+
+// Iterations over a sequence's keys.
+CTCSPEC_BOTH int q4_iterations(int nodes, int len, int window, int sink) {
+  return (q4_tiles(len, window, sink).count + (nodes + 31) / 32 + kQ4Tiles - 1) / kQ4Tiles;
+}
+// Whether every block of rows is one workgroup's, in a single launch: where no length makes more than kQ4AloneIterations of them, and every workgroup
+// has its place at once.  (bf16, us with a deal and a join / alone, capacities of 16, 448, 960, 1984 rows, all filled.  One sequence, 32
+// heads on 8, a node: 10.8 / 7.4, 13.1 / 10.1, 13.7 / 13.0, 14.0 / 19.3; eight 12.4 / 7.5, 14.1 / 10.1, 14.6 / 13.4, 15.3 / 19.5; with 32 key heads
+// 12.0 / 7.7, 14.2 / 10.3, 18.3 / 14.2, 24.2 / 20.9, 64 nodes 15.0 / 11.3, 18.7 / 16.2, 24.0 / 22.0, 43.3 / 32.7: beyond, short sequences
+// beside long ones would leave the card empty.)
+constexpr int kQ4AloneIterations = 8;
+inline bool q4_alone(long long B, int H_kv, long long seq_rows, int kv_cap, int max_nodes, int window, int sink) {
+  long long tiles = (kv_cap + 31LL) / 32;
+  const long long seen = (sink + 31LL) / 32 + window / 32 + 3;  // those of a window, and at its ends
+  if (window > 0 && seen < tiles) tiles = seen;
+  return tiles + (max_nodes + 31) / 32 <= kQ4AloneIterations * kQ4Tiles && B * H_kv * ((seq_rows + kQ4Rows - 1) / kQ4Rows) <= kQ4Groups;
+}
 
 // Rows, keys and units are counted in 32 bits: whether that is enough for the largest lengths.
 inline bool q4_units_fit(long long B, int H_kv, long long seq_rows, int kv_cap, int max_nodes) {

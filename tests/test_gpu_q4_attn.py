@@ -12,12 +12,12 @@ from workloads.generate import round_to_storage
 pytestmark = pytest.mark.gpu
 
 
-def make(seed, B, H, Hkv, N, dh, ctx, n_nodes, *, window=0, sink=0, spread=1.0, spikes=0):
+def make(seed, B, H, Hkv, N, dh, ctx, n_nodes, *, window=0, sink=0, spread=1.0, spikes=0, room=0):
     """Operands with room behind every length; the sequences' blocks lie in another order than they count, and what lies behind a
     sequence's length stands for NaN."""
     rng = np.random.default_rng(seed)
     f = lambda *s: round_to_storage(rng.standard_normal(s, dtype=np.float32), "bf16")  # noqa: E731
-    cap = max(ctx) + int(rng.integers(0, 5))
+    cap = max(ctx) + int(rng.integers(0, 5)) + room  # (more room: the work is dealt, where it would not be otherwise)
     c = dict(B=B, H=H, Hkv=Hkv, N=N, dh=dh, cap=cap, ctx=list(ctx), n=list(n_nodes), scale=dh ** -0.5, window=window, sink=sink)
     c["q"] = round_to_storage(f(B, H, N, dh) * np.float32(spread), "bf16")
     c["kt"], c["vt"] = f(B, Hkv, N, dh), f(B, Hkv, N, dh)
@@ -141,11 +141,12 @@ SHAPES = [
 ]
 
 
+@pytest.mark.parametrize("room", [0, 1100])
 @pytest.mark.parametrize("bf16", [False, True])
 @pytest.mark.parametrize("shape", SHAPES)
-def test_against_the_oracle(shape, bf16):
+def test_against_the_oracle(shape, bf16, room):
     import torch
-    c = make(len(str(shape)), *shape, spikes=3)
+    c = make(len(str(shape)), *shape, spikes=3, room=room)
     d, ctx = upload(c), context(c)
     dtype = torch.bfloat16 if bf16 else torch.float32
     out = {"out": torch.full((c["B"], c["H"], c["N"], c["dh"]), 55.0, dtype=dtype, device="cuda"),
@@ -165,6 +166,18 @@ def test_windows(shape, window, sink):
     d, ctx = upload(c), context(c)
     for dtype in (torch.float32, torch.bfloat16):
         check(c, call(ctx, c, d, dtype))
+    ctx.close()
+
+
+@pytest.mark.parametrize("window,sink", [(1, 0), (7, 40), (33, 5), (150, 64)])
+def test_windows_of_many_blocks(window, sink):
+    """More blocks of rows than workgroups: shares with parts of several."""
+    import torch
+    rng = np.random.default_rng(window)
+    c = make(window, 64, 13, 13, 2, 16, [int(x) for x in rng.integers(0, 300, 64)], [int(x) for x in rng.integers(0, 3, 64)], window=window, sink=sink)
+    ctx = context(c)
+    for dtype in (torch.float32, torch.bfloat16):
+        check(c, call(ctx, c, upload(c), dtype))
     ctx.close()
 
 
@@ -214,9 +227,10 @@ def test_peaked_and_far_scores():
         ctx.close()
 
 
-def test_rows_without_keys():
+@pytest.mark.parametrize("room", [0, 1100])
+def test_rows_without_keys(room):
     import torch
-    c = make(7, 3, 4, 2, 9, 64, [0, 0, 40], [9, 4, 9])
+    c = make(7, 3, 4, 2, 9, 64, [0, 0, 40], [9, 4, 9], room=room)
     c["seen"][0, 2] = c["seen"][0, 8] = c["seen"][1] = c["seen"][2, 5] = False
     ctx = context(c)
     for cap_zero in (False, True):
@@ -246,6 +260,22 @@ def test_no_numbers_in_hidden_and_seen_places(N, n, bf16):
     res = call(ctx, c, upload(c), dtype)
     check(c, res)
     assert torch.isnan(res["out"]).any() and torch.isinf(res["out"]).any() and torch.isfinite(res["out"][0, :, :2]).any()
+    ctx.close()
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+def test_no_numbers_in_dealt_shares(bf16):
+    """The same where blocks are cut to pieces, and where a workgroup has one whole beside them."""
+    import torch
+    c = make(71, 3, 4, 2, 70, 80, [1500, 61, 1100], [66, 70, 5])
+    c["vt"][0, 0, 3, 7], c["vt"][0, 1, 4, 8], c["vt"][0, 0, 65, 79] = np.inf, -np.inf, np.nan
+    c["vt"][1, 1, 40, 0], c["vt"][2, 0, 1, 33] = np.nan, np.inf
+    c["parts"][3][0, 0, 1499, 2] = c["parts"][3][1, 1, 60, 0] = 255  # blocks in the last, partial tile
+    c["seen"][0, 10:20, 3] = False
+    ctx = context(c)
+    res = call(ctx, c, upload(c), torch.bfloat16 if bf16 else torch.float32)
+    check(c, res)
+    assert torch.isinf(res["out"]).any() and torch.isnan(res["out"]).any()
     ctx.close()
 
 
@@ -282,7 +312,7 @@ def test_lengths_outside_their_range_count_as_its_ends():
 
 # ---- the calls ---------------------------------------------------------------------------------------------------
 def big(seed=1, **more):
-    return make(seed, 3, 8, 2, 40, 128, [700, 64, 350], [40, 17, 1], **more)
+    return make(seed, 3, 8, 2, 40, 128, [700, 64, 350], [40, 17, 1], **{"room": 1100 * (seed % 2), **more})
 
 
 def test_codes_beyond_32_bits():
@@ -332,11 +362,12 @@ def test_two_streams_at_once_without_a_workspace():
         ctx.close()
 
 
-def test_captured_and_replayed():
+@pytest.mark.parametrize("more", [dict(window=90, sink=6, room=0), dict(room=1100)])
+def test_captured_and_replayed(more):
     """Two calls that share a workspace in one graph; other lengths and inputs between the replays."""
     import torch
     stream = torch.cuda.Stream()
-    cases = [big(s, window=90, sink=6) for s in (3, 4, 5)]
+    cases = [big(s, **more) for s in (3, 4, 5)]
     for c in cases[1:]:  # (one shape of the buffers)
         assert c["B"] == cases[0]["B"]
         pad = cases[0]["cap"]

@@ -17,6 +17,13 @@ int main() {
     if (what == 't') {
       const Q4Tiles t = q4_tiles(a, b, c);
       printf("%d %d %d\n", t.lead, t.gap, t.count);
+    } else if (what == 'a') {  // alone, and the most iterations that a length makes
+      int most = 0;
+      for (int len = 0; len <= b; ++len) {
+        const int n = q4_iterations(c, len, d, e);
+        most = n > most ? n : most;
+      }
+      printf("%d %d 0\n", (int)q4_alone(a, 8, c, b, c, d, e), most);
     } else if (what == 'p') {
       const int pieces = q4_pieces(a, b);
       for (int i = 0; i <= pieces; ++i) printf("%d %d %d\n", pieces, i, pieces ? q4_piece_begin(a, pieces, i) : 0);
@@ -53,6 +60,16 @@ def test_a_window_keeps_every_tile_that_a_row_sees():
         seen = {j // 32 for j in range(L) if not W or j > L - W or j < S}  # (a row at a later position sees fewer)
         assert seen <= tiles <= set(range((L + 31) // 32)), (L, W, S)
         assert len(tiles) == count <= len(seen) + 1  # (a window of 1 sees no cached row, its tile is kept)
+
+
+def test_workgroups_alone_have_few_iterations_whatever_the_lengths():
+    cases = [(B, cap, n, W, S) for B in (1, 24, 200) for cap in (0, 16, 500, 896, 1024, 3000) for n in (1, 33, 128) for W, S in ((0, 0), (1, 0), (31, 5), (700, 100), (2900, 0))]
+    got = ask([("a", *c) for c in cases])
+    for (B, cap, n, W, S), (alone, most, _) in zip(cases, got):
+        assert not alone or (most <= 8 and B * 8 * -(-n // 32) <= 768), (B, cap, n, W, S)
+        if W == 0:
+            assert alone == (most <= 8 and B * 8 * -(-n // 32) <= 768)
+    assert {a for a, *_ in got} == {0, 1}
 
 
 def test_pieces_cover_a_block():
