@@ -16,6 +16,7 @@
 #include <type_traits>
 
 #include "common.h"
+#include "filter_plan.h"
 
 namespace ctcspec {
 
@@ -753,7 +754,7 @@ __device__ __forceinline__ bool sample_listed(const FilterParams& p, ListShared&
     __syncthreads();
   };
   const bool of_all = want.by_p && !want.by_k;  // top-p's share is of all tokens
-  float bound = want.by_k ? below_parts((unsigned)want.top_k) : (want.by_p ? below_parts(parts / 4 + 1) : -INFINITY);
+  float bound = want.by_k ? below_parts((unsigned)want.top_k) : (want.by_p ? below_parts(filter_parts_above(parts, 0)) : -INFINITY);
   float distance = -INFINITY;  // every token that min-p keeps is above this
   if (want.by_min && !(want.by_k && want.by_p)) {  // (top-p's share is of all top-k tokens)
     const float nats = -__logf(fminf(fmaxf(want.min_p, 1e-37f), 1.f));
@@ -795,7 +796,7 @@ __device__ __forceinline__ bool sample_listed(const FilterParams& p, ListShared&
       weighed = listed;
       if ((double)weighs >= enough || bound == -INFINITY || bound == distance) break;
       const float upto = bound;
-      bound = fmaxf(round == 1 ? below_parts(parts / 4 * 3) : (round == 2 ? below_parts(parts / 40 * 39) : -INFINITY), distance);
+      bound = filter_next_bound(upto, round < kFilterPartRounds ? below_parts(filter_parts_above(parts, round)) : -INFINITY, distance);
       list(bound, upto, [](const f32x4&) {}, std::true_type{});
       listed = sh.candidates;
     }
