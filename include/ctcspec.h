@@ -632,7 +632,8 @@ int kv_read_q4(ctcspec_ctx* ctx, const ctcspec_q4_cache* cache, const int64_t* k
  * A row that sees no key (no cached row, an empty mask row), or none whose score is above -infinity, has out = 0 and lse = -inf.  Rows
  * i >= n_nodes[b] are not written; n_nodes[b] may be 0.  No positional encoding is applied.  The lengths are read on the device; those
  * beyond their capacity count as the capacity, negative ones as 0.  A value that is infinite or not a number reaches the rows that see its
- * key and no other row; a score that is, likewise.
+ * key and no other row; a score that is, likewise.  Scores are float numbers, before and after they are scaled: of any magnitude, infinite where
+ * float ends.
  *
  * dt            element type of q, k_tree, v_tree: CTCSPEC_BF16
  * q             [B,H,max_nodes,dh]; k_tree, v_tree [B,H_kv,max_nodes,dh]

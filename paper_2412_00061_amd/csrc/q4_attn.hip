@@ -54,6 +54,9 @@ struct Q4AttnParams {
   float* lse;                     // [B][H][max_nodes] or null
 };
 
+// Up to here a weight's exponent - a scaled score less the rounded reference, in one rounding - is off by 16 at the most, by the same for all of a row.
+constexpr float kQ4Far = 536870912.f;  // 2^29
+
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 // DT: blocks of 32 components, of a row of the cache too.  FINE: weights in three bf16 parts, 24 bits together, for a float result; for a bf16 one
 // they are one bf16 each, off by 2^-9 at most as the result itself (against 64 bits the result is off by 1.8e-3 of its norm, 1.7e-3 with float
@@ -416,16 +419,27 @@ __global__ __launch_bounds__(64 * SH::NW, kQ4Waves) void q4_attn_kernel(Q4AttnPa
 #pragma unroll
       for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
       if (__builtin_amdgcn_ballot_w64(fmaf(mx, p.sl2, -m_run) > 8.0f) != 0ull) {
-        const float m = half_max(mx);
-        if (fmaf(m, p.sl2, -m_run) > 8.0f) {
-          const float top = m * p.sl2, alpha = __builtin_amdgcn_exp2f(m_run - top);  // 0 on first use
+        const float m = half_max(mx), top = m * p.sl2;
+        if (fmaf(m, p.sl2, -m_run) > 8.0f && top > m_run) {  // (not above where scaling takes every score to -infinity)
+          const float alpha = __builtin_amdgcn_exp2f(m_run - top);  // 0 on first use
           l_run *= alpha;
 #pragma unroll
           for (int dt = 0; dt < DT; ++dt) o[dt] *= alpha;
           m_run = top;
         }
       }
-      const float ms = m_run > -INFINITY ? m_run : 0.f;
+      float ms = m_run > -INFINITY ? m_run : 0.f;
+      // Far from 0 the reference is off by more than an exponential has room for.  There a score is rounded as the reference was: it is the same, with a
+      // weight of 1, or below it by 32 at the least, with none.
+      if (__builtin_amdgcn_ballot_w64(fabsf(ms) >= kQ4Far) != 0ull) {
+        const bool far = fabsf(ms) >= kQ4Far;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float scaled = s[i] * p.sl2;
+          s[i] = far ? (scaled < ms ? -INFINITY : scaled * 0.f) : s[i];  // (what is no number stays none)
+        }
+        ms = far ? 0.f : ms;
+      }
       u32x4 hi, lo, rest;
       auto weights = [&](int kb) __attribute__((always_inline)) {  // of 16 keys
 #pragma unroll
