@@ -419,7 +419,9 @@ __global__ __launch_bounds__(64 * SH::NW, kQ4Waves) void q4_attn_kernel(Q4AttnPa
 #pragma unroll
       for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
       if (__builtin_amdgcn_ballot_w64(fmaf(mx, p.sl2, -m_run) > 8.0f) != 0ull) {
-        const float m = half_max(mx), top = m * p.sl2;
+        const float m = half_max(mx);
+        float top = m * p.sl2;
+        asm volatile("" : "+v"(top));  // (rounded for the factor below as for the weights: left to itself the compiler may form one exponent from the product)
         if (fmaf(m, p.sl2, -m_run) > 8.0f && top > m_run) {  // (not above where scaling takes every score to -infinity)
           const float alpha = __builtin_amdgcn_exp2f(m_run - top);  // 0 on first use
           l_run *= alpha;

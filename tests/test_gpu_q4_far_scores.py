@@ -118,3 +118,29 @@ def test_no_numbers_beside_far_scores(bf16):
                 none = any(np.isnan(s) or s == np.inf for s in scores)
                 assert np.all(np.isnan(out[b, h, i])) if none else np.all(np.isfinite(out[b, h, i])), (b, h, i)
     ctx.close()
+
+
+@pytest.mark.parametrize("ctx_len,room", [([900, 70], 0), ([900, 70], 1100), ([6000, 3000], 0)])
+@pytest.mark.parametrize("bf16", [False, True])
+def test_references_that_move_between_large_scores(ctx_len, room, bf16):
+    """Scores near 2^20, those of the last four tiles' last keys higher by 64 (8 when scaled): what the keys before them have gathered is scaled down
+    by exactly what their weights would have been, whatever the references' roundings - half a unit of 2^-6 here."""
+    import torch
+    c = make(8, 2, 4, 2, 20, 64, ctx_len, [20, 20], room=room)
+    codes, scales = c["parts"][0], c["parts"][1]
+    codes[..., 0] = 0x02  # a first component of 1, a second one of 0
+    scales[scales != 255] = 127
+    for b, L in enumerate(ctx_len):
+        codes[b, :, [L - 1, L - 33, L - 65], 0] = 0x22  # a second one of 1
+        if L > 97:
+            codes[b, :, L - 97, 0] = 0x22
+    c["kt"][..., 0], c["kt"][..., 1] = 1.0, 0.0
+    rows = np.arange(20)
+    for b in range(2):
+        for h in range(4):
+            c["q"][b, h] = 0
+            c["q"][b, h, :, 0] = 2.0 ** 20 * (1 + (7 * rows + 29 * h + 3 * b) % 128 / 128)
+            c["q"][b, h, :, 1] = 64
+    ctx = context(c)
+    check(c, call(ctx, c, upload(c), torch.bfloat16 if bf16 else torch.float32))
+    ctx.close()
