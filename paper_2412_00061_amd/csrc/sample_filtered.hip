@@ -89,8 +89,10 @@ __device__ __forceinline__ double fma_scalar(double p, double f, double c) {
 #endif
 }
 // 2^x for x <= 0 in 64 bits: 2^f for |f| <= 1/2 by the polynomial that meets it at the ten Chebyshev nodes, within 2.1e-14 of it; its
-// constant, 1.4e-14 above 1, is 1 here, so that 2^0 is.
+// constant, 1.4e-14 above 1, is 1 here, so that 2^0 is.  (x less its integer is formed of the rounded x: beyond 2^53 it is 0, where the product that x
+// comes from may be off from it by more than a polynomial has room for.)
 __device__ __forceinline__ double exp2_64(double x) {
+#pragma clang fp contract(off)
   const double n = __builtin_rint(x), f = x - n;
   double p = __builtin_fma(f, 1.0213253744950635e-07, 1.3259724569891773e-06);
   p = fma_scalar(p, f, 1.5252635829510196e-05);
@@ -132,7 +134,10 @@ struct Filters {
 // Weights of logits above -infinity, relative to the largest.
 struct Weights {
   double mx, per;
-  __device__ __forceinline__ double operator()(float v) const { return exp2_64(((double)v - mx) * per); }
+  __device__ __forceinline__ double operator()(float v) const {
+#pragma clang fp contract(off)
+    return exp2_64(((double)v - mx) * per);
+  }
 };
 // Where the largest logit is infinite it takes all: it counts as 0, all others as -infinity.
 __device__ __forceinline__ f32x4 of_infinite(f32x4 v) {
