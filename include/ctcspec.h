@@ -588,7 +588,7 @@ typedef struct {
  * dt              element type of the rows
  * k_rows, v_rows  [B,H_kv,max_rows,dh] 16-byte aligned; rows from n_rows[b] on are not read
  * n_rows          [B] int32 device (counts beyond max_rows count as max_rows, negative ones as 0)
- * ctx_len_out     [B] int32 out or NULL; must not be the ctx_len buffer itself
+ * ctx_len_out     [B] int32 out or NULL; must not be the ctx_len, n_rows, accept_len or accept_nodes buffer itself
  *
  * kv_commit_q4 - the accepted path's keys and values join it: kv_commit for such a cache, with its arguments.  Entries of accept_nodes that
  * are no node write nothing; ctx_len_out counts their rows, as there.

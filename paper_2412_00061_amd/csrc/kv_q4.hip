@@ -185,7 +185,9 @@ extern "C" int kv_append_q4(ctcspec_ctx* ctx, ctcspec_dtype dt, const void* k_ro
   if (const int owed = flush_deferred(ctx)) return owed;
   CTCSPEC_REQUIRE(ctx, n_rows && kv_off && ctx_len, CTCSPEC_EINVAL, "kv_append_q4: null pointer");
   if (const int bad = q4_check(ctx, "kv_append_q4", dt, cache, k_rows, v_rows, kv_cap, B, H_kv, dh, max_rows)) return bad;
-  CTCSPEC_REQUIRE(ctx, ctx_len_out != ctx_len, CTCSPEC_EINVAL, "kv_append_q4: ctx_len_out must not be the ctx_len buffer");
+  // (one workgroup of a sequence writes it, others may still have to read these)
+  CTCSPEC_REQUIRE(ctx, ctx_len_out != ctx_len && ctx_len_out != n_rows, CTCSPEC_EINVAL,
+                  "kv_append_q4: ctx_len_out must not be the ctx_len or n_rows buffer");
   return q4_store(ctx, dt, k_rows, v_rows, max_rows, n_rows, nullptr, 0, cache, kv_off, ctx_len, kv_cap, B, H_kv, dh, ctx_len_out);
 }
 
@@ -199,7 +201,8 @@ extern "C" int kv_commit_q4(ctcspec_ctx* ctx, ctcspec_dtype dt, const void* k_tr
   CTCSPEC_REQUIRE(ctx, T > 0, CTCSPEC_EINVAL, "kv_commit_q4: sizes must be positive");
   CTCSPEC_REQUIRE(ctx, T <= CTCSPEC_MAX_SLOTS && max_nodes <= CTCSPEC_MAX_NODES && max_nodes <= ctx->lim.max_nodes, CTCSPEC_EUNSUPPORTED,
                   "kv_commit_q4: T <= %d, max_nodes <= %d and within the context's limits", CTCSPEC_MAX_SLOTS, CTCSPEC_MAX_NODES);
-  CTCSPEC_REQUIRE(ctx, ctx_len_out != ctx_len, CTCSPEC_EINVAL, "kv_commit_q4: ctx_len_out must not be the ctx_len buffer");
+  CTCSPEC_REQUIRE(ctx, ctx_len_out != ctx_len && ctx_len_out != accept_len && ctx_len_out != accept_nodes, CTCSPEC_EINVAL,
+                  "kv_commit_q4: ctx_len_out must not be the ctx_len, accept_len or accept_nodes buffer");
   return q4_store(ctx, dt, k_tree, v_tree, max_nodes, accept_len, accept_nodes, T, cache, kv_off, ctx_len, kv_cap, B, H_kv, dh, ctx_len_out);
 }
 
