@@ -57,3 +57,25 @@ def test_hardly_any_parts(V):
     checked(z, u, p=[0.5, 0.9, 0.99, 0.9999], ctx=ctx)
     checked(z, u, p=[0.5, 0.9, 0.99, 0.9999], m=[0.3, 0.02, 1e-3, 0.0], ctx=ctx)
     ctx.close()
+
+
+def test_borders_within_what_the_float_sum_is_off_by():
+    """top_p such that the share ends within 2^-22 of it from a token's border, on either side: 2^-22 is less than the 2^-21 that the sum in float is
+    trusted to, and more than the 2^-24 that a share rounded to float may move by.  All rows of a sequence have one share, so each has one row."""
+    V, B = 14000, 64
+    rng = np.random.default_rng(23)
+    z = (rng.standard_normal((B, 1, V)) * 0.2).astype(np.float32)
+    top_p, open_ends = [], 0
+    for b in range(B):
+        x = np.sort(z[b, 0].astype(np.float64))[::-1]
+        w = np.exp(x - x[0])
+        cum = np.cumsum(w) / w.sum()
+        border = cum[rng.integers(V // 3, V - 100)]
+        share = float(np.float32(border * (1 + (2.0 ** -22 if b % 2 else -2.0 ** -22))))
+        top_p.append(share)
+        open_ends += np.searchsorted(cum, share * (1 - 2.0 ** -21)) != np.searchsorted(cum, share * (1 + 2.0 ** -21))
+        assert np.abs(cum - share).min() > 2.0 ** -26  # (no border within the roundings of 64 bits)
+    assert open_ends == B
+    ctx = pkg.Context(max_batch=B, max_slots=1, max_topk=1, max_vocab_rows=8, max_nodes=8, max_heads=1, max_head_dim=8)
+    checked(z, rng.random((B, 1)).astype(np.float32), p=top_p, ctx=ctx)
+    ctx.close()
