@@ -226,7 +226,7 @@ int ctc_collapse_tree(ctcspec_ctx* ctx, const int32_t* topk_id, const float* top
  *                     must be a multiple of 16.
  * kv_off       [B] int64 device, ctx_len [B] int32 device (0 <= ctx_len[b] <= kv_cap)
  * n_nodes      [B] int32 device, anc_mask as written by ctc_collapse_tree
- * scale        softmax scale, normally 1/sqrt(dh)
+ * scale        softmax scale, normally 1/sqrt(dh).  Scaled scores are below 2^29 in magnitude: from about 2^31 on rows are no numbers
  * out          [B,H,max_nodes,dh] float out; rows >= n_nodes[b] are unspecified
  * Limits: dh <= CTCSPEC_MAX_HEAD_DIM and dh % 8 == 0, max_nodes <= CTCSPEC_MAX_NODES, H <= limits.
  */
@@ -472,7 +472,7 @@ int ctc_loss(ctcspec_ctx* ctx, const float* logits, const int32_t* labels, const
  * k_cache, v_cache, kv_off, ctx_len, kv_cap   as for tree_verify_attn, with [H_kv][kv_cap][dh] per sequence
  * k_tree, v_tree [B,H_kv,max_nodes,dh]
  * n_nodes, anc_mask   as for tree_verify_attn
- * scale         positive, at most 2e38
+ * scale         positive, at most 2e38; scaled scores as for tree_verify_attn
  * workspace     device scratch of at least prefix_verify_attn_workspace_bytes(B, H, H_kv, dh, max_nodes) bytes, owned by the
  *               caller, contents undefined afterwards; calls that share it must not overlap.  Bytes for some B and max_nodes
  *               serve every smaller B and max_nodes
@@ -563,7 +563,8 @@ int kv_evict(ctcspec_ctx* ctx, ctcspec_dtype dt, void* k_cache, void* v_cache, c
  *
  * The calls that fill the cache choose for s the smallest of 2 to 252 with |x| <= 7 * 2^(s - 127) in the block, for c the nearest value -
  * of two the even code; beyond 6: 6; no sign on what rounds to 0 -: x^ is off by at most 2^(s - 127) (for magnitudes up to 7 * 2^125) and
- * exact in bf16.  A block with an infinity or NaN has s = 255 and stands for NaN in all its elements.
+ * exact in bf16.  A block with an infinity or NaN has s = 255 and stands for NaN in all its elements.  Blocks written elsewhere may have any of these
+ * scale bytes; of 0, 1, 253 and 254, whose values float or bf16 hold in part only, it is not defined what the calls make.
  *
  *   k_codes, v_codes    bytes, 16-byte aligned: a sequence's block is [H_kv][kv_cap][16 * blocks]
  *   k_scales, v_scales  bytes, 4-byte aligned:  a sequence's block is [H_kv][kv_cap][blocks]
@@ -633,7 +634,7 @@ int kv_read_q4(ctcspec_ctx* ctx, const ctcspec_q4_cache* cache, const int64_t* k
  * i >= n_nodes[b] are not written; n_nodes[b] may be 0.  No positional encoding is applied.  The lengths are read on the device; those
  * beyond their capacity count as the capacity, negative ones as 0.  A value that is infinite or not a number reaches the rows that see its
  * key and no other row; a score that is, likewise.  Scores are float numbers, before and after they are scaled: of any magnitude, infinite where
- * float ends.
+ * float ends.  Values are summed up with weights of up to 2^24 before they are divided: magnitude times number of keys below 2^103.
  *
  * dt            element type of q, k_tree, v_tree: CTCSPEC_BF16
  * q             [B,H,max_nodes,dh]; k_tree, v_tree [B,H_kv,max_nodes,dh]

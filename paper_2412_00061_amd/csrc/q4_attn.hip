@@ -12,7 +12,7 @@
 // caches and windows need neither: a workgroup has a block of rows whole.
 //
 // What bounds it.  Four single tokens behind 16384 to 65536 rows (8 key heads of 128): the cache's bytes, 178 MB in 37 to 39 us (4.7 TB/s), and the join,
-// 5 us.  64 rows a sequence and key head behind 32768 rows (four sequences, 32 heads, 577 MB, 121 GFLOP): 174 to 183 us, the matrix units busy for 0.43
+// 5 us.  64 rows a sequence and key head behind 32768 rows (four sequences, 32 heads, 577 MB, of which HBM gives 1.05 times as much, 121 GFLOP): 170 to 183 us, the matrix units busy for 0.43
 // of them, the vector units for about half, and the two overlap only in part: a tile takes a wavefront 174 vector instructions beside its 16
 // matrix ones, 64 of them conversions (every block of 32 rows converts every key and value), 16 exponentials.  Short calls (8 single tokens
 // behind 256 to 2048 rows 19 to 22 us, 64-node trees 31 us with weights in three parts): the way in - lengths, shares, first tile -, segments of
@@ -59,8 +59,8 @@ constexpr float kQ4Far = 536870912.f;  // 2^29
 
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 // DT: blocks of 32 components, of a row of the cache too.  FINE: weights in three bf16 parts, 24 bits together, for a float result; for a bf16 one
-// they are one bf16 each, off by 2^-9 at most as the result itself (against 64 bits the result is off by 1.8e-3 of its norm, 1.7e-3 with float
-// weights), and a tile has 16 products instead of 32.
+// they are one bf16 each, off by 2^-8 of themselves at most, as the result itself (against 64 bits the result is off by 1.8e-3 of its norm, 1.7e-3 with float
+// weights), and a tile has 16 products instead of 32.  The sum that they are divided by, from which lse is formed, has 24 bits in both.
 // ALONE: a workgroup has a block of rows whole, there is neither a deal nor a join.
 template <int DT_, bool FINE_, bool ALONE_>
 struct Q4Shape {

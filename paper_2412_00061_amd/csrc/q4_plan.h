@@ -10,7 +10,8 @@ constexpr int kQ4Tiles = 4;  // tiles of 32 keys in an iteration: one for each w
 
 // Query rows of a workgroup (nodes of a sequence x heads that share a key head), and the workgroups that a compute unit holds at once: with
 // 32 rows the registers of three wavefronts a SIMD hold a row's result and the next tile, with 64 those of two.  (8 sequences x 64 nodes x 32
-// heads behind 256 to 2048 rows, four behind 32768, us: 64 rows and two 57 and 253, 32 and three 42 and 210 - of the kernel as it was then.)
+// heads behind 256 to 2048 rows, four behind 32768, us: 64 rows and two 57 and 253, 32 and three 42 and 210 - of a kernel that had bank conflicts and spilled
+// registers, and with codes fetched in another way: 64 rows have not been measured by themselves.)
 constexpr int kQ4Rows = 32;
 constexpr int kQ4Waves = 3;
 constexpr int kQ4Groups = 256 * kQ4Waves;
@@ -58,8 +59,10 @@ CTCSPEC_BOTH int q4_iterations(int nodes, int len, int window, int sink) {
 // Whether every block of rows is one workgroup's, in a single launch: where no length makes more than kQ4AloneIterations of them, and every workgroup
 // has its place at once.  (bf16, us with a deal and a join / alone, capacities of 16, 448, 960, 1984 rows, all filled.  One sequence, 32
 // heads on 8, a node: 10.8 / 7.4, 13.1 / 10.1, 13.7 / 13.0, 14.0 / 19.3; eight 12.4 / 7.5, 14.1 / 10.1, 14.6 / 13.4, 15.3 / 19.5; with 32 key heads
-// 12.0 / 7.7, 14.2 / 10.3, 18.3 / 14.2, 24.2 / 20.9, 64 nodes 15.0 / 11.3, 18.7 / 16.2, 24.0 / 22.0, 43.3 / 32.7: beyond, short sequences
-// beside long ones would leave the card empty.)
+// 12.0 / 7.7, 14.2 / 10.3, 18.3 / 14.2, 24.2 / 20.9, 64 nodes 15.0 / 11.3, 18.7 / 16.2, 24.0 / 22.0, 43.3 / 32.7.  Beyond, alone loses where blocks are few or
+// one length is far from the others: 17 iterations, eight sequences, bf16 and float result.  8 key heads, single tokens behind 256 to 2048 rows 14.8 / 20.7 and
+// 16.0 / 25.8; 32 key heads 22.0 / 21.7 and 24.7 / 26.6, one behind 2048 and seven behind 64 16.7 / 20.6 and 18.6 / 25.9; 64 nodes 32.0 / 28.1 and
+// 40.3 / 36.5, 22.2 / 23.1 and 24.1 / 28.5.  The limit is one for all of these, and for both results, though 256 blocks of many rows would take a higher one.)
 constexpr int kQ4AloneIterations = 8;
 inline bool q4_alone(long long B, int H_kv, long long seq_rows, int kv_cap, int max_nodes, int window, int sink) {
   long long tiles = (kv_cap + 31LL) / 32;
