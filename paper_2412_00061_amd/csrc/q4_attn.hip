@@ -12,10 +12,10 @@
 // caches and windows need neither: a workgroup has a block of rows whole.
 //
 // What bounds it.  Four single tokens behind 16384 to 65536 rows (8 key heads of 128): the cache's bytes, 178 MB in 37 to 39 us (4.7 TB/s), and the join,
-// 5 us.  64 rows a sequence and key head behind 32768 rows (four sequences, 32 heads, 577 MB, of which HBM gives 1.05 times as much, 121 GFLOP): 170 to 183 us, the matrix units busy for 0.43
-// of them, the vector units for about half, and the two overlap only in part: a tile takes a wavefront 174 vector instructions beside its 16
-// matrix ones, 64 of them conversions (every block of 32 rows converts every key and value), 16 exponentials.  Short calls (8 single tokens
-// behind 256 to 2048 rows 19 to 22 us, 64-node trees 31 us with weights in three parts): the way in - lengths, shares, first tile -, segments of
+// 5 us.  64 rows a sequence and key head behind 32768 rows (four sequences, 32 heads, 577 MB, 1.05 times that from HBM, 121 GFLOP): 170 to 183 us, the
+// matrix units busy for 0.43 of them, the vector units for about half, and the two overlap only in part: a tile takes a wavefront 174 vector instructions
+// beside its 16 matrix ones, 64 of them conversions (every block of 32 rows converts every key and value), 16 exponentials.  Short calls (8 single
+// tokens behind 256 to 2048 rows 19 to 22 us, 64-node trees 31 us with weights in three parts): the way in - lengths, shares, first tile -, segments of
 // a few iterations, and their joins.
 #include <type_traits>
 
